@@ -1,0 +1,273 @@
+"""Thin ctypes binding of the training operators (include/maestro_train.h).
+
+Argument marshalling only, in the manner of ``_native``: the tensors are checked, outputs and
+workspaces allocated where the caller passes none, and every computation runs in the HIP kernels of
+libmaestro.so on the current stream. There is no fallback.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+from typing import NamedTuple, Optional, Sequence
+
+import torch
+
+from . import _native
+from ._native import MAESTRO_BF16, MAESTRO_F32, _check, _dev, _ptr, _scratch, _shape, _stream, _workspace
+
+# Every function declared in include/maestro_train.h.
+EXPORTS = ("maestro_logprobs_workspace", "maestro_logprobs", "maestro_logprobs_grad", "maestro_layer",
+           "maestro_layer_grad_workspace", "maestro_layer_grad", "maestro_clip_gradients_workspace",
+           "maestro_clip_gradients")
+
+MAX_ALTERNATIVES = 16
+
+_DTYPE = {torch.float32: MAESTRO_F32, torch.bfloat16: MAESTRO_BF16}
+
+
+class Logprobs(NamedTuple):
+    """Outputs of ``logprobs``; ``stats`` [n][2] are the row maxima and the logs of the sums of
+    exponentials less the maximum, for ``logprobs_grad``. What was not asked for is None."""
+    logprob: Optional[torch.Tensor]
+    entropy: Optional[torch.Tensor]
+    top_id: torch.Tensor
+    top_logprob: torch.Tensor
+    stats: Optional[torch.Tensor]
+
+
+class LayerGrad(NamedTuple):
+    """Outputs of ``layer_grad``: ``x`` in the layer's type (None where not wanted), ``weight`` and
+    ``bias`` float32."""
+    x: Optional[torch.Tensor]
+    weight: torch.Tensor
+    bias: torch.Tensor
+
+
+_lib = None
+
+
+def load():
+    """libmaestro.so with the argument types of the training operators set."""
+    global _lib
+    if _lib is not None:
+        return _lib
+    lib = _native.load()
+    P, i32, i64, f32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
+    lib.maestro_logprobs_workspace.argtypes = [i64, i32, i32, i32]
+    lib.maestro_logprobs.argtypes = [i64, i32, P, i64, i32, P, i32, P, P, P, P, P, P, sz, P]
+    lib.maestro_logprobs_grad.argtypes = [i64, i32, P, i64, i32, P, P, P, P, P, P, i64, P]
+    lib.maestro_layer.argtypes = [i64, i32, i32, i32, P, P, P, i32, P, P]
+    lib.maestro_layer_grad_workspace.argtypes = [i64, i32, i32, i32]
+    lib.maestro_layer_grad.argtypes = [i64, i32, i32, i32, P, P, P, i32, P, P, P, P, sz, P]
+    lib.maestro_clip_gradients_workspace.argtypes = [i32]
+    lib.maestro_clip_gradients.argtypes = [i32, P, P, P, P, f32, P, P, sz, P]
+    for f in EXPORTS:
+        getattr(lib, f).restype = sz if f.endswith("_workspace") else ctypes.c_int
+    _lib = lib
+    return lib
+
+
+def _rows(t: torch.Tensor, name: str) -> int:
+    """dtype code of a [n][v] float32 or bfloat16 tensor whose rows are contiguous, any row stride."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    code = _DTYPE.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
+    if t.dim() != 2 or t.shape[1] < 1:
+        raise ValueError(f"{name} must be [n][v] with v >= 1")
+    if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise ValueError(f"{name} must have contiguous rows that do not overlap")
+    return code
+
+
+def _stride(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def logprobs(logits: torch.Tensor, token: Optional[torch.Tensor] = None, k: int = 0, want_entropy: bool = True,
+             want_stats: bool = True, out: Optional[Logprobs] = None, workspace: Optional[torch.Tensor] = None,
+             stream=None) -> Logprobs:
+    """maestro_logprobs: for every row of ``logits`` [n][v] (float32 or bfloat16; rows may lie in a wider
+    array) the log probability of its ``token`` (int32 [n], outside [0, v): none, 0), the entropy, the
+    ``k`` likeliest tokens with their log probabilities, and the row statistics. -inf masks a logit."""
+    lib = load()
+    dt = _rows(logits, "logits")
+    n, v = logits.shape
+    dev = logits.device
+    if not 0 <= k <= MAX_ALTERNATIVES:
+        raise ValueError(f"k must be 0 .. {MAX_ALTERNATIVES}")
+    if token is not None:
+        _shape(_dev(token, "token", torch.int32), "token", (n,))
+    if out is None:
+        f = dict(dtype=torch.float32, device=dev)
+        out = Logprobs(torch.empty(n, **f) if token is not None else None, torch.empty(n, **f) if want_entropy else None,
+                       torch.empty((n, k), dtype=torch.int32, device=dev), torch.empty((n, k), **f),
+                       torch.empty((n, 2), **f) if want_stats else None)
+    else:
+        if (out.logprob is None) != (token is None):
+            raise ValueError("logprob goes with token")
+        for t, name, shape in ((out.logprob, "logprob", (n,)), (out.entropy, "entropy", (n,)), (out.stats, "stats", (n, 2))):
+            if t is not None:
+                _shape(_dev(t, name, torch.float32), name, shape)
+        if k or out.top_id is not None:
+            _shape(_dev(out.top_id, "top_id", torch.int32), "top_id", (n, k))
+        if k or out.top_logprob is not None:
+            _shape(_dev(out.top_logprob, "top_logprob", torch.float32), "top_logprob", (n, k))
+    need = lib.maestro_logprobs_workspace(n, v, k, dt)
+    _workspace(workspace)
+    if workspace is None and need:
+        workspace = _scratch(need, dev, stream)
+    st = lib.maestro_logprobs(n, v, _ptr(logits), _stride(logits), dt, _ptr(token), k, _ptr(out.logprob),
+                              _ptr(out.entropy), _ptr(out.top_id), _ptr(out.top_logprob), _ptr(out.stats),
+                              _ptr(workspace), workspace.numel() if workspace is not None else 0, _stream(stream))
+    _check("maestro_logprobs", st)
+    return out
+
+
+def logprobs_grad(logits: torch.Tensor, token: Optional[torch.Tensor], stats: torch.Tensor,
+                  entropy: Optional[torch.Tensor], g_logprob: Optional[torch.Tensor],
+                  g_entropy: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                  stream=None) -> torch.Tensor:
+    """maestro_logprobs_grad: the gradient with respect to the logits of the sums of ``g_logprob`` times
+    the log probabilities and ``g_entropy`` times the entropies (float32 [n], either may be None), in the
+    logits' type. ``stats`` and ``entropy`` are what ``logprobs`` returned; ``out`` may be ``logits``."""
+    lib = load()
+    dt = _rows(logits, "logits")
+    n, v = logits.shape
+    if (token is None) != (g_logprob is None) or (g_logprob is None and g_entropy is None):
+        raise ValueError("g_logprob goes with token, and one of g_logprob and g_entropy is needed")
+    if g_entropy is not None and entropy is None:
+        raise ValueError("g_entropy needs the entropies")
+    if token is not None:
+        _shape(_dev(token, "token", torch.int32), "token", (n,))
+    _shape(_dev(stats, "stats", torch.float32), "stats", (n, 2))
+    for t, name in ((entropy, "entropy"), (g_logprob, "g_logprob"), (g_entropy, "g_entropy")):
+        if t is not None:
+            _shape(_dev(t, name, torch.float32), name, (n,))
+    if out is None:
+        out = torch.empty((n, v), dtype=logits.dtype, device=logits.device)
+    elif _rows(out, "out") != dt or out.shape != logits.shape:
+        raise ValueError("out must have the logits' shape and type")
+    st = lib.maestro_logprobs_grad(n, v, _ptr(logits), _stride(logits), dt, _ptr(token), _ptr(stats), _ptr(entropy),
+                                   _ptr(g_logprob), _ptr(g_entropy), _ptr(out), _stride(out), _stream(stream))
+    _check("maestro_logprobs_grad", st)
+    return out
+
+
+def _layer_shapes(x: torch.Tensor, weight: torch.Tensor):
+    code = _DTYPE.get(weight.dtype) if isinstance(weight, torch.Tensor) else None
+    if code is None:
+        raise TypeError("weight must be a float32 or bfloat16 tensor")
+    _dev(weight, "weight", weight.dtype)
+    _dev(x, "x", weight.dtype)
+    if weight.dim() != 2 or x.dim() != 2 or x.shape[1] != weight.shape[1]:
+        raise ValueError("x must be [n][d_in] and weight [d_out][d_in]")
+    return code, x.shape[0], weight.shape[1], weight.shape[0]
+
+
+def layer(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor, relu: bool = True,
+          out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """maestro_layer: y [n][d_out] = x weight^T + bias, rectified with ``relu``, in the weights' type
+    (float32 or bfloat16; bias float32). Widths are multiples of 16."""
+    lib = load()
+    dt, n, i, o = _layer_shapes(x, weight)
+    _shape(_dev(bias, "bias", torch.float32), "bias", (o,))
+    if out is None:
+        out = torch.empty((n, o), dtype=weight.dtype, device=x.device)
+    else:
+        _shape(_dev(out, "out", weight.dtype), "out", (n, o))
+    st = lib.maestro_layer(n, i, o, dt, _ptr(x), _ptr(weight), _ptr(bias), int(bool(relu)), _ptr(out), _stream(stream))
+    _check("maestro_layer", st)
+    return out
+
+
+def layer_grad(x: torch.Tensor, weight: torch.Tensor, g_z: torch.Tensor, relu_input: bool = False,
+               want_x: bool = True, out: Optional[LayerGrad] = None, workspace: Optional[torch.Tensor] = None,
+               stream=None) -> LayerGrad:
+    """maestro_layer_grad: gradients of z = x weight^T + bias given ``g_z`` [n][d_out]: those of the weights and
+    biases in float32, and with ``want_x`` the input's in the layer's type, 0 where x <= 0 with
+    ``relu_input`` (x the output of a rectified layer: the result is the gradient of that layer's z)."""
+    lib = load()
+    dt, n, i, o = _layer_shapes(x, weight)
+    _shape(_dev(g_z, "g_z", weight.dtype), "g_z", (n, o))
+    dev = x.device
+    if out is None:
+        out = LayerGrad(torch.empty((n, i), dtype=weight.dtype, device=dev) if want_x else None,
+                        torch.empty((o, i), dtype=torch.float32, device=dev),
+                        torch.empty(o, dtype=torch.float32, device=dev))
+    else:
+        if (out.x is not None) != want_x:
+            raise ValueError("out.x goes with want_x")
+        if want_x:
+            _shape(_dev(out.x, "out.x", weight.dtype), "out.x", (n, i))
+        _shape(_dev(out.weight, "out.weight", torch.float32), "out.weight", (o, i))
+        _shape(_dev(out.bias, "out.bias", torch.float32), "out.bias", (o,))
+    need = lib.maestro_layer_grad_workspace(n, i, o, dt)
+    _workspace(workspace)
+    if workspace is None and need:
+        workspace = _scratch(need, dev, stream)
+    st = lib.maestro_layer_grad(n, i, o, dt, _ptr(x), _ptr(weight), _ptr(g_z), int(bool(relu_input)), _ptr(out.x),
+                                _ptr(out.weight), _ptr(out.bias), _ptr(workspace),
+                                workspace.numel() if workspace is not None else 0, _stream(stream))
+    _check("maestro_layer_grad", st)
+    return out
+
+
+def _pointers(tensors: Sequence[torch.Tensor], name: str, like=None):
+    """Host array of the tensors' addresses; contiguous float32 or bfloat16 tensors on one GPU."""
+    out = (ctypes.c_void_p * len(tensors))()
+    for i, t in enumerate(tensors):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise TypeError(f"{name}[{i}] must be a CUDA (HIP) tensor")
+        if not t.is_contiguous():
+            raise ValueError(f"{name}[{i}] must be contiguous")
+        if t.dtype not in _DTYPE:
+            raise TypeError(f"{name}[{i}] must be float32 or bfloat16, got {t.dtype}")
+        if like is not None and (t.dtype != like[i].dtype or t.shape != like[i].shape):
+            raise ValueError(f"{name}[{i}] must have its tensor's shape and type")
+        out[i] = t.data_ptr()
+    return out
+
+
+def clip_gradients(tensors: Sequence[torch.Tensor], max_norm: float, out: Optional[Sequence[torch.Tensor]] = None,
+                   norm: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                   stream=None) -> torch.Tensor:
+    """maestro_clip_gradients: scales all ``tensors`` (float32 or bfloat16, contiguous) by max_norm / norm where
+    the norm of all their values together exceeds ``max_norm``, in place or into ``out``. Returns the
+    norm before clipping, float32 [1] on the device. A norm that is not finite scales nothing."""
+    lib = load()
+    tensors = list(tensors)
+    if not tensors:
+        raise ValueError("at least one tensor")
+    max_norm = float(max_norm)
+    if not max_norm >= 0.0:
+        raise ValueError("max_norm must not be negative or NaN")
+    ptr = _pointers(tensors, "tensors")
+    optr = None
+    if out is not None:
+        out = list(out)
+        if len(out) != len(tensors):
+            raise ValueError("one output per tensor")
+        optr = _pointers(out, "out", tensors)
+    count = len(tensors)
+    sizes = (ctypes.c_int64 * count)(*[t.numel() for t in tensors])
+    dtypes = (ctypes.c_int32 * count)(*[_DTYPE[t.dtype] for t in tensors])
+    dev = tensors[0].device
+    if norm is None:
+        norm = torch.empty(1, dtype=torch.float32, device=dev)
+    else:
+        _shape(_dev(norm, "norm", torch.float32), "norm", (1,))
+    _workspace(workspace)
+    if workspace is None:
+        workspace = _scratch(lib.maestro_clip_gradients_workspace(count), dev, stream)
+    st = lib.maestro_clip_gradients(count, ptr, optr, sizes, dtypes, max_norm, _ptr(norm), _ptr(workspace),
+                                    workspace.numel(), _stream(stream))
+    _check("maestro_clip_gradients", st)
+    return norm
+
+
+def gradient_norm(tensors: Sequence[torch.Tensor], norm: Optional[torch.Tensor] = None,
+                  workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The norm of ``clip_gradients`` alone; nothing is scaled."""
+    return clip_gradients(tensors, math.inf, None, norm, workspace, stream)
