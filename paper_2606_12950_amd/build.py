@@ -18,7 +18,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libmaestro.so")
 SOURCES = ("api.hip", "predict.hip", "predict_split.hip", "roles.hip", "route.hip", "fitness.hip", "fitness_pruned.hip", "prioritize.hip",
-           "train_api.hip", "logprobs.hip", "layers.hip", "clip.hip")
+           "train_api.hip", "logprobs.hip", "layers.hip", "layers_bf16.hip", "clip.hip")
 CALIBRATE_LIB = os.path.join(PKG, "libmaestro_calibrate.so")
 CALIBRATE_SOURCE = "calibrate.hip"
 

@@ -99,27 +99,24 @@ maestro_status grads(int64_t n, int32_t d_in, int32_t d_out, const T* x, const T
 
 maestro_status launch_layer(int64_t n, int32_t d_in, int32_t d_out, int32_t dtype, const void* x, const void* weight,
                             const float* bias, bool relu, void* y, hipStream_t stream) {
-  if (dtype == MAESTRO_F32)
-    forward_kernel<<<grid_of(n, d_out), kThreads, 0, stream>>>(n, d_in, d_out, static_cast<const float*>(x),
-                                                               static_cast<const float*>(weight), bias, relu,
-                                                               static_cast<float*>(y));
-  else
-    forward_kernel<<<grid_of(n, d_out), kThreads, 0, stream>>>(n, d_in, d_out, static_cast<const __bf16*>(x),
-                                                               static_cast<const __bf16*>(weight), bias, relu,
-                                                               static_cast<__bf16*>(y));
+  if (dtype == MAESTRO_BF16) return launch_layer_bf16(n, d_in, d_out, x, weight, bias, relu, y, stream);
+  forward_kernel<<<grid_of(n, d_out), kThreads, 0, stream>>>(n, d_in, d_out, static_cast<const float*>(x),
+                                                             static_cast<const float*>(weight), bias, relu,
+                                                             static_cast<float*>(y));
   return launch_status();
 }
 
-size_t layer_grad_workspace_bytes(int64_t, int32_t, int32_t, int32_t) { return 0; }
+size_t layer_grad_workspace_bytes(int64_t n, int32_t d_in, int32_t d_out, int32_t dtype) {
+  return dtype == MAESTRO_BF16 ? layer_grad_bf16_workspace_bytes(n, d_in, d_out) : 0;
+}
 
 maestro_status launch_layer_grad(int64_t n, int32_t d_in, int32_t d_out, int32_t dtype, const void* x,
                                  const void* weight, const void* g_z, bool relu_input, void* g_x, float* g_weight,
-                                 float* g_bias, void*, hipStream_t stream) {
-  if (dtype == MAESTRO_F32)
-    return grads(n, d_in, d_out, static_cast<const float*>(x), static_cast<const float*>(weight),
-                 static_cast<const float*>(g_z), relu_input, static_cast<float*>(g_x), g_weight, g_bias, stream);
-  return grads(n, d_in, d_out, static_cast<const __bf16*>(x), static_cast<const __bf16*>(weight),
-               static_cast<const __bf16*>(g_z), relu_input, static_cast<__bf16*>(g_x), g_weight, g_bias, stream);
+                                 float* g_bias, void* workspace, hipStream_t stream) {
+  if (dtype == MAESTRO_BF16)
+    return launch_layer_grad_bf16(n, d_in, d_out, x, weight, g_z, relu_input, g_x, g_weight, g_bias, workspace, stream);
+  return grads(n, d_in, d_out, static_cast<const float*>(x), static_cast<const float*>(weight),
+               static_cast<const float*>(g_z), relu_input, static_cast<float*>(g_x), g_weight, g_bias, stream);
 }
 
 }  // namespace maestro

@@ -22,6 +22,14 @@ maestro_status launch_layer_grad(int64_t n, int32_t d_in, int32_t d_out, int32_t
                                  const void* weight, const void* g_z, bool relu_input, void* g_x, float* g_weight,
                                  float* g_bias, void* workspace, hipStream_t stream);
 
+// the bfloat16 layers, on the matrix cores
+maestro_status launch_layer_bf16(int64_t n, int32_t d_in, int32_t d_out, const void* x, const void* weight,
+                                 const float* bias, bool relu, void* y, hipStream_t stream);
+size_t layer_grad_bf16_workspace_bytes(int64_t n, int32_t d_in, int32_t d_out);
+maestro_status launch_layer_grad_bf16(int64_t n, int32_t d_in, int32_t d_out, const void* x, const void* weight,
+                                      const void* g_z, bool relu_input, void* g_x, float* g_weight, float* g_bias,
+                                      void* workspace, hipStream_t stream);
+
 size_t clip_workspace_bytes(int32_t n_tensors);
 maestro_status launch_clip(int32_t n_tensors, void* const* tensors, void* const* out, const int64_t* sizes,
                            const int32_t* dtypes, float max_norm, float* norm, void* workspace, hipStream_t stream);
