@@ -5,13 +5,19 @@
 //   input's gradient g_x[n][i] P = weight (p contiguous)   Q = g_z (k contiguous)   k over d_out
 //   weights'         g_w[o][i] P = x      (p contiguous)   Q = g_z (q contiguous)   k over the n rows
 // A workgroup of four wavefronts makes a tile of TP x TQ of C, each wavefront 32 WP x 32 WQ of it in
-// 32x32x16 MFMAs. k advances in stages of 32; a stage's TP + TQ rows of 64 bytes come straight into LDS
-// (four buffers, three stages ahead of their use). An operand whose k is contiguous lies in LDS as
-// [p][32 k]; one whose p (or q) is contiguous as [32 k][p], and is turned by the transposing LDS read
-// (ds_read_b64_tr_b16: sixteen lanes read a 4 x 16 block row-wise and get it column-wise).
-// P's 32 rows of a block are taken in an order (tile_row_neuron) that leaves every lane runs of 8 consecutive p.
-// Workgroups are persistent: the loads of the next tile's first stages run under a tile's last
-// products and its stores.
+// 32x32x16 MFMAs. k advances in stages of kDepth (32 or 64) that come straight into LDS, kBufs buffers round. An
+// operand whose k is contiguous lies in LDS as [p][k]; one whose p (or q) is contiguous as [k][p], and
+// is turned by the transposing LDS read (ds_read_b64_tr_b16: sixteen lanes read a 4 x 16 block row-wise
+// and get it column-wise). P's 32 rows of a block are taken in an order (tile_row_neuron) that leaves every lane runs
+// of 8 consecutive p. Workgroups are persistent: the loads of the next tile's first stages run under a
+// tile's last products and its stores, and its stores under the next tile's products.
+//
+// Bound by the matrix cores on wide layers, by HBM on narrow ones. Measured: 262,139 x 1024 -> 1024
+// (0.55 TFLOP a product) activations 522 us = 1.05 PFLOP/s, input's gradient 564, weights' 505; a
+// 16,384-cubed library product reaches 1.55 on the same card, and the library's products of these shapes 555, 618
+// and 1,230 us. 512 -> 256: activations 95 us for 403 MB, input's gradient 132 us for 671 MB = 5.1 TB/s, what a copy reaches.
+#include <type_traits>
+
 #include "mlp.h"
 #include "train.h"
 
@@ -22,8 +28,6 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 constexpr int kThreads = 256;
-constexpr int kDepth = 32;           // k of a stage
-constexpr int kBufs = 4;
 
 struct Product {
   const __bf16* p;                   // P and Q and their leading dimensions (elements)
@@ -35,18 +39,41 @@ struct Product {
   int64_t items;                     // splits * tiles
 };
 
-// What becomes of C, for a run of 8 consecutive p of one q.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// Rows of a bfloat16 matrix seen through a buffer resource: accesses past its end read zeros and write nothing.
+struct Rows {
+  __amdgpu_buffer_rsrc_t rsrc;
+  __device__ __forceinline__ void init(const void* m, int64_t row0, int64_t rows, int64_t most, int64_t row_bytes) {
+    const int64_t left = rows - row0 < most ? rows - row0 : most;
+    rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(static_cast<const unsigned char*>(m)) +
+                                                 (left > 0 ? row0 * row_bytes : 0),
+                                             0, (uint32_t)(left > 0 ? left * row_bytes : 0), 0x00020000);
+  }
+  __device__ __forceinline__ u32x4 load(uint32_t off) const {
+    return __builtin_amdgcn_raw_buffer_load_b128(rsrc, off, 0, 0);
+  }
+  __device__ __forceinline__ void store(const u32x4& v, uint32_t off) const {
+    __builtin_amdgcn_raw_buffer_store_b128(v, rsrc, off, 0, 0);
+  }
+};
+
+// What becomes of C. kMasked: C is 0 wherever `x`, of C's shape, is not positive. kBias: `bias` [p] is added and,
+// with relu, negative values become 0.
 struct Forward {
+  static constexpr bool kMasked = false, kBias = true;
   const float* bias;
-  __bf16* y;
+  __bf16* c;
   int32_t relu;
 };
 struct InputGrad {
+  static constexpr bool kMasked = true, kBias = false;
   const __bf16* x;
-  __bf16* gx;
+  __bf16* c;
   int32_t relu;
 };
 struct WeightGrad {
+  static constexpr bool kBias = false;
   float* gw;                         // [splits][nq][np]
   float* gb;                         // [splits * parts][nq]
   int32_t parts;                     // workgroups (of one split and q) that share the sum over Q
@@ -67,24 +94,45 @@ __device__ __forceinline__ bf16x8 read_turned(const unsigned char* at, int step)
 }
 
 // One operand of a tile: T rows (p or q), kTurned: rows contiguous in memory instead of k.
-template <int T, bool kTurned>
+// Of this wavefront alone: at most N of its vector memory operations outstanding.
+template <int N>
+__device__ __forceinline__ void wait_own() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+  asm volatile("" ::: "memory");
+}
+
+template <int T, int kDepth, bool kTurned>
 struct Operand {
-  static constexpr int kLoads = T / 64;                     // 1 KB loads of a wavefront and stage
+  static constexpr int kLoads = T * kDepth / 2048;          // 1 KB loads of a wavefront and stage
+  static constexpr int kUnits = kDepth / 8;                 // k contiguous: 16-byte units of a row
+  static constexpr int kRows = 64 / kUnits;                 // k contiguous: rows of a load
   uint32_t off[kLoads];                                     // per lane, within the resource
-  uint32_t unit;                                            // k-contiguous: the 16-byte unit this lane loads
-  const unsigned char* base;
-  i32x4 rsrc;
-  int64_t ld2;                                              // bytes
+  uint32_t unit;                                            // k contiguous: the byte of the row this lane loads next
+  uint32_t row_bytes;                                       // k contiguous: bytes of k; turned: bytes of a row of k
+  const unsigned char* base;                                // turned: the next stage's first row
+  int64_t left;                                             // turned: rows of k from there on
+  uint32_t bytes;                                           // k contiguous: of the resource
 
   // 64-byte blocks of a turned row k are stored at block ^ turn(k), so that the four rows of a
   // transposing read lie in different banks
   static __device__ __forceinline__ int turn(int k) { return T >= 128 ? k & 3 : (k >> 1) & 1; }
+  // unit u of a row whose k is contiguous is stored at u ^ place(row): sixteen rows' reads of one unit meet all banks
+  static __device__ __forceinline__ int place(int row) { return (row / (16 / kUnits)) & (kUnits - 1); }
 
-  __device__ __forceinline__ void tile(const __bf16* m, int64_t ld, int64_t row0, int64_t rows, int64_t k0, int wave,
-                                       int lane) {
-    ld2 = ld * 2;
+  // place() goes round in 16 rows: where a load has 8, the odd ones take the other half of its values
+  static __device__ __forceinline__ uint32_t odd(int j) {
+    static_assert(kRows == 16 || (kRows == 8 && kLoads % 2 == 0), "place()'s period");
+    return kRows == 8 && j % 2 ? 64 : 0;
+  }
+
+  __device__ __forceinline__ void tile(const __bf16* m, int64_t ld, int64_t row0, int64_t rows, int64_t k0, int64_t kn,
+                                       int wave, int lane) {
+    const int64_t ld2 = ld * 2;
     if constexpr (kTurned) {
       base = reinterpret_cast<const unsigned char*>(m) + k0 * ld2;
+      left = kn;
+      row_bytes = (uint32_t)ld2;
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) {
         const int o = 1024 * (wave * kLoads + j) + 16 * lane, k = o / (2 * T), slot = o % (2 * T) / 16;
@@ -92,33 +140,44 @@ struct Operand {
       }
     } else {
       base = reinterpret_cast<const unsigned char*>(m) + row0 * ld2;
-      const int64_t left = rows - row0;
-      rsrc = buffer_rsrc(base, (uint32_t)((left < T ? left : T) * ld2));
-      unit = ((lane & 3) ^ ((lane >> 4) & 3)) << 4;
+      bytes = (uint32_t)((rows - row0 < T ? rows - row0 : T) * ld2);
+      row_bytes = (uint32_t)(kn * 2);
+      unit = ((lane % kUnits) ^ place(lane / kUnits)) << 4;
 #pragma unroll
-      for (int j = 0; j < kLoads; ++j) off[j] = (uint32_t)((16 * (wave * kLoads + j) + (lane >> 2)) * ld2) + unit;
+      for (int j = 0; j < kLoads; ++j)
+        off[j] = (uint32_t)((kRows * (wave * kLoads + j) + lane / kUnits) * ld2) + (unit ^ odd(j));
     }
   }
-  // stage s of k_n values of k in all, into the buffer at LDS address lds (uniform)
-  __device__ __forceinline__ void fetch(int64_t s, int64_t k_n, uint32_t lds, int wave) {
-    const int64_t left = k_n - s * kDepth;                  // <= 0: past the end, nothing is read
+  // no tile: the loads read nothing
+  __device__ __forceinline__ void none() {
+    left = 0;
+    bytes = 0;
+  }
+  // the next stage, into the buffer at LDS address lds (uniform)
+  __device__ __forceinline__ void fetch(uint32_t lds, int wave) {
     const uint32_t at = __builtin_amdgcn_readfirstlane(lds + 1024 * kLoads * wave);
     if constexpr (kTurned) {
-      const i32x4 r = buffer_rsrc(base + (left > 0 ? s * kDepth * ld2 : 0),
-                                  left > 0 ? (uint32_t)((left < kDepth ? left : kDepth) * ld2) : 0);
+      const i32x4 r = buffer_rsrc(base, (uint32_t)(left < kDepth ? left < 0 ? 0 : left : kDepth) * row_bytes);
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) dma16(r, off[j], 0, at, 1024 * j);
+      base += kDepth * row_bytes;
+      left -= kDepth;
     } else {
-      const bool in = (int64_t)unit < left * 2;
+      const i32x4 r = buffer_rsrc(base, bytes);
 #pragma unroll
-      for (int j = 0; j < kLoads; ++j) dma16(rsrc, in ? off[j] + (uint32_t)(s * 64) : 0x80000000u, 0, at, 1024 * j);
+      for (int j = 0; j < kLoads; ++j) {
+        dma16(r, (unit ^ odd(j)) < row_bytes ? off[j] : 0x80000000u, 0, at, 1024 * j);
+        off[j] += 2 * kDepth;
+      }
+      unit += 2 * kDepth;
     }
   }
 };
 
 // LDS offsets of a lane's fragments in an operand's stage: block b (of 32 rows) of the wavefront's, k half kk.
-template <int T, bool kTurned, int W, bool kPermuted>
+template <int T, int kDepth, bool kTurned, int W, bool kPermuted>
 struct Fragments {
+  using Op = Operand<T, kDepth, kTurned>;
   int at[kTurned ? W : 1];
   __device__ __forceinline__ void init(int block0, int lane) {
     const int r = lane & 31, h = lane >> 5;
@@ -129,71 +188,138 @@ struct Fragments {
       const int k = 8 * h + (s >> 2);
 #pragma unroll
       for (int b = 0; b < W; ++b)
-        at[b] = k * 2 * T + 64 * ((block0 + b) ^ Operand<T, true>::turn(k)) + 8 * c;
+        at[b] = k * 2 * T + 64 * ((block0 + b) ^ Op::turn(k)) + 8 * c;
     } else {
       const int row = 32 * block0 + (kPermuted ? tile_row_neuron(r) : r);
-      at[0] = row * 64 + ((h ^ ((row >> 2) & 3)) << 4);
+      at[0] = row * 2 * kDepth + ((h ^ Op::place(row)) << 4);
     }
   }
-  __device__ __forceinline__ void read(const unsigned char* stage, int kk, bf16x8 (&f)[W]) const {
+  __device__ __forceinline__ void read(const unsigned char* stage, int kk, bf16x8 (&f)[W], int first = 0,
+                                       int end = W) const {
 #pragma unroll
-    for (int b = 0; b < W; ++b) {
+    for (int b = first; b < end; ++b) {
       if constexpr (kTurned) f[b] = read_turned(stage + at[b] + kk * 16 * 2 * T, 4 * 2 * T);
-      else f[b] = *reinterpret_cast<const bf16x8*>(stage + (at[0] ^ (kk * 32)) + b * 32 * 64);
+      else f[b] = *reinterpret_cast<const bf16x8*>(stage + (at[0] ^ (kk * 32)) + b * 32 * 2 * kDepth);
     }
   }
 };
+
+template <class Out>
+__device__ __forceinline__ int32_t parts_of(const Out& out) {
+  if constexpr (std::is_same<Out, WeightGrad>::value) return out.parts;
+  else return 1;
+}
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
   const f32x2 f = {a, b};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));
 }
 
-__device__ __forceinline__ void store8(__bf16* at, const float (&c)[8]) {
-  *reinterpret_cast<uint4*>(at) = make_uint4(pack2(c[0], c[1]), pack2(c[2], c[3]), pack2(c[4], c[5]), pack2(c[6], c[7]));
+// eight consecutive values rounded
+__device__ __forceinline__ u32x4 pack8(const float (&v)[8]) {
+  return u32x4{pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])};
 }
 
-// what a run of 8 consecutive p needs for every q: the biases
-__device__ __forceinline__ void begin(const Forward& e, int64_t p, float (&b)[8]) {
-  const float4 b0 = *reinterpret_cast<const float4*>(e.bias + p), b1 = *reinterpret_cast<const float4*>(e.bias + p + 4);
-  b[0] = b0.x, b[1] = b0.y, b[2] = b0.z, b[3] = b0.w, b[4] = b1.x, b[5] = b1.y, b[6] = b1.z, b[7] = b1.w;
+// the bfloat16 pair c where the pair x is positive
+__device__ __forceinline__ uint32_t where_positive(uint32_t c, uint32_t x) {
+  const float lo = __uint_as_float(x << 16), hi = __uint_as_float(x & 0xFFFF0000u);
+  return c & ((lo > 0.0f ? 0xFFFFu : 0u) | (hi > 0.0f ? 0xFFFF0000u : 0u));
 }
-template <class Out>
-__device__ __forceinline__ void begin(const Out&, int64_t, float (&)[8]) {}
 
-__device__ __forceinline__ void finish(const Forward& e, const Product& g, int64_t q, int64_t p, int64_t,
-                                       const float (&b)[8], float (&c)[8]) {
+// max(., 0) of a bfloat16 pair; a NaN stays one
+__device__ __forceinline__ uint32_t rectify(uint32_t c) {
+  const float lo = __uint_as_float(c << 16), hi = __uint_as_float(c & 0xFFFF0000u);
+  return c & ((lo < 0.0f ? 0u : 0xFFFFu) | (hi < 0.0f ? 0u : 0xFFFF0000u));
+}
+
+// A wavefront's 32 WP x 32 WQ part of C in bfloat16, by way of LDS, so that memory sees whole lines: a lane holds
+// runs of 8 p (16 bytes) of one q and leaves them at their place in [32 q][32 WS p]; then 4 WS lanes take a
+// row together. Units of 16 bytes are stored at unit ^ place(q): neither access meets bank conflicts. Every
+// wavefront issues 2 WP WQ stores, whatever lies outside C: the main loop's waits count them.
+template <int WP>
+struct Staging {
+  static constexpr int WS = WP < 4 ? 1 : 2;                 // blocks of 32 p at a time
+  static constexpr int kRowBytes = 64 * WS, kUnits = 4 * WS, kRows = 64 / kUnits;
+  static constexpr int kBytes = 32 * kRowBytes;             // of a wavefront
+  static __device__ __forceinline__ int place(int q) { return (q / (16 / kUnits)) & (kUnits - 1); }
+};
+
+template <int WP, int WQ, class Out>
+__device__ __forceinline__ void store_rows(const Out& out, const Product& g, unsigned char* staging, int64_t q0, int64_t p0,
+                                           int lane, const f32x16 (&acc)[WP][WQ]) {
+  using S = Staging<WP>;
+  constexpr int kStores = 32 / S::kRows;                    // of one q block and WS p blocks
+  const int r = lane & 31, h = lane >> 5;
+  const int row0 = lane / S::kUnits, unit0 = lane % S::kUnits;
+  const uint32_t ld = (uint32_t)g.np * 2, step = S::kRows * ld;
+  Rows c, x;
+  c.init(out.c, q0, g.nq, 32 * WQ, ld);
+  uint32_t at[WP / S::WS];                                  // of the first row's unit, outside C: past the resource
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    c[i] += b[i];
-    c[i] = e.relu && c[i] < 0.0f ? 0.0f : c[i];
+  for (int w = 0; w < WP / S::WS; ++w) {
+    const int64_t p = p0 + 32 * S::WS * w + 8 * unit0;
+    at[w] = p < g.np ? (uint32_t)(row0 * ld + p * 2) : 0x80000000u;
   }
-  store8(e.y + q * g.np + p, c);
-}
-
-__device__ __forceinline__ void finish(const InputGrad& e, const Product& g, int64_t q, int64_t p, int64_t,
-                                       const float (&)[8], float (&c)[8]) {
-  if (e.relu) {
-    const bf16x8 x = *reinterpret_cast<const bf16x8*>(e.x + q * g.np + p);
+  u32x4 xv[WP / S::WS][kStores];
+  const bool relu = out.relu;
+  if constexpr (Out::kMasked) {
+    x.init(out.x, q0, g.nq, 32 * WQ, relu ? ld : 0);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) c[i] = (float)x[i] > 0.0f ? c[i] : 0.0f;
+    for (int w = 0; w < WP / S::WS; ++w)
+#pragma unroll
+      for (int j = 0; j < kStores; ++j) xv[w][j] = x.load(at[w] + j * step);
   }
-  store8(e.gx + q * g.np + p, c);
+#pragma unroll
+  for (int b = 0; b < WQ; ++b) {
+#pragma unroll
+    for (int w = 0; w < WP / S::WS; ++w) {
+#pragma unroll
+      for (int a = 0; a < S::WS; ++a)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = acc[w * S::WS + a][b][8 * half + e];
+          *reinterpret_cast<u32x4*>(staging + r * S::kRowBytes + (((4 * a + 2 * half + h) ^ S::place(r)) << 4)) = pack8(v);
+        }
+      u32x4 v[kStores];
+#pragma unroll
+      for (int j = 0; j < kStores; ++j) {
+        const int row = j * S::kRows + row0;
+        v[j] = *reinterpret_cast<const u32x4*>(staging + row * S::kRowBytes + ((unit0 ^ S::place(row)) << 4));
+      }
+      if constexpr (!Out::kMasked) {
+        if (relu)
+#pragma unroll
+          for (int j = 0; j < kStores; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[j][e] = rectify(v[j][e]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < kStores; ++j) {
+          if (relu)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[j][e] = where_positive(v[j][e], xv[w][j][e]);
+          if (b + 1 < WQ) xv[w][j] = x.load(at[w] + ((b + 1) * kStores + j) * step);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kStores; ++j) c.store(v[j], at[w] + (b * kStores + j) * step);
+      asm volatile("" ::: "memory");                        // one block's values at a time: registers
+    }
+  }
 }
 
-__device__ __forceinline__ void finish(const WeightGrad& e, const Product& g, int64_t q, int64_t p, int64_t split,
-                                       const float (&)[8], float (&c)[8]) {
-  float* at = e.gw + (split * g.nq + q) * g.np + p;
-  *reinterpret_cast<float4*>(at) = make_float4(c[0], c[1], c[2], c[3]);
-  *reinterpret_cast<float4*>(at + 4) = make_float4(c[4], c[5], c[6], c[7]);
-}
-
-template <int WP, int WQ, int NP, int NQ, bool kPT, bool kQT, class Out>
+template <int WP, int WQ, int kDepth, int kBufs, bool kPT, bool kQT, class Out>
 __global__ __launch_bounds__(kThreads, WP * WQ > 8 ? 1 : WP * WQ > 2 ? 2 : 4) void product_kernel(Product g, Out out) {
-  static_assert(NP * NQ == 4, "four wavefronts");
+  constexpr int NP = 2, NQ = 2;                             // four wavefronts
   constexpr int TP = 32 * WP * NP, TQ = 32 * WQ * NQ;
-  constexpr int kStage = (TP + TQ) * 64, kLoads = TP / 64 + TQ / 64;
+  constexpr int kStage = (TP + TQ) * 2 * kDepth, kLoads = (TP + TQ) * kDepth / 2048, kHalves = kDepth / 16;
+  constexpr int kQ = TP * 2 * kDepth;                       // Q's place in a stage
   constexpr bool kSums = kQT;                               // the weights' gradient sums Q too (the biases')
+  constexpr int kBiasLoads = Out::kBias ? (WP + 1) / 2 : 0;
+  constexpr int kStores = kSums ? 0 : 2 * WP * WQ + kBiasLoads;      // between two tiles, exactly
+  static_assert(kLoads * (kBufs - 2) + kStores < 64, "vmcnt range");
   extern __shared__ unsigned char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wp = wave % NP, wq = wave / NP;
@@ -221,158 +347,209 @@ __global__ __launch_bounds__(kThreads, WP * WQ > 8 ? 1 : WP * WQ > 2 ? 2 : 4) vo
     return t;
   };
 
-  Operand<TP, kPT> op;
-  Operand<TQ, kQT> oq;
-  int64_t fetch_item = first, fetch_stage = 0, fetch_kn = 0, fetch_stages = 0;
+  Operand<TP, kDepth, kPT> op;
+  Operand<TQ, kDepth, kQT> oq;
+  int64_t fetch_item = first, fetch_left = 0;               // the tile being loaded, and its stages still to load
   auto open = [&]() {
-    if (fetch_item >= last) {                               // no more tiles: loads that read nothing
-      fetch_kn = 0;
-      fetch_stages = INT64_MAX;
+    if (fetch_item >= last) {
+      op.none();
+      oq.none();
+      fetch_left = INT64_MAX;
       return;
     }
     const Item t = item(fetch_item);
-    op.tile(g.p, g.ldp, t.p0, g.np, t.k0, wave, lane);
-    oq.tile(g.q, g.ldq, t.q0, g.nq, t.k0, wave, lane);
-    fetch_kn = t.kn;
-    fetch_stages = t.stages;
+    op.tile(g.p, g.ldp, t.p0, g.np, t.k0, t.kn, wave, lane);
+    oq.tile(g.q, g.ldq, t.q0, g.nq, t.k0, t.kn, wave, lane);
+    fetch_left = t.stages;
   };
   const uint32_t lds0 = lds_addr(lds);
-  auto fetch = [&](int buf) {
-    op.fetch(fetch_stage, fetch_kn, lds0 + buf * kStage, wave);
-    oq.fetch(fetch_stage, fetch_kn, lds0 + buf * kStage + TP * 64, wave);
-    if (++fetch_stage == fetch_stages) {
-      fetch_stage = 0;
+  auto fetched = [&]() {
+    if (--fetch_left == 0) {
       fetch_item += step;
       open();
     }
   };
 
-  Fragments<TP, kPT, WP, true> fp;
-  Fragments<TQ, kQT, WQ, false> fq;
+  Fragments<TP, kDepth, kPT, WP, true> fp;
+  Fragments<TQ, kDepth, kQT, WQ, false> fq;
   fp.init(wp * WP, lane);
   fq.init(wq * WQ, lane);
 
+  // this wavefront's biases of item j, into LDS a tile ahead of their use; two places in turn
+  float* biases = reinterpret_cast<float*>(lds + kBufs * kStage + 4 * Staging<WP>::kBytes) + wave * 128 * kBiasLoads;
+  int parity = 0;
+  auto fetch_biases = [&](int64_t j) {
+    if constexpr (Out::kBias) {
+      const int64_t pw = item(j).p0 + 32 * WP * wp;
+      const i32x4 r = buffer_rsrc(out.bias, j < last ? (uint32_t)(g.np * 4) : 0);
+#pragma unroll
+      for (int l = 0; l < kBiasLoads; ++l)
+        dma4(r, (uint32_t)(pw + 64 * l + lane) * 4,
+             __builtin_amdgcn_readfirstlane(lds_addr(biases + (parity ? 64 * kBiasLoads : 0)) + 256 * l));
+    }
+  };
+  fetch_biases(first);
+
   open();
 #pragma unroll
-  for (int b = 0; b < kBufs; ++b) fetch(b);
+  for (int b = 0; b < kBufs; ++b) {
+    op.fetch(lds0 + b * kStage, wave);
+    oq.fetch(lds0 + b * kStage + kQ, wave);
+    fetched();
+  }
   wait_loads<kLoads * (kBufs - 1)>();
 
-  bf16x8 p0[WP], q0[WQ], p1[WP], q1[WQ];
-  fp.read(lds, 0, p0);
-  fq.read(lds + TP * 64, 0, q0);
+  bf16x8 pf[2][WP], qf[2][WQ];                              // this step's fragments and the next one's
+  fp.read(lds, 0, pf[0]);
+  fq.read(lds + kQ, 0, qf[0]);
   int buf = 0;
+#pragma clang loop unroll(disable)
   for (int64_t i = first; i < last; i += step) {
     const Item t = item(i);
-    f32x16 acc[WP][WQ] = {};
-    float sums[kSums ? WQ : 1] = {};
-    int64_t mine = 0;                                       // the next stage whose Q this workgroup sums
-    int64_t parts = 1;
-    if constexpr (kSums) {
-      parts = out.parts;
-      mine = t.p0 / TP;
+    f32x16 acc[WP][WQ];
+    if constexpr (Out::kBias) {                             // the sums begin with the biases
+      const float* bias = biases + (parity ? 64 * kBiasLoads : 0) + 8 * (lane >> 5);
+      parity ^= 1;
+#pragma unroll
+      for (int a = 0; a < WP; ++a)
+#pragma unroll
+        for (int b = 0; b < WQ; ++b)
+#pragma unroll
+          for (int v = 0; v < 16; v += 4) {
+            const float4 f = *reinterpret_cast<const float4*>(bias + 32 * a + 2 * (v & 8) + (v & 4));
+            acc[a][b][v] = f.x, acc[a][b][v + 1] = f.y, acc[a][b][v + 2] = f.z, acc[a][b][v + 3] = f.w;
+          }
+      fetch_biases(i + step);
+    } else {
+#pragma unroll
+      for (int a = 0; a < WP; ++a)
+#pragma unroll
+        for (int b = 0; b < WQ; ++b)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) acc[a][b][v] = 0.0f;
     }
+    float sums[kSums ? WQ : 1] = {};
+    // the sum over Q's k (the biases' gradient): a stage's by one of the workgroups with these rows of Q,
+    // half of k by each of the wavefronts
+    const int64_t turns = parts_of(out);
+    int64_t mine = kSums ? t.p0 / TP : INT64_MAX;
+#pragma clang loop unroll(disable)                            // nor peel: copies of 256 accumulators
     for (int64_t s = 0; s < t.stages; ++s) {
       const unsigned char* stage = lds + buf * kStage;
-      fp.read(stage, 1, p1);
-      fq.read(stage + TP * 64, 1, q1);
+      uint32_t into = 0;
 #pragma unroll
-      for (int a = 0; a < WP; ++a)
+      for (int kk = 0; kk < kHalves; ++kk) {
+        // One step of 16 k. The next step's fragments are read, and with the stage's last one the loads of a
+        // later stage issued, between the products: a wavefront has its SIMD's matrix core to itself
+        // (256 x 256), so what is not between two products is a gap.
+        const bool end = kk == kHalves - 1;
+        bf16x8(&pc)[WP] = pf[kk & 1], (&pn)[WP] = pf[1 - (kk & 1)];
+        bf16x8(&qc)[WQ] = qf[kk & 1], (&qn)[WQ] = qf[1 - (kk & 1)];
+        if constexpr (kSums) {
+          if (kk % 2 && s == mine) {                        // steps kk - 1 and kk: one for each wavefront
 #pragma unroll
-        for (int b = 0; b < WQ; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(p0[a], q0[b], acc[a][b], 0, 0, 0);
-      if constexpr (kSums) {
-        if (s == mine) {                                    // wavefronts of the same Q rows take a half each
-          mine += parts;
+            for (int b = 0; b < WQ; ++b) {
+              const u32x4 v = wp ? __builtin_bit_cast(u32x4, qc[b]) : __builtin_bit_cast(u32x4, qn[b]);
 #pragma unroll
-          for (int b = 0; b < WQ; ++b) {
-            if (NP == 1 || wp == 0)
-#pragma unroll
-              for (int e = 0; e < 8; ++e) sums[b] += (float)q0[b][e];
-            if (NP == 1 || wp == 1)
-#pragma unroll
-              for (int e = 0; e < 8; ++e) sums[b] += (float)q1[b][e];
-          }
-        }
-      }
-      wait_loads<kLoads * (kBufs - 2)>();                   // the next stage is there, this one read by all
-      fetch(buf);
-      buf = (buf + 1) & (kBufs - 1);
-      fp.read(lds + buf * kStage, 0, p0);
-      fq.read(lds + buf * kStage + TP * 64, 0, q0);
-#pragma unroll
-      for (int a = 0; a < WP; ++a)
-#pragma unroll
-        for (int b = 0; b < WQ; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(p1[a], q1[b], acc[a][b], 0, 0, 0);
-    }
-    const int r = lane & 31, h = lane >> 5;
-#pragma unroll
-    for (int a = 0; a < WP; ++a) {
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        asm volatile("" ::: "memory");                      // one run's loads at a time: registers
-        const int64_t p = t.p0 + 32 * (wp * WP + a) + 16 * half + 8 * h;
-        if (p < g.np) {
-          float bias[8];
-          begin(out, p, bias);
-#pragma unroll
-          for (int b = 0; b < WQ; ++b) {
-            const int64_t q = t.q0 + 32 * (wq * WQ + b) + r;
-            if (q < g.nq) {
-              float c[8];
-#pragma unroll
-              for (int e = 0; e < 8; ++e) c[e] = acc[a][b][8 * half + e];
-              finish(out, g, q, p, t.split, bias, c);
+              for (int e = 0; e < 4; ++e)
+                sums[b] += __uint_as_float(v[e] << 16) + __uint_as_float(v[e] & 0xFFFF0000u);
             }
+            if (end) mine += turns;
           }
         }
+        if (end) {
+          // The next stage is there, and this one read by all. Vector memory operations complete in order:
+          // for the first stages after a tile's stores, those are newer than the loads waited for.
+          if (kStores && s < kBufs - 1 && i != first) wait_loads<kLoads * (kBufs - 2) + kStores>();
+          else wait_loads<kLoads * (kBufs - 2)>();
+          into = lds0 + buf * kStage;
+          buf = buf == kBufs - 1 ? 0 : buf + 1;
+          stage = lds + buf * kStage;
+        }
+        const int to = end ? 0 : kk + 1;
+#pragma unroll
+        for (int a = 0; a < WP; ++a) {
+          if (a == 0) fq.read(stage + kQ, to, qn);
+          if (WP < 4 ? a == 0 : a == 1 || a == 2) fp.read(stage, to, pn, WP < 4 ? 0 : 2 * a - 2, WP < 4 ? WP : 2 * a);
+          if (end && a == 0) op.fetch(into, wave);
+          if (end && a == WP / 2) oq.fetch(into + kQ, wave);
+#pragma unroll
+          for (int b = 0; b < WQ; ++b)
+            acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(pc[a], qc[b], acc[a][b], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
+      fetched();
     }
-    if constexpr (kSums) {
-      // NP wavefronts and `parts` workgroups hold shares of the sum over Q
-      const int64_t part = t.p0 / TP;
+    if (Out::kBias && t.stages < kBufs) wait_own<0>();      // else a stage's wait has covered the next biases
+    const int64_t qw = t.q0 + 32 * WQ * wq, pw = t.p0 + 32 * WP * wp;        // this wavefront's part
+    if constexpr (!kSums) {
+      store_rows<WP, WQ>(out, g, lds + kBufs * kStage + wave * Staging<WP>::kBytes, qw, pw, lane, acc);
+    } else {
+      const int r = lane & 31, h = lane >> 5;
 #pragma unroll
       for (int b = 0; b < WQ; ++b) {
-        const int64_t q = t.q0 + 32 * (wq * WQ + b) + r;
+        const int64_t q = qw + 32 * b + r;
+#pragma unroll
+        for (int a = 0; a < WP; ++a)
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const int64_t p = pw + 32 * a + 16 * half + 8 * h;
+            float* at = out.gw + (t.split * g.nq + q) * g.np + p;
+            if (q < g.nq && p < g.np) {
+#pragma unroll
+              for (int e = 0; e < 2; ++e)
+                reinterpret_cast<float4*>(at)[e] = make_float4(acc[a][b][8 * half + 4 * e], acc[a][b][8 * half + 4 * e + 1],
+                                                               acc[a][b][8 * half + 4 * e + 2], acc[a][b][8 * half + 4 * e + 3]);
+            }
+          }
+        // NP wavefronts and `parts` workgroups hold shares of the sum over Q
         const float s = sums[b] + __shfl_xor(sums[b], 32);
-        if (h == 0 && q < g.nq) out.gb[((t.split * out.parts + part) * NP + wp) * g.nq + q] = s;
+        if (h == 0 && q < g.nq) out.gb[((t.split * out.parts + t.p0 / TP) * NP + wp) * g.nq + q] = s;
       }
     }
   }
   wait_loads<0>();                                          // no load into LDS outlives the workgroup
 }
 
-// g_w and g_b from their shares, summed in order
+// g_w and g_b from their shares, summed in order. The loads of eight shares are issued before the first is added.
 __global__ __launch_bounds__(kThreads) void join_kernel(const float* gw_parts, int32_t n_gw, float* gw, int64_t size,
                                                         const float* gb_parts, int32_t n_gb, float* gb, int32_t d_out) {
-  const int64_t quads = n_gw != 1 ? size / 4 : 0, all = quads + d_out;      // one share is g_w itself
+  const int64_t quads = n_gw != 1 ? size / 4 : 0, all = quads + d_out / 4;      // one share is g_w itself
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < all; i += (int64_t)gridDim.x * kThreads) {
-    if (i < quads) {
-      float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      for (int32_t j = 0; j < n_gw; ++j) {
-        const float4 a = reinterpret_cast<const float4*>(gw_parts + j * size)[i];
-        s.x += a.x, s.y += a.y, s.z += a.z, s.w += a.w;
-      }
-      reinterpret_cast<float4*>(gw)[i] = s;
-    } else {
-      const int64_t c = i - quads;
-      float s = 0.0f;
-      for (int32_t j = 0; j < n_gb; ++j) s += gb_parts[(int64_t)j * d_out + c];
-      gb[c] = s;
+    const bool w = i < quads;
+    const float4* at = w ? reinterpret_cast<const float4*>(gw_parts) + i : reinterpret_cast<const float4*>(gb_parts) + (i - quads);
+    const int64_t step = w ? size / 4 : d_out / 4;
+    const int32_t n = w ? n_gw : n_gb;
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    int32_t j = 0;
+    for (; j + 8 <= n; j += 8) {
+      float4 a[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) a[u] = at[(j + u) * step];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s.x += a[u].x, s.y += a[u].y, s.z += a[u].z, s.w += a[u].w;
     }
+    for (; j < n; ++j) {
+      const float4 a = at[j * step];
+      s.x += a.x, s.y += a.y, s.z += a.z, s.w += a.w;
+    }
+    (w ? reinterpret_cast<float4*>(gw) + i : reinterpret_cast<float4*>(gb) + (i - quads))[0] = s;
   }
 }
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int64_t kCus = 256;
 
-template <int WP, int WQ, int NP, int NQ, bool kPT, bool kQT, class Out>
+template <int WP, int WQ, int kDepth, int kBufs, bool kPT, bool kQT, class Out>
 maestro_status launch(Product g, const Out& out, hipStream_t stream) {
-  constexpr int TP = 32 * WP * NP, TQ = 32 * WQ * NQ;
-  constexpr int kLds = kBufs * (TP + TQ) * 64;
-  constexpr int64_t kResident = kLds > 81920 ? 1 : kLds > 40960 ? 2 : 4;     // workgroups of a CU
+  constexpr int TP = 64 * WP, TQ = 64 * WQ;
+  constexpr int kLds = kBufs * (TP + TQ) * 2 * kDepth + (kQT ? 0 : 4 * Staging<WP>::kBytes) + (Out::kBias ? 2 * 4 * ((WP + 1) / 2) * 256 : 0);
+  constexpr int64_t kResident = WP * WQ > 8 ? 1 : WP * WQ > 2 ? 2 : 4;     // workgroups of a CU
   g.p_tiles = (int32_t)cdiv(g.np, TP);
   g.splits = (int32_t)cdiv(g.nk, g.k_split);
   g.items = cdiv(g.nq, TQ) * g.p_tiles * g.splits;
-  const auto kernel = product_kernel<WP, WQ, NP, NQ, kPT, kQT, Out>;
+  const auto kernel = product_kernel<WP, WQ, kDepth, kBufs, kPT, kQT, Out>;
   if (kLds > 65536 &&
       hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kLds) != hipSuccess)
     return MAESTRO_ERR_LAUNCH;
@@ -381,40 +558,48 @@ maestro_status launch(Product g, const Out& out, hipStream_t stream) {
   return launch_status();
 }
 
-// Tiles of 256 x 256 keep the matrix cores fed best; smaller ones where 256 x 256 would leave CUs idle or most
-// of a tile outside the product.
+// Tile of the activations and the input's gradient. A wavefront of a 256 x 256 tile reads half a KB of LDS for a
+// product, of a 128 x 128 tile one, of a 64 x 64 tile two; but each size needs its tiles to be many: two
+// rounds of workgroups or more, one for 128. Measured (us, tile 256 / 128 / 64): 262,139 x 1024 -> 1024
+// 522 / 659 / 1568, 65,536 x 256 -> 512 (512 and 2,048 tiles) 28 / 30 / 55, 16,384 x 512 -> 512 (128 and 512) 22 / 15 / 23,
+// 4,096 x 1024 -> 1024 (64 and 256) 30 / 15 / 20, 16,384 x 1024 -> 64 (128 of 128) 29 / 15 / 12.
 int tile_of(int64_t np, int64_t nq) {
-  for (int t = 256; t > 64; t /= 2)
-    if (np > t / 2 && nq > t / 2 && cdiv(np, t) * cdiv(nq, t) >= kCus) return t;
-  return 64;
+  if (np > 128 && cdiv(np, 256) * cdiv(nq, 256) >= 2 * kCus) return 256;
+  return cdiv(np, 128) * cdiv(nq, 128) >= kCus ? 128 : 64;
 }
 
-template <bool kPT, bool kQT, class Out>
-maestro_status dispatch(int tile, const Product& g, const Out& out, hipStream_t stream) {
-  if (tile == 256) return launch<4, 4, 2, 2, kPT, kQT>(g, out, stream);
-  if (tile == 128) return launch<2, 2, 2, 2, kPT, kQT>(g, out, stream);
-  return launch<1, 1, 2, 2, kPT, kQT>(g, out, stream);
+// Stages of 64 k: rows whose k is contiguous come as whole 128-byte lines. (With stages of 32 and four buffers
+// each line is fetched twice, its halves a stage apart: 552 against 522 us at 262,139 x 1024 -> 1024.)
+template <bool kPT, class Out>
+maestro_status launch_rows(const Product& g, const Out& out, hipStream_t stream) {
+  const int tile = tile_of(g.np, g.nq);
+  if (tile == 256) return launch<4, 4, 64, 2, kPT, false>(g, out, stream);
+  if (tile == 128) return launch<2, 2, 64, 2, kPT, false>(g, out, stream);
+  return launch<1, 1, 64, 2, kPT, false>(g, out, stream);
 }
 
-// How the weights' gradient is cut: tile, splits of the n rows, and workgroups that share the biases' sum.
+// How the weights' gradient is cut: tile, k of one split, splits of the n rows, and workgroups that share the
+// biases' sum. 256 x 256 tiles for many rows, else 256 (d_in) x 64, or 128 x 128 where d_in is narrow;
+// rows split so that there is one round of workgroups, none with fewer than 512 rows. Measured (us,
+// 256 x 256 / 256 x 64 / 128 x 128): 262,139 x 1024 -> 1024 505 / 668 / 591, 512 -> 512 163 / 199 / 194,
+// 1024 -> 64 153 / 149 / 154, 64 -> 1024 155 / 170 / 118; 65,536 x 512 -> 512 68 / 58 / 65; 16,384 41 / 32 / 38.
 struct Cut {
-  int tile;
+  int32_t tp, tq;
   int64_t k_split, splits;
   int32_t parts;
 };
 
 Cut cut_of(int64_t n, int64_t d_in, int64_t d_out) {
   Cut c;
-  c.tile = d_in > 128 && d_out > 128 && n >= 32768 ? 256 : d_in > 64 && d_out > 64 && n >= 8192 ? 128 : 64;
-  const int64_t tiles = cdiv(d_in, c.tile) * cdiv(d_out, c.tile);
-  const int64_t resident = c.tile == 256 ? 1 : c.tile == 128 ? 2 : 4;
-  // one round of workgroups, none with fewer than 512 rows
+  c.tp = d_in > 128 ? 256 : 128;
+  c.tq = c.tp == 128 ? 128 : d_out > 128 && n >= 131072 ? 256 : 64;
+  const int64_t tiles = cdiv(d_in, c.tp) * cdiv(d_out, c.tq), resident = c.tq == 256 ? 1 : 2;
   int64_t splits = kCus * resident / tiles;
   if (splits > cdiv(n, 512)) splits = cdiv(n, 512);
   if (splits < 1) splits = 1;
-  c.k_split = cdiv(cdiv(n, splits), kDepth) * kDepth;
+  c.k_split = cdiv(cdiv(n, splits), 64) * 64;
   c.splits = cdiv(n, c.k_split);
-  c.parts = (int32_t)cdiv(d_in, c.tile);
+  c.parts = (int32_t)cdiv(d_in, c.tp);
   return c;
 }
 
@@ -423,7 +608,7 @@ Cut cut_of(int64_t n, int64_t d_in, int64_t d_out) {
 maestro_status launch_layer_bf16(int64_t n, int32_t d_in, int32_t d_out, const void* x, const void* weight,
                                  const float* bias, bool relu, void* y, hipStream_t stream) {
   Product g{static_cast<const __bf16*>(weight), static_cast<const __bf16*>(x), d_in, d_in, d_out, n, d_in, d_in, 1, 0, 0};
-  return dispatch<false, false>(tile_of(d_out, n), g, Forward{bias, static_cast<__bf16*>(y), relu}, stream);
+  return launch_rows<false>(g, Forward{bias, static_cast<__bf16*>(y), relu}, stream);
 }
 
 size_t layer_grad_bf16_workspace_bytes(int64_t n, int32_t d_in, int32_t d_out) {
@@ -437,24 +622,26 @@ maestro_status launch_layer_grad_bf16(int64_t n, int32_t d_in, int32_t d_out, co
                                       void* workspace, hipStream_t stream) {
   const __bf16 *xb = static_cast<const __bf16*>(x), *gz = static_cast<const __bf16*>(g_z);
   if (n == 0) {
-    join_kernel<<<(unsigned)cdiv((int64_t)d_in * d_out / 4 + d_out, kThreads), kThreads, 0, stream>>>(
+    join_kernel<<<(unsigned)cdiv(((int64_t)d_in + 1) * d_out / 4, kThreads), kThreads, 0, stream>>>(
         nullptr, 0, g_weight, (int64_t)d_in * d_out, nullptr, 0, g_bias, d_out);
     return launch_status();
   }
   if (g_x) {
     Product g{static_cast<const __bf16*>(weight), gz, d_in, d_out, d_in, n, d_out, d_out, 1, 0, 0};
     const maestro_status st =
-        dispatch<true, false>(tile_of(d_in, n), g, InputGrad{xb, static_cast<__bf16*>(g_x), relu_input}, stream);
+        launch_rows<true>(g, InputGrad{xb, static_cast<__bf16*>(g_x), relu_input}, stream);
     if (st != MAESTRO_OK) return st;
   }
   const Cut c = cut_of(n, d_in, d_out);
   float* parts = static_cast<float*>(workspace);
   float* gb_parts = parts + (c.splits > 1 ? c.splits * d_in * d_out : 0);
   Product g{xb, gz, d_in, d_out, d_in, d_out, n, c.k_split, 1, 0, 0};
-  const maestro_status st =
-      dispatch<true, true>(c.tile, g, WeightGrad{c.splits > 1 ? parts : g_weight, gb_parts, c.parts}, stream);
+  const WeightGrad out{c.splits > 1 ? parts : g_weight, gb_parts, c.parts};
+  const maestro_status st = c.tq == 256   ? launch<4, 4, 32, 4, true, true>(g, out, stream)
+                            : c.tp == 256 ? launch<4, 1, 64, 2, true, true>(g, out, stream)
+                                          : launch<2, 2, 64, 2, true, true>(g, out, stream);
   if (st != MAESTRO_OK) return st;
-  const int64_t work = (c.splits > 1 ? (int64_t)d_in * d_out / 4 : 0) + d_out, blocks = cdiv(work, kThreads);
+  const int64_t work = ((c.splits > 1 ? (int64_t)d_in : 0) + 1) * d_out / 4, blocks = cdiv(work, kThreads);
   join_kernel<<<(unsigned)(blocks < 4096 ? blocks : 4096), kThreads, 0, stream>>>(
       parts, (int32_t)c.splits, g_weight, (int64_t)d_in * d_out, gb_parts, (int32_t)(c.splits * c.parts * 2), g_bias, d_out);
   return launch_status();
