@@ -621,11 +621,6 @@ maestro_status launch_layer_grad_bf16(int64_t n, int32_t d_in, int32_t d_out, co
                                       const void* g_z, bool relu_input, void* g_x, float* g_weight, float* g_bias,
                                       void* workspace, hipStream_t stream) {
   const __bf16 *xb = static_cast<const __bf16*>(x), *gz = static_cast<const __bf16*>(g_z);
-  if (n == 0) {
-    join_kernel<<<(unsigned)cdiv(((int64_t)d_in + 1) * d_out / 4, kThreads), kThreads, 0, stream>>>(
-        nullptr, 0, g_weight, (int64_t)d_in * d_out, nullptr, 0, g_bias, d_out);
-    return launch_status();
-  }
   if (g_x) {
     Product g{static_cast<const __bf16*>(weight), gz, d_in, d_out, d_in, n, d_out, d_out, 1, 0, 0};
     const maestro_status st =
@@ -641,9 +636,14 @@ maestro_status launch_layer_grad_bf16(int64_t n, int32_t d_in, int32_t d_out, co
                             : c.tp == 256 ? launch<4, 1, 64, 2, true, true>(g, out, stream)
                                           : launch<2, 2, 64, 2, true, true>(g, out, stream);
   if (st != MAESTRO_OK) return st;
-  const int64_t work = ((c.splits > 1 ? (int64_t)d_in : 0) + 1) * d_out / 4, blocks = cdiv(work, kThreads);
-  join_kernel<<<(unsigned)(blocks < 4096 ? blocks : 4096), kThreads, 0, stream>>>(
-      parts, (int32_t)c.splits, g_weight, (int64_t)d_in * d_out, gb_parts, (int32_t)(c.splits * c.parts * 2), g_bias, d_out);
+  return launch_join(parts, (int32_t)c.splits, g_weight, (int64_t)d_in * d_out, gb_parts, (int32_t)(c.splits * c.parts * 2),
+                     g_bias, d_out, stream);
+}
+
+maestro_status launch_join(const float* gw_parts, int32_t n_gw, float* gw, int64_t size, const float* gb_parts,
+                           int32_t n_gb, float* gb, int32_t d_out, hipStream_t stream) {
+  const int64_t blocks = cdiv((n_gw != 1 ? size / 4 : 0) + d_out / 4, kThreads);
+  join_kernel<<<(unsigned)(blocks < 4096 ? blocks : 4096), kThreads, 0, stream>>>(gw_parts, n_gw, gw, size, gb_parts, n_gb, gb, d_out);
   return launch_status();
 }
 

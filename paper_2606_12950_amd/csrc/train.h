@@ -30,6 +30,10 @@ maestro_status launch_layer_grad_bf16(int64_t n, int32_t d_in, int32_t d_out, co
                                       const void* g_z, bool relu_input, void* g_x, float* g_weight, float* g_bias,
                                       void* workspace, hipStream_t stream);
 
+// g_w (size values; n_gw = 1: it is there already) and g_b from their shares, summed in order; no shares: zeros
+maestro_status launch_join(const float* gw_parts, int32_t n_gw, float* gw, int64_t size, const float* gb_parts,
+                           int32_t n_gb, float* gb, int32_t d_out, hipStream_t stream);
+
 size_t clip_workspace_bytes(int32_t n_tensors);
 maestro_status launch_clip(int32_t n_tensors, void* const* tensors, void* const* out, const int64_t* sizes,
                            const int32_t* dtypes, float max_norm, float* norm, void* workspace, hipStream_t stream);
