@@ -1,8 +1,13 @@
-// The global norm over many gradient tensors, and clipping by it.
+// The global norm over many gradient tensors, and clipping by it: one pass that leaves sums of squares, one that adds
+// them up (every workgroup for itself, in the same order) and scales.
 //
 // Tensors reach the kernels as tables in the kernel arguments, up to kTensors a launch, so a call keeps
 // nothing and a captured graph holds its own copy. Squares are summed in float64: a product of two
-// float32 is exact there and cannot overflow, and the sum needs no care for order or length.
+// float32 is exact there and cannot overflow, and the sum needs no care for order or length. The scaled value is a float64
+// product rounded to float32 (and then to the tensor's type), so no factor is too small for a float32.
+//
+// Bound by HBM. The second pass goes through the tensors backwards: what the first read last is still in the memory-side
+// cache. MEASURED
 #include <math.h>
 
 #include "train.h"
@@ -12,8 +17,9 @@ namespace {
 
 constexpr int kTensors = 96;         // 96 * 32 bytes of table: within the 4 KB of kernel arguments
 constexpr int kThreads = 256;
-constexpr int kChunk = 16384;        // values of one unit of work
-constexpr int kBlocks = 1024;        // workgroups a launch, and partial sums it leaves
+constexpr int kAhead = 8;            // 16-byte vectors of a thread in flight
+constexpr int64_t kChunk = 16 * kThreads * kAhead;        // bytes of one unit of work
+constexpr int kBlocks = 2048;        // the most workgroups, and so partial sums, of a launch
 
 struct Table {
   const void* in[kTensors];
@@ -25,8 +31,19 @@ struct Table {
   int32_t count;
 };
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 __attribute__((aligned(2))) u32x4_at2;        // tensors start anywhere
+typedef u32x4 __attribute__((aligned(4))) u32x4_at4;
+
+template <typename T>
+constexpr int kVec = 16 / sizeof(T);
+
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(__bf16 v) { return (float)v; }
+__device__ __forceinline__ u32x4 load16(const float* p) { return *reinterpret_cast<const u32x4_at4*>(p); }
+__device__ __forceinline__ u32x4 load16(const __bf16* p) { return *reinterpret_cast<const u32x4_at2*>(p); }
+__device__ __forceinline__ void store16(float* p, const u32x4& w) { *reinterpret_cast<u32x4_at4*>(p) = w; }
+__device__ __forceinline__ void store16(__bf16* p, const u32x4& w) { *reinterpret_cast<u32x4_at2*>(p) = w; }
 
 // the tensor that chunk c lies in: the last one whose first chunk is not past it
 __device__ __forceinline__ int tensor_of(const Table& t, int64_t c) {
@@ -50,104 +67,188 @@ __device__ __forceinline__ double block_sum(double s) {
   return s;
 }
 
+__device__ __forceinline__ void add_squares(const u32x4& w, const float*, double& s) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const double v = __uint_as_float(w[i]);
+    s = fma(v, v, s);
+  }
+}
+__device__ __forceinline__ void add_squares(const u32x4& w, const __bf16*, double& s) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const double lo = __uint_as_float(w[i] << 16), hi = __uint_as_float(w[i] & 0xFFFF0000u);
+    s = fma(lo, lo, s);
+    s = fma(hi, hi, s);
+  }
+}
+__device__ __forceinline__ float scaled(float v, double f) { return (float)((double)v * f); }
+__device__ __forceinline__ u32x4 scale16(const u32x4& w, const float*, double f) {
+  return u32x4{__float_as_uint(scaled(__uint_as_float(w[0]), f)), __float_as_uint(scaled(__uint_as_float(w[1]), f)),
+               __float_as_uint(scaled(__uint_as_float(w[2]), f)), __float_as_uint(scaled(__uint_as_float(w[3]), f))};
+}
+__device__ __forceinline__ u32x4 scale16(const u32x4& w, const __bf16*, double f) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  u32x4 out;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const f32x2 v = {scaled(__uint_as_float(w[i] << 16), f), scaled(__uint_as_float(w[i] & 0xFFFF0000u), f)};
+    out[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+  }
+  return out;
+}
+
+// values [lo, hi), at most a chunk
 template <typename T>
 __device__ __forceinline__ double square_sum(const T* x, int64_t lo, int64_t hi) {
+  constexpr int V = kVec<T>;
   double s = 0.0;
-  for (int64_t i = lo + threadIdx.x; i < hi; i += kThreads) {
-    const double v = to_f32(x[i]);
-    s = fma(v, v, s);
+  if (hi - lo == kThreads * kAhead * V) {
+    u32x4 w[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) w[u] = load16(x + lo + (u * kThreads + threadIdx.x) * V);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) add_squares(w[u], x, s);
+  } else {
+    for (int64_t i = lo + threadIdx.x * V; i < hi; i += kThreads * V) {
+      if (i + V <= hi) add_squares(load16(x + i), x, s);
+      else
+        for (int64_t j = i; j < hi; ++j) {
+          const double v = to_f32(x[j]);
+          s = fma(v, v, s);
+        }
+    }
   }
   return s;
 }
 
 template <typename T>
 __device__ __forceinline__ void scale(const T* x, T* y, int64_t lo, int64_t hi, double f) {
-  for (int64_t i = lo + threadIdx.x; i < hi; i += kThreads) y[i] = (T)(float)((double)to_f32(x[i]) * f);
+  constexpr int V = kVec<T>;
+  if (hi - lo == kThreads * kAhead * V) {
+    u32x4 w[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) w[u] = load16(x + lo + (u * kThreads + threadIdx.x) * V);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) store16(y + lo + (u * kThreads + threadIdx.x) * V, scale16(w[u], x, f));
+  } else {
+    for (int64_t i = lo + threadIdx.x * V; i < hi; i += kThreads * V) {
+      if (i + V <= hi) store16(y + i, scale16(load16(x + i), x, f));
+      else
+        for (int64_t j = i; j < hi; ++j) y[j] = (T)scaled(to_f32(x[j]), f);
+    }
+  }
 }
 
 __global__ __launch_bounds__(kThreads) void square_kernel(Table t, double* partial) {
   double s = 0.0;
   for (int64_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
     const int i = tensor_of(t, c);
-    const int64_t lo = (c - t.chunk[i]) * kChunk, hi = lo + kChunk < t.size[i] ? lo + kChunk : t.size[i];
-    if ((t.bf16[i >> 6] >> (i & 63)) & 1) s += square_sum(static_cast<const __bf16*>(t.in[i]), lo, hi);
+    const bool bf16 = (t.bf16[i >> 6] >> (i & 63)) & 1;
+    const int64_t most = kChunk / (bf16 ? 2 : 4), lo = (c - t.chunk[i]) * most;
+    const int64_t hi = lo + most < t.size[i] ? lo + most : t.size[i];
+    if (bf16) s += square_sum(static_cast<const __bf16*>(t.in[i]), lo, hi);
     else s += square_sum(static_cast<const float*>(t.in[i]), lo, hi);
   }
   s = block_sum(s);
   if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
 
-// total[0] = the sum of squares
-__global__ __launch_bounds__(kThreads) void total_kernel(const double* partial, int64_t n, double* total, float* norm) {
+// the sum of all partial sums, in every thread
+__device__ __forceinline__ double total(const double* partial, int64_t n) {
   double s = 0.0;
   for (int64_t i = threadIdx.x; i < n; i += kThreads) s += partial[i];
-  s = block_sum(s);
-  if (threadIdx.x == 0) {
-    total[0] = s;
-    norm[0] = (float)sqrt(s);
-  }
+  return block_sum(s);
 }
 
-__global__ __launch_bounds__(kThreads) void scale_kernel(Table t, const double* total, double max_norm, bool in_place) {
-  const double norm = sqrt(total[0]);
-  const bool over = norm > max_norm && norm < INFINITY;
+__global__ __launch_bounds__(kThreads) void norm_kernel(const double* partial, int64_t n, float* norm) {
+  const double s = total(partial, n);
+  if (threadIdx.x == 0) norm[0] = (float)sqrt(s);
+}
+
+// norm: written by the first launch's first workgroup, NULL in the others
+__global__ __launch_bounds__(kThreads) void scale_kernel(Table t, const double* partial, int64_t n, double max_norm,
+                                                         bool in_place, float* norm) {
+  const double all = sqrt(total(partial, n));
+  if (norm && blockIdx.x == 0 && threadIdx.x == 0) norm[0] = (float)all;
+  const bool over = all > max_norm && all < INFINITY;
   if (!over && in_place) return;
-  const double f = over ? max_norm / norm : 1.0;
-  for (int64_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+  const double f = over ? max_norm / all : 1.0;
+  for (int64_t c = t.chunks - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
     const int i = tensor_of(t, c);
-    const int64_t lo = (c - t.chunk[i]) * kChunk, hi = lo + kChunk < t.size[i] ? lo + kChunk : t.size[i];
-    if ((t.bf16[i >> 6] >> (i & 63)) & 1)
-      scale(static_cast<const __bf16*>(t.in[i]), static_cast<__bf16*>(t.out[i]), lo, hi, f);
-    else
-      scale(static_cast<const float*>(t.in[i]), static_cast<float*>(t.out[i]), lo, hi, f);
+    const bool bf16 = (t.bf16[i >> 6] >> (i & 63)) & 1;
+    const int64_t most = kChunk / (bf16 ? 2 : 4), lo = (c - t.chunk[i]) * most;
+    const int64_t hi = lo + most < t.size[i] ? lo + most : t.size[i];
+    if (bf16) scale(static_cast<const __bf16*>(t.in[i]), static_cast<__bf16*>(t.out[i]), lo, hi, f);
+    else scale(static_cast<const float*>(t.in[i]), static_cast<float*>(t.out[i]), lo, hi, f);
   }
 }
 
-// the next launch's table, from tensor `next` on; empty tensors take no entry
-void fill(Table& t, int32_t& next, int32_t n, void* const* tensors, void* const* out, const int64_t* sizes,
-          const int32_t* dtypes) {
+struct Call {
+  int32_t n;
+  void* const* tensors;
+  void* const* out;
+  const int64_t* sizes;
+  const int32_t* dtypes;
+};
+
+// The table of the tensors [from, to): at most kTensors that are not empty.
+void fill(Table& t, const Call& c, int32_t from, int32_t to) {
   t.count = 0;
   t.chunks = 0;
   t.bf16[0] = t.bf16[1] = 0;
-  for (; next < n && t.count < kTensors; ++next) {
-    if (sizes[next] == 0) continue;
+  for (int32_t j = from; j < to; ++j) {
+    if (c.sizes[j] == 0) continue;
     const int i = t.count++;
-    t.in[i] = tensors[next];
-    t.out[i] = out ? out[next] : tensors[next];
-    t.size[i] = sizes[next];
+    t.in[i] = c.tensors[j];
+    t.out[i] = c.out ? c.out[j] : c.tensors[j];
+    t.size[i] = c.sizes[j];
     t.chunk[i] = t.chunks;
-    t.chunks += (sizes[next] + kChunk - 1) / kChunk;
-    if (dtypes[next] == MAESTRO_BF16) t.bf16[i >> 6] |= 1ull << (i & 63);
+    const int64_t most = kChunk / (c.dtypes[j] == MAESTRO_BF16 ? 2 : 4);
+    t.chunks += (c.sizes[j] + most - 1) / most;
+    if (c.dtypes[j] == MAESTRO_BF16) t.bf16[i >> 6] |= 1ull << (i & 63);
   }
 }
 
-unsigned grid_of(const Table& t) { return (unsigned)(t.chunks < kBlocks ? t.chunks : kBlocks); }
+int32_t launches_of(int32_t n) { return (int32_t)(((int64_t)n + kTensors - 1) / kTensors); }
+
+// Workgroups of a launch: fewer where there are many launches, so that the partial sums stay soon added up.
+unsigned grid_of(const Table& t, int32_t launches) {
+  int64_t most = 2 * kBlocks / launches;
+  most = most < 64 ? 64 : most > kBlocks ? kBlocks : most;
+  return (unsigned)(t.chunks < most ? t.chunks : most);
+}
 
 }  // namespace
 
-// the total, then every launch's partial sums
 size_t clip_workspace_bytes(int32_t n_tensors) {
-  return 16 + ((size_t)n_tensors + kTensors - 1) / kTensors * kBlocks * sizeof(double);
+  return 16 + (size_t)launches_of(n_tensors) * kBlocks * sizeof(double);
 }
 
 maestro_status launch_clip(int32_t n_tensors, void* const* tensors, void* const* out, const int64_t* sizes,
                            const int32_t* dtypes, float max_norm, float* norm, void* workspace, hipStream_t stream) {
-  double* total = static_cast<double*>(workspace);
-  double* partial = total + 2;
+  const Call c{n_tensors, tensors, out, sizes, dtypes};
+  const int32_t launches = launches_of(n_tensors);
+  double* partial = static_cast<double*>(workspace);
   int64_t sums = 0;
   Table t;
-  for (int32_t next = 0; next < n_tensors;) {
-    fill(t, next, n_tensors, tensors, out, sizes, dtypes);
-    if (t.count == 0) break;
-    square_kernel<<<grid_of(t), kThreads, 0, stream>>>(t, partial + sums);
-    sums += grid_of(t);
+  for (int32_t l = 0; l < launches; ++l) {
+    fill(t, c, l * kTensors, l == launches - 1 ? n_tensors : (l + 1) * kTensors);
+    if (t.count == 0) continue;
+    const unsigned grid = grid_of(t, launches);
+    square_kernel<<<grid, kThreads, 0, stream>>>(t, partial + sums);
+    sums += grid;
   }
-  total_kernel<<<1, kThreads, 0, stream>>>(partial, sums, total, norm);
-  if (max_norm == INFINITY) return launch_status();
-  for (int32_t next = 0; next < n_tensors;) {
-    fill(t, next, n_tensors, tensors, out, sizes, dtypes);
-    if (t.count == 0) break;
-    scale_kernel<<<grid_of(t), kThreads, 0, stream>>>(t, total, max_norm, !out);
+  if (max_norm == INFINITY || sums == 0) {
+    norm_kernel<<<1, kThreads, 0, stream>>>(partial, sums, norm);
+    return launch_status();
+  }
+  for (int32_t l = launches - 1; l >= 0; --l) {             // backwards: see the top
+    if (launches > 1) fill(t, c, l * kTensors, l == launches - 1 ? n_tensors : (l + 1) * kTensors);
+    if (t.count == 0) continue;
+    scale_kernel<<<grid_of(t, 1), kThreads, 0, stream>>>(t, partial, sums, max_norm, !out, norm);
+    norm = nullptr;
   }
   return launch_status();
 }
