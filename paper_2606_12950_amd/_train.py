@@ -13,7 +13,7 @@ from typing import NamedTuple, Optional, Sequence
 import torch
 
 from . import _native
-from ._native import MAESTRO_BF16, MAESTRO_F32, _check, _dev, _ptr, _scratch, _shape, _stream, _workspace
+from ._native import MAESTRO_BF16, MAESTRO_F32, _check, _dev, _ptr, _scratch, _shape, _stream, _Tensor, _workspace
 
 # Every function declared in include/maestro_train.h.
 EXPORTS = ("maestro_logprobs_workspace", "maestro_logprobs", "maestro_logprobs_grad", "maestro_layer",
@@ -214,20 +214,22 @@ def layer_grad(x: torch.Tensor, weight: torch.Tensor, g_z: torch.Tensor, relu_in
     return out
 
 
-def _pointers(tensors: Sequence[torch.Tensor], name: str, like=None):
-    """Host array of the tensors' addresses; contiguous float32 or bfloat16 tensors on one GPU."""
-    out = (ctypes.c_void_p * len(tensors))()
-    for i, t in enumerate(tensors):
-        if not isinstance(t, torch.Tensor) or not t.is_cuda:
-            raise TypeError(f"{name}[{i}] must be a CUDA (HIP) tensor")
+def _host_arrays(tensors: Sequence[torch.Tensor], name: str):
+    """(addresses, element counts, dtype codes) of contiguous float32 or bfloat16 tensors on a GPU, as lists. Runs for
+    every tensor of a call: 0.3 us each."""
+    at, sizes, codes = [], [], []
+    for t in tensors:
+        if not isinstance(t, _Tensor) or not t.is_cuda:
+            raise TypeError(f"{name} must be CUDA (HIP) tensors")
         if not t.is_contiguous():
-            raise ValueError(f"{name}[{i}] must be contiguous")
-        if t.dtype not in _DTYPE:
-            raise TypeError(f"{name}[{i}] must be float32 or bfloat16, got {t.dtype}")
-        if like is not None and (t.dtype != like[i].dtype or t.shape != like[i].shape):
-            raise ValueError(f"{name}[{i}] must have its tensor's shape and type")
-        out[i] = t.data_ptr()
-    return out
+            raise ValueError(f"{name} must be contiguous")
+        code = _DTYPE.get(t.dtype)
+        if code is None:
+            raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
+        at.append(t.data_ptr())
+        sizes.append(t.numel())
+        codes.append(code)
+    return at, sizes, codes
 
 
 def clip_gradients(tensors: Sequence[torch.Tensor], max_norm: float, out: Optional[Sequence[torch.Tensor]] = None,
@@ -243,16 +245,16 @@ def clip_gradients(tensors: Sequence[torch.Tensor], max_norm: float, out: Option
     max_norm = float(max_norm)
     if not max_norm >= 0.0:
         raise ValueError("max_norm must not be negative or NaN")
-    ptr = _pointers(tensors, "tensors")
+    at, sizes, codes = _host_arrays(tensors, "tensors")
+    count = len(tensors)
+    pointers = ctypes.c_void_p * count
     optr = None
     if out is not None:
-        out = list(out)
-        if len(out) != len(tensors):
-            raise ValueError("one output per tensor")
-        optr = _pointers(out, "out", tensors)
-    count = len(tensors)
-    sizes = (ctypes.c_int64 * count)(*[t.numel() for t in tensors])
-    dtypes = (ctypes.c_int32 * count)(*[_DTYPE[t.dtype] for t in tensors])
+        oat, osizes, ocodes = _host_arrays(out, "out")
+        if osizes != sizes or ocodes != codes:
+            raise ValueError("out must have one output per tensor, of its size and type")
+        optr = pointers(*oat)
+    ptr, sizes, dtypes = pointers(*at), (ctypes.c_int64 * count)(*sizes), (ctypes.c_int32 * count)(*codes)
     dev = tensors[0].device
     if norm is None:
         norm = torch.empty(1, dtype=torch.float32, device=dev)

@@ -320,7 +320,8 @@ __global__ __launch_bounds__(kThreads, WP * WQ > 8 ? 1 : WP * WQ > 2 ? 2 : 4) vo
   constexpr int kBiasLoads = Out::kBias ? (WP + 1) / 2 : 0;
   constexpr int kStores = kSums ? 0 : 2 * WP * WQ + kBiasLoads;      // between two tiles, exactly
   static_assert(kLoads * (kBufs - 2) + kStores < 64, "vmcnt range");
-  extern __shared__ unsigned char lds[];
+  constexpr int kBiasBytes = 2 * 4 * 256 * kBiasLoads;      // two places for each wavefront
+  __shared__ __attribute__((aligned(16))) unsigned char lds[kBufs * kStage + (kSums ? 0 : 4 * Staging<WP>::kBytes) + kBiasBytes];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wp = wave % NP, wq = wave / NP;
 
@@ -544,17 +545,13 @@ constexpr int64_t kCus = 256;
 template <int WP, int WQ, int kDepth, int kBufs, bool kPT, bool kQT, class Out>
 maestro_status launch(Product g, const Out& out, hipStream_t stream) {
   constexpr int TP = 64 * WP, TQ = 64 * WQ;
-  constexpr int kLds = kBufs * (TP + TQ) * 2 * kDepth + (kQT ? 0 : 4 * Staging<WP>::kBytes) + (Out::kBias ? 2 * 4 * ((WP + 1) / 2) * 256 : 0);
   constexpr int64_t kResident = WP * WQ > 8 ? 1 : WP * WQ > 2 ? 2 : 4;     // workgroups of a CU
   g.p_tiles = (int32_t)cdiv(g.np, TP);
   g.splits = (int32_t)cdiv(g.nk, g.k_split);
   g.items = cdiv(g.nq, TQ) * g.p_tiles * g.splits;
   const auto kernel = product_kernel<WP, WQ, kDepth, kBufs, kPT, kQT, Out>;
-  if (kLds > 65536 &&
-      hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kLds) != hipSuccess)
-    return MAESTRO_ERR_LAUNCH;
   const int64_t want = cdiv(g.items, 8) * 8, most = kCus * kResident;
-  kernel<<<(unsigned)(want < most ? want : most), kThreads, kLds, stream>>>(g, out);
+  kernel<<<(unsigned)(want < most ? want : most), kThreads, 0, stream>>>(g, out);
   return launch_status();
 }
 
