@@ -113,6 +113,8 @@ struct Operand {
   const unsigned char* base;                                // turned: the next stage's first row
   int64_t left;                                             // turned: rows of k from there on
   uint32_t bytes;                                           // k contiguous: of the resource
+  i32x4 rsrc;                                               // of the stage being fetched, and its place
+  uint32_t to;
 
   // 64-byte blocks of a turned row k are stored at block ^ turn(k), so that the four rows of a
   // transposing read lie in different banks
@@ -153,24 +155,30 @@ struct Operand {
     left = 0;
     bytes = 0;
   }
-  // the next stage, into the buffer at LDS address lds (uniform)
-  __device__ __forceinline__ void fetch(uint32_t lds, int wave) {
-    const uint32_t at = __builtin_amdgcn_readfirstlane(lds + 1024 * kLoads * wave);
+  // The next stage, into the buffer at LDS address lds (uniform): aim, every load, advance.
+  __device__ __forceinline__ void aim(uint32_t lds, int wave) {
+    to = __builtin_amdgcn_readfirstlane(lds + 1024 * kLoads * wave);
+    rsrc = buffer_rsrc(base, kTurned ? (uint32_t)(left < kDepth ? left < 0 ? 0 : left : kDepth) * row_bytes : bytes);
+  }
+  __device__ __forceinline__ void fetch(int j) const {
+    if constexpr (kTurned) dma16(rsrc, off[j], 0, to, 1024 * j);
+    else dma16(rsrc, (unit ^ odd(j)) < row_bytes ? off[j] : 0x80000000u, 0, to, 1024 * j);
+  }
+  __device__ __forceinline__ void advance() {
     if constexpr (kTurned) {
-      const i32x4 r = buffer_rsrc(base, (uint32_t)(left < kDepth ? left < 0 ? 0 : left : kDepth) * row_bytes);
-#pragma unroll
-      for (int j = 0; j < kLoads; ++j) dma16(r, off[j], 0, at, 1024 * j);
       base += kDepth * row_bytes;
       left -= kDepth;
     } else {
-      const i32x4 r = buffer_rsrc(base, bytes);
 #pragma unroll
-      for (int j = 0; j < kLoads; ++j) {
-        dma16(r, (unit ^ odd(j)) < row_bytes ? off[j] : 0x80000000u, 0, at, 1024 * j);
-        off[j] += 2 * kDepth;
-      }
+      for (int j = 0; j < kLoads; ++j) off[j] += 2 * kDepth;
       unit += 2 * kDepth;
     }
+  }
+  __device__ __forceinline__ void fetch_all(uint32_t lds, int wave) {
+    aim(lds, wave);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) fetch(j);
+    advance();
   }
 };
 
@@ -194,13 +202,9 @@ struct Fragments {
       at[0] = row * 2 * kDepth + ((h ^ Op::place(row)) << 4);
     }
   }
-  __device__ __forceinline__ void read(const unsigned char* stage, int kk, bf16x8 (&f)[W], int first = 0,
-                                       int end = W) const {
-#pragma unroll
-    for (int b = first; b < end; ++b) {
-      if constexpr (kTurned) f[b] = read_turned(stage + at[b] + kk * 16 * 2 * T, 4 * 2 * T);
-      else f[b] = *reinterpret_cast<const bf16x8*>(stage + (at[0] ^ (kk * 32)) + b * 32 * 2 * kDepth);
-    }
+  __device__ __forceinline__ bf16x8 read(const unsigned char* stage, int kk, int b) const {
+    if constexpr (kTurned) return read_turned(stage + at[b] + kk * 16 * 2 * T, 4 * 2 * T);
+    else return *reinterpret_cast<const bf16x8*>(stage + (at[0] ^ (kk * 32)) + b * 32 * 2 * kDepth);
   }
 };
 
@@ -394,15 +398,17 @@ __global__ __launch_bounds__(kThreads, WP * WQ > 8 ? 1 : WP * WQ > 2 ? 2 : 4) vo
   open();
 #pragma unroll
   for (int b = 0; b < kBufs; ++b) {
-    op.fetch(lds0 + b * kStage, wave);
-    oq.fetch(lds0 + b * kStage + kQ, wave);
+    op.fetch_all(lds0 + b * kStage, wave);
+    oq.fetch_all(lds0 + b * kStage + kQ, wave);
     fetched();
   }
   wait_loads<kLoads * (kBufs - 1)>();
 
   bf16x8 pf[2][WP], qf[2][WQ];                              // this step's fragments and the next one's
-  fp.read(lds, 0, pf[0]);
-  fq.read(lds + kQ, 0, qf[0]);
+#pragma unroll
+  for (int a = 0; a < WP; ++a) pf[0][a] = fp.read(lds, 0, a);
+#pragma unroll
+  for (int b = 0; b < WQ; ++b) qf[0][b] = fq.read(lds + kQ, 0, b);
   int buf = 0;
 #pragma clang loop unroll(disable)
   for (int64_t i = first; i < last; i += step) {
@@ -440,9 +446,9 @@ __global__ __launch_bounds__(kThreads, WP * WQ > 8 ? 1 : WP * WQ > 2 ? 2 : 4) vo
       uint32_t into = 0;
 #pragma unroll
       for (int kk = 0; kk < kHalves; ++kk) {
-        // One step of 16 k. The next step's fragments are read, and with the stage's last one the loads of a
-        // later stage issued, between the products: a wavefront has its SIMD's matrix core to itself
-        // (256 x 256), so what is not between two products is a gap.
+        // One step of 16 k. A wavefront has its SIMD's matrix core to itself (256 x 256), and whatever does not fit
+        // between one product's issue and the next is a gap: so the next step's fragments are read, and with
+        // the stage's last step the loads of a later stage issued, a few after each product.
         const bool end = kk == kHalves - 1;
         bf16x8(&pc)[WP] = pf[kk & 1], (&pn)[WP] = pf[1 - (kk & 1)];
         bf16x8(&qc)[WQ] = qf[kk & 1], (&qn)[WQ] = qf[1 - (kk & 1)];
@@ -468,16 +474,33 @@ __global__ __launch_bounds__(kThreads, WP * WQ > 8 ? 1 : WP * WQ > 2 ? 2 : 4) vo
           stage = lds + buf * kStage;
         }
         const int to = end ? 0 : kk + 1;
+        if (end) {
+          op.aim(into, wave);
+          oq.aim(into + kQ, wave);
+        }
+        // of the products, the first half is followed by a share of the reads each, all by one of the loads
+        constexpr int kProducts = WP * WQ, kHalf = (kProducts + 1) / 2, kFrags = WP + WQ;
 #pragma unroll
-        for (int a = 0; a < WP; ++a) {
-          if (a == 0) fq.read(stage + kQ, to, qn);
-          if (WP < 4 ? a == 0 : a == 1 || a == 2) fp.read(stage, to, pn, WP < 4 ? 0 : 2 * a - 2, WP < 4 ? WP : 2 * a);
-          if (end && a == 0) op.fetch(into, wave);
-          if (end && a == WP / 2) oq.fetch(into + kQ, wave);
+        for (int m = 0; m < kProducts; ++m) {
+          const int a = m / WQ, b = m % WQ;
+          acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(pc[a], qc[b], acc[a][b], 0, 0, 0);
 #pragma unroll
-          for (int b = 0; b < WQ; ++b)
-            acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(pc[a], qc[b], acc[a][b], 0, 0, 0);
+          for (int f = m * kFrags / kHalf; f < (m + 1) * kFrags / kHalf && f < kFrags; ++f) {
+            if (f < WQ) qn[f] = fq.read(stage + kQ, to, f);
+            else pn[f - WQ] = fp.read(stage, to, f - WQ);
+          }
+          if (end) {
+#pragma unroll
+            for (int l = m * kLoads / kProducts; l < (m + 1) * kLoads / kProducts; ++l) {
+              if (l < op.kLoads) op.fetch(l);
+              else oq.fetch(l - op.kLoads);
+            }
+          }
           __builtin_amdgcn_sched_barrier(0);
+        }
+        if (end) {
+          op.advance();
+          oq.advance();
         }
       }
       fetched();
