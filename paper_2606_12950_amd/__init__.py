@@ -2,7 +2,8 @@
 
 The computation lives in libmaestro.so (hand-written HIP kernels behind the C-ABI of
 include/maestro.h); this package is its thin Python binding plus the seeded workload
-generator. include/maestro_train.h adds what the length predictor is scored and trained with. PyTorch supplies device memory and streams only.
+generator. include/maestro_train.h adds what the length predictor is scored and trained with (``fit``
+runs it together). PyTorch supplies device memory and streams only.
 """
 from ._native import (LIBRARY_PATH, MaestroError, Predictor, TwoPhase, load, make_predictor, predict,
                       predict_two_phase, predict_role_lengths,
