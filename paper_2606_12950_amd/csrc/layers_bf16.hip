@@ -75,7 +75,7 @@ struct InputGrad {
 struct WeightGrad {
   static constexpr bool kBias = false;
   float* gw;                         // [splits][nq][np]
-  float* gb;                         // [splits * parts][nq]
+  float* gb;                         // one split: [nq], whole; else [splits][parts][two wavefronts][nq]
   int32_t parts;                     // workgroups (of one split and q) that share the sum over Q
 };
 
@@ -207,6 +207,13 @@ struct Fragments {
     else return *reinterpret_cast<const bf16x8*>(stage + (at[0] ^ (kk * 32)) + b * 32 * 2 * kDepth);
   }
 };
+
+__device__ __forceinline__ float add8(const u32x4& v) {
+  float s = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) s += __uint_as_float(v[e] << 16) + __uint_as_float(v[e] & 0xFFFF0000u);
+  return s;
+}
 
 template <class Out>
 __device__ __forceinline__ int32_t parts_of(const Out& out) {
@@ -439,7 +446,7 @@ __global__ __launch_bounds__(kThreads, WP * WQ > 8 ? 1 : WP * WQ > 2 ? 2 : 4) vo
     // the sum over Q's k (the biases' gradient): a stage's by one of the workgroups with these rows of Q,
     // half of k by each of the wavefronts
     const int64_t turns = parts_of(out);
-    int64_t mine = kSums ? t.p0 / TP : INT64_MAX;
+    int64_t mine = kSums && t.p0 / TP < turns ? t.p0 / TP : INT64_MAX;
 #pragma clang loop unroll(disable)                            // nor peel: copies of 256 accumulators
     for (int64_t s = 0; s < t.stages; ++s) {
       const unsigned char* stage = lds + buf * kStage;
@@ -453,13 +460,12 @@ __global__ __launch_bounds__(kThreads, WP * WQ > 8 ? 1 : WP * WQ > 2 ? 2 : 4) vo
         bf16x8(&pc)[WP] = pf[kk & 1], (&pn)[WP] = pf[1 - (kk & 1)];
         bf16x8(&qc)[WQ] = qf[kk & 1], (&qn)[WQ] = qf[1 - (kk & 1)];
         if constexpr (kSums) {
-          if (kk % 2 && s == mine) {                        // steps kk - 1 and kk: one for each wavefront
+          if (kk % 2 && s == mine) {                        // steps kk - 1 and kk: one for each wavefront, or both
 #pragma unroll
             for (int b = 0; b < WQ; ++b) {
               const u32x4 v = wp ? __builtin_bit_cast(u32x4, qc[b]) : __builtin_bit_cast(u32x4, qn[b]);
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                sums[b] += __uint_as_float(v[e] << 16) + __uint_as_float(v[e] & 0xFFFF0000u);
+              sums[b] += add8(v);
+              if (g.splits == 1) sums[b] += add8(wp ? __builtin_bit_cast(u32x4, qn[b]) : __builtin_bit_cast(u32x4, qc[b]));
             }
             if (end) mine += turns;
           }
@@ -527,9 +533,14 @@ __global__ __launch_bounds__(kThreads, WP * WQ > 8 ? 1 : WP * WQ > 2 ? 2 : 4) vo
                                                                acc[a][b][8 * half + 4 * e + 2], acc[a][b][8 * half + 4 * e + 3]);
             }
           }
-        // NP wavefronts and `parts` workgroups hold shares of the sum over Q
+        // NP wavefronts and `parts` workgroups hold shares of the sum over Q; of a single split, each the whole
         const float s = sums[b] + __shfl_xor(sums[b], 32);
-        if (h == 0 && q < g.nq) out.gb[((t.split * out.parts + t.p0 / TP) * NP + wp) * g.nq + q] = s;
+        const int64_t part = t.p0 / TP;
+        if (g.splits > 1) {
+          if (h == 0 && part < out.parts && q < g.nq) out.gb[((t.split * out.parts + part) * NP + wp) * g.nq + q] = s;
+        } else if (h == 0 && part == 0 && wp == 0 && q < g.nq) {
+          out.gb[q] = s;
+        }
       }
     }
   }
@@ -599,7 +610,7 @@ maestro_status launch_rows(const Product& g, const Out& out, hipStream_t stream)
 }
 
 // How the weights' gradient is cut: tile, k of one split, splits of the n rows, and workgroups that share the
-// biases' sum. 256 x 256 tiles for many rows, else 256 (d_in) x 64, or 128 x 128 where d_in is narrow;
+// biases' sum (one where the rows are not split, so that no second launch is needed). 256 x 256 tiles for many rows, else 256 (d_in) x 64, or 128 x 128 where d_in is narrow;
 // rows split so that there is one round of workgroups, none with fewer than 512 rows. Measured (us,
 // 256 x 256 / 256 x 64 / 128 x 128): 262,139 x 1024 -> 1024 505 / 668 / 591, 512 -> 512 163 / 199 / 194,
 // 1024 -> 64 153 / 149 / 154, 64 -> 1024 155 / 170 / 118; 65,536 x 512 -> 512 68 / 58 / 65; 16,384 41 / 32 / 38.
@@ -619,7 +630,7 @@ Cut cut_of(int64_t n, int64_t d_in, int64_t d_out) {
   if (splits < 1) splits = 1;
   c.k_split = cdiv(cdiv(n, splits), 64) * 64;
   c.splits = cdiv(n, c.k_split);
-  c.parts = (int32_t)cdiv(d_in, c.tp);
+  c.parts = c.splits > 1 ? (int32_t)cdiv(d_in, c.tp) : 1;
   return c;
 }
 
@@ -634,7 +645,7 @@ maestro_status launch_layer_bf16(int64_t n, int32_t d_in, int32_t d_out, const v
 size_t layer_grad_bf16_workspace_bytes(int64_t n, int32_t d_in, int32_t d_out) {
   if (n == 0) return 0;
   const Cut c = cut_of(n, d_in, d_out);
-  return sizeof(float) * (size_t)((c.splits > 1 ? c.splits * d_in * d_out : 0) + c.splits * c.parts * 2 * d_out);
+  return c.splits > 1 ? sizeof(float) * (size_t)(c.splits * ((int64_t)d_in + c.parts * 2) * d_out) : 0;
 }
 
 maestro_status launch_layer_grad_bf16(int64_t n, int32_t d_in, int32_t d_out, const void* x, const void* weight,
@@ -649,13 +660,13 @@ maestro_status launch_layer_grad_bf16(int64_t n, int32_t d_in, int32_t d_out, co
   }
   const Cut c = cut_of(n, d_in, d_out);
   float* parts = static_cast<float*>(workspace);
-  float* gb_parts = parts + (c.splits > 1 ? c.splits * d_in * d_out : 0);
+  float* gb_parts = parts + c.splits * d_in * d_out;
   Product g{xb, gz, d_in, d_out, d_in, d_out, n, c.k_split, 1, 0, 0};
-  const WeightGrad out{c.splits > 1 ? parts : g_weight, gb_parts, c.parts};
+  const WeightGrad out{c.splits > 1 ? parts : g_weight, c.splits > 1 ? gb_parts : g_bias, c.parts};
   const maestro_status st = c.tq == 256   ? launch<4, 4, 32, 4, true, true>(g, out, stream)
                             : c.tp == 256 ? launch<4, 1, 64, 2, true, true>(g, out, stream)
                                           : launch<2, 2, 64, 2, true, true>(g, out, stream);
-  if (st != MAESTRO_OK) return st;
+  if (st != MAESTRO_OK || c.splits == 1) return st;
   return launch_join(parts, (int32_t)c.splits, g_weight, (int64_t)d_in * d_out, gb_parts, (int32_t)(c.splits * c.parts * 2),
                      g_bias, d_out, stream);
 }
