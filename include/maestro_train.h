@@ -73,7 +73,7 @@ MAESTRO_API maestro_status maestro_layer(int64_t n, int32_t d_in, int32_t d_out,
 /* Gradients of a layer z = x * weight^T + bias given g_z [n][d_out] (of z, in `dtype`):
  *   g_weight (out) [d_out][d_in] float32: g_z^T * x      g_bias (out) [d_out] float32: sum of g_z over rows
  *   g_x      (out) [n][d_in] in `dtype`, or NULL where it is not wanted: g_z * weight, and 0 wherever
- *            x <= 0 if relu_input is not 0 (x is a rectified layer's output, g_x the gradient of that layer's z)
+ *            x is not positive if relu_input is not 0 (x is a rectified layer's output, g_x the gradient of that layer's z)
  * Sums are float32; g_x is rounded once. Sizes, alignment and errors as maestro_layer; outputs overlap no
  * input. n = 0 writes zeros. Workspace: maestro_layer_grad_workspace() bytes. */
 MAESTRO_API size_t maestro_layer_grad_workspace(int64_t n, int32_t d_in, int32_t d_out, int32_t dtype);

@@ -22,6 +22,8 @@ EXPORTS = ("maestro_logprobs_workspace", "maestro_logprobs", "maestro_logprobs_g
 
 MAX_ALTERNATIVES = 16
 
+_MOST = (1 << 31) - 1      # of an int32 argument: ctypes would cut a larger number off
+
 _DTYPE = {torch.float32: MAESTRO_F32, torch.bfloat16: MAESTRO_BF16}
 
 
@@ -67,22 +69,26 @@ def load():
     return lib
 
 
-def _rows(t: torch.Tensor, name: str) -> int:
-    """dtype code of a [n][v] float32 or bfloat16 tensor whose rows are contiguous, any row stride."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+def _rows(t: torch.Tensor, name: str):
+    """(dtype code, n, v, row stride) of a [n][v] float32 or bfloat16 tensor whose rows are contiguous and do
+    not overlap."""
+    if not isinstance(t, _Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
     code = _DTYPE.get(t.dtype)
     if code is None:
         raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
-    if t.dim() != 2 or t.shape[1] < 1:
+    shape = t.shape
+    if len(shape) != 2 or shape[1] < 1:
         raise ValueError(f"{name} must be [n][v] with v >= 1")
-    if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+    n, v = shape
+    if v > _MOST:
+        raise ValueError(f"{name} has more columns than an int32 counts")
+    stride, inner = t.stride()
+    if n <= 1:
+        stride = v
+    if (v > 1 and inner != 1) or stride < v:
         raise ValueError(f"{name} must have contiguous rows that do not overlap")
-    return code
-
-
-def _stride(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return code, n, v, stride
 
 
 def logprobs(logits: torch.Tensor, token: Optional[torch.Tensor] = None, k: int = 0, want_entropy: bool = True,
@@ -92,8 +98,7 @@ def logprobs(logits: torch.Tensor, token: Optional[torch.Tensor] = None, k: int 
     array) the log probability of its ``token`` (int32 [n], outside [0, v): none, 0), the entropy, the
     ``k`` likeliest tokens with their log probabilities, and the row statistics. -inf masks a logit."""
     lib = load()
-    dt = _rows(logits, "logits")
-    n, v = logits.shape
+    dt, n, v, stride = _rows(logits, "logits")
     dev = logits.device
     if not 0 <= k <= MAX_ALTERNATIVES:
         raise ValueError(f"k must be 0 .. {MAX_ALTERNATIVES}")
@@ -118,7 +123,7 @@ def logprobs(logits: torch.Tensor, token: Optional[torch.Tensor] = None, k: int 
     _workspace(workspace)
     if workspace is None and need:
         workspace = _scratch(need, dev, stream)
-    st = lib.maestro_logprobs(n, v, _ptr(logits), _stride(logits), dt, _ptr(token), k, _ptr(out.logprob),
+    st = lib.maestro_logprobs(n, v, _ptr(logits), stride, dt, _ptr(token), k, _ptr(out.logprob),
                               _ptr(out.entropy), _ptr(out.top_id), _ptr(out.top_logprob), _ptr(out.stats),
                               _ptr(workspace), workspace.numel() if workspace is not None else 0, _stream(stream))
     _check("maestro_logprobs", st)
@@ -133,8 +138,7 @@ def logprobs_grad(logits: torch.Tensor, token: Optional[torch.Tensor], stats: to
     the log probabilities and ``g_entropy`` times the entropies (float32 [n], either may be None), in the
     logits' type. ``stats`` and ``entropy`` are what ``logprobs`` returned; ``out`` may be ``logits``."""
     lib = load()
-    dt = _rows(logits, "logits")
-    n, v = logits.shape
+    dt, n, v, stride = _rows(logits, "logits")
     if (token is None) != (g_logprob is None) or (g_logprob is None and g_entropy is None):
         raise ValueError("g_logprob goes with token, and one of g_logprob and g_entropy is needed")
     if g_entropy is not None and entropy is None:
@@ -146,11 +150,13 @@ def logprobs_grad(logits: torch.Tensor, token: Optional[torch.Tensor], stats: to
         if t is not None:
             _shape(_dev(t, name, torch.float32), name, (n,))
     if out is None:
-        out = torch.empty((n, v), dtype=logits.dtype, device=logits.device)
-    elif _rows(out, "out") != dt or out.shape != logits.shape:
-        raise ValueError("out must have the logits' shape and type")
-    st = lib.maestro_logprobs_grad(n, v, _ptr(logits), _stride(logits), dt, _ptr(token), _ptr(stats), _ptr(entropy),
-                                   _ptr(g_logprob), _ptr(g_entropy), _ptr(out), _stride(out), _stream(stream))
+        out, out_stride = torch.empty((n, v), dtype=logits.dtype, device=logits.device), v
+    else:
+        *same, out_stride = _rows(out, "out")
+        if same != [dt, n, v]:
+            raise ValueError("out must have the logits' shape and type")
+    st = lib.maestro_logprobs_grad(n, v, _ptr(logits), stride, dt, _ptr(token), _ptr(stats), _ptr(entropy),
+                                   _ptr(g_logprob), _ptr(g_entropy), _ptr(out), out_stride, _stream(stream))
     _check("maestro_logprobs_grad", st)
     return out
 
@@ -163,7 +169,10 @@ def _layer_shapes(x: torch.Tensor, weight: torch.Tensor):
     _dev(x, "x", weight.dtype)
     if weight.dim() != 2 or x.dim() != 2 or x.shape[1] != weight.shape[1]:
         raise ValueError("x must be [n][d_in] and weight [d_out][d_in]")
-    return code, x.shape[0], weight.shape[1], weight.shape[0]
+    o, i = weight.shape
+    if o > _MOST or i > _MOST:
+        raise ValueError("weight has more rows or columns than an int32 counts")
+    return code, x.shape[0], i, o
 
 
 def layer(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor, relu: bool = True,
