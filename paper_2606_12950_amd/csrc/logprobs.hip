@@ -339,26 +339,31 @@ struct Segments {
   int64_t length;
 };
 
-// Thread t takes the vectors t, t + kThreads, ... and keeps their maximum beside its sums. The k-th largest of those
-// maxima bounds the k-th largest logit from below, so only the vectors of threads that reach it are read again (from
-// the cache; about k of them, by all threads together), and of these only the logits that reach it are ranked. Where more than
+// Thread t takes the vectors t, t + kThreads, ... and keeps their maximum beside its sums. The k-th largest of any of
+// those maxima bounds the k-th largest logit from below, so only the vectors of threads that reach it are read again (from
+// the cache; hardly more than k of them, by all threads together), and of these only the logits that reach it are ranked. Where more than
 // kCandidates do (long runs of equal logits), k scans find them instead.
 //
-// A wavefront to a row (no barriers, 64 threads) where rows are many and short, 256 threads otherwise: 16,384 x 4,096
-// bfloat16 36 us against 110, 4,096 x 20,000 39 against 48, but 2,048 x 131,072 171 against 111. Against short_kernel's widest form
-// it takes 88 us to 106 at 65,536 x 2,048 bfloat16, and 190 to 98 at 131,072 x 1,000.
+// A wavefront to a row (no barriers, 64 threads) where rows are many and short, 512 threads where they are few and long, else 256.
+// Measured (us): 16,384 x 4,096 bfloat16 36 with 64 threads and 110 with 256, 4,096 x 20,000 39 and 48, but
+// 2,048 x 131,072 171 and 111; one row of 32,000 with eight alternatives 8.6 with 256 and 7.8 with 512, one of 5,000
+// 6.6 and 7.5. Against short_kernel's widest form 64 threads take 88 to 106 at 65,536 x 2,048 bfloat16, 190 to 98 at
+// 131,072 x 1,000.
 template <typename T, int kThreads>
 __global__ __launch_bounds__(kThreads) void long_kernel(int64_t n, int32_t v, const T* logits, int64_t stride,
                                                         const int32_t* token, int32_t k, Outputs o, Segments seg) {
   constexpr int V = kVec<T>, kWaves = kThreads / 64, kAhead = 4;
   __shared__ Part s_part[kWaves];
-  __shared__ float s_top[kWaves * kMaxAlternatives], s_value[kCandidates], s_bound;
+  constexpr int kTop = kThreads / 16 * ((kMaxAlternatives + kThreads / 16 - 1) / (kThreads / 16) + 1);
+  __shared__ float s_top[kTop], s_value[kCandidates], s_bound;
   __shared__ int32_t s_id[kCandidates], s_who[kThreads];
   __shared__ uint32_t s_who_count, s_count;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t jobs = n * seg.count;
   for (int64_t job = blockIdx.x; job < jobs; job += gridDim.x) {
-    const int64_t row = job / seg.count, first = (job - row * seg.count) * seg.length;
+    // more than one segment: few rows, and 32 bits do
+    const int64_t row = seg.count == 1 ? job : (int64_t)((uint32_t)job / (uint32_t)seg.count);
+    const int64_t first = (job - row * seg.count) * seg.length;
     const T* x = logits + row * stride + first;
     const int64_t len = v - first < seg.length ? v - first : seg.length, vecs = (len + V - 1) / V;
 
@@ -419,29 +424,31 @@ __global__ __launch_bounds__(kThreads) void long_kernel(int64_t n, int32_t v, co
       if (r.bad || r.none) {
         if (tid < k) put(tid, -1, -INFINITY);
       } else {
-        float left = own, w = 0.0f;
-        for (int i = 0; i < k; ++i) {                       // the wavefront's k largest maxima
-          w = group_max<64>(left);
-          if (lane == __builtin_ctzll(__ballot(left == w))) left = -INFINITY;
-          if (kWaves > 1 && lane == 0) s_top[wave * k + i] = w;
+        // every 16 lanes their largest maxima, a few more than k in all, and the k-th of those
+        constexpr int kGroups = kThreads / 16;
+        const int rounds = (k + kGroups - 1) / kGroups + (2 * k > kGroups), values = kGroups * rounds;
+        float left = own;
+        for (int i = 0; i < rounds; ++i) {
+          const float m = group_max<16>(left);
+          if ((lane & 15) == 0) s_top[tid / 16 * rounds + i] = m;
+          const uint64_t have = __ballot(left == m) >> (lane & 48) & 0xFFFF;
+          if ((lane & 15) == __builtin_ctzll(have)) left = -INFINITY;
         }
         __syncthreads();
-        if constexpr (kWaves > 1) {
-          if (tid < kWaves * k) {
-            const float mine = s_top[tid];
-            int rank = 0;
+        if (tid < values) {
+          const float mine = s_top[tid];
+          int rank = 0;
 #pragma unroll 8
-            for (int i = 0; i < kWaves * k; ++i) rank += s_top[i] > mine || (s_top[i] == mine && i < tid);
-            if (rank == k - 1) s_bound = mine;
-          }
-          __syncthreads();
-          w = s_bound;
+          for (int i = 0; i < values; ++i) rank += s_top[i] > mine || (s_top[i] == mine && i < tid);
+          if (rank == k - 1) s_bound = mine;
         }
+        __syncthreads();
+        const float w = s_bound;
         if (own >= w && own > -INFINITY) s_who[atomicAdd(&s_who_count, 1u)] = tid;
         __syncthreads();
-        const int64_t each = (vecs + kThreads - 1) / kThreads, all = each * s_who_count;
-        for (int64_t i = tid; i < all; i += kThreads) {
-          const int64_t j = (s_who[i / each] + i % each * kThreads) * V;
+        const uint32_t each = (uint32_t)((vecs + kThreads - 1) / kThreads), all = each * s_who_count;     // < 2^31 / V + 256
+        for (uint32_t i = tid; i < all; i += kThreads) {
+          const int64_t j = (s_who[i / each] + (int64_t)(i % each) * kThreads) * V;
           if (j < len) {
             float z[V];
             load_vec(x, j, len, z);
@@ -682,7 +689,8 @@ int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
 constexpr int64_t kCus = 256;
 
 // Segments of a row: one where there are rows enough for the chip, or the row is soon read. One row of 131,072
-// float32 takes 22 us in one piece and 11 in 16 to 32 (both launches); one of 32,000 bfloat16 9.7 in one, 11 in four.
+// float32 with eight alternatives takes 22 us in one piece and 10 in 16 to 32 (both launches); one of 32,000 bfloat16 8 in one, 11
+// in four.
 int64_t segments_of(int64_t n, int64_t bytes) {
   if (n >= kCus || bytes < 131072) return 1;
   return least(least(64, cdiv(2 * kCus, n)), bytes / 16384);
@@ -717,6 +725,8 @@ maestro_status launch(int64_t n, int32_t v, const T* x, int64_t stride, const in
     const int64_t jobs = n * seg.count;
     if (jobs >= 4096 && seg.length * (int64_t)sizeof(T) <= 65536)
       long_kernel<T, 64><<<(unsigned)least(jobs, kCus * 32), 64, 0, stream>>>(n, v, x, stride, token, k, o, seg);
+    else if (jobs <= 2 * kCus && seg.length >= 16384)
+      long_kernel<T, 512><<<(unsigned)jobs, 512, 0, stream>>>(n, v, x, stride, token, k, o, seg);
     else
       long_kernel<T, 256><<<(unsigned)least(jobs, kCus * 8), 256, 0, stream>>>(n, v, x, stride, token, k, o, seg);
     if (seg.count > 1)
