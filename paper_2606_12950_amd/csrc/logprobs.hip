@@ -7,7 +7,7 @@
 // A pass reads every logit once and is bound by HBM, but for short rows with alternatives, which are bound by the
 // vector ALU. Measured (a copy reaches 5.0 TB/s): 4,096 rows of 50,257 float32 with 5 alternatives 158 us = 5.2 TB/s,
 // 2,048 of 131,072 bfloat16 with 8 111 us = 4.8; 2^20 rows of 64 bfloat16 30 us without alternatives, 40 with one
-// and 52 with four (floor 38). Gradient: 2^20 x 64 bfloat16 61 us = 4.6 TB/s, 2,048 x 131,072 187 us = 5.7.
+// and 52 with four (floor 38). Gradient: 2^20 x 64 bfloat16 56 us = 5.1 TB/s, 2,048 x 131,072 187 us = 5.7.
 #include "train.h"
 
 namespace maestro {
@@ -15,6 +15,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLeast = -1e30f;     // below any log probability in range; times 0 it is 0
+constexpr float kUnseen = -1e3f;     // below any whose probability is not 0 in float32; times a large coefficient still finite
 constexpr int kMaxAlternatives = MAESTRO_MAX_ALTERNATIVES;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -39,7 +40,27 @@ __device__ __forceinline__ void unpack(const u32x4& w, float (&x)[8]) {
   for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
 }
 
-// the vector at x[j], what lies past v filled with -inf
+// the vector at x[j] as it lies in memory, what lies past v filled with -inf
+__device__ __forceinline__ u32x4 load_raw(const float* x, int32_t j, int32_t v) {
+  if (j + 4 <= v) return load16(x + j);
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = j + i < v ? __float_as_uint(x[j + i]) : 0xFF800000u;
+  return w;
+}
+__device__ __forceinline__ u32x4 load_raw(const __bf16* x, int32_t j, int32_t v) {
+  if (j + 8 <= v) return load16(x + j);
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t lo = j + 2 * i < v ? __builtin_bit_cast(uint16_t, x[j + 2 * i]) : 0xFF80;
+    const uint32_t hi = j + 2 * i + 1 < v ? __builtin_bit_cast(uint16_t, x[j + 2 * i + 1]) : 0xFF80;
+    w[i] = lo | (hi << 16);
+  }
+  return w;
+}
+
+// the same, unpacked
 template <typename T>
 __device__ __forceinline__ void load_vec(const T* x, int64_t j, int64_t v, float (&out)[kVec<T>]) {
   if (j + kVec<T> <= v) {
@@ -238,23 +259,7 @@ __global__ __launch_bounds__(kShortThreads) void short_kernel(int64_t n, int32_t
   // a vector past v, or part of it, is -inf
   auto load = [&](const T* x, u32x4(&w)[R]) {
 #pragma unroll
-    for (int u = 0; u < R; ++u) {
-      const int j = (u * G + g) * V;
-      if (j + V <= v) {
-        w[u] = load16(x + j);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if constexpr (V == 4) {
-            w[u][i] = j + i < v ? __float_as_uint(x[j + i]) : 0xFF800000u;
-          } else {
-            const uint32_t lo = j + 2 * i < v ? __builtin_bit_cast(uint16_t, x[j + 2 * i]) : 0xFF80;
-            const uint32_t hi = j + 2 * i + 1 < v ? __builtin_bit_cast(uint16_t, x[j + 2 * i + 1]) : 0xFF80;
-            w[u][i] = lo | (hi << 16);
-          }
-        }
-      }
-    }
+    for (int u = 0; u < R; ++u) w[u] = load_raw(x, (u * G + g) * V, v);
   };
   const T* x = logits + row * stride;
   const int64_t ahead = step * stride;
@@ -509,14 +514,14 @@ __global__ __launch_bounds__(kThreads) void long_kernel(int64_t n, int32_t v, co
   }
 }
 
-// The segments of a row joined by one wavefront, a segment to a lane: their parts, then k times the best of the
-// segments' next alternatives.
 // order-preserving bits of a visible logit, never 0; -0 equals 0
 __device__ __forceinline__ uint32_t order_of(float x) {
   const uint32_t b = __float_as_uint(x + 0.0f);
   return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 
+// The segments of a row joined by one wavefront, a segment to a lane: their parts, then k times the best of the
+// segments' next alternatives.
 __global__ __launch_bounds__(64) void join_kernel(int64_t n, int32_t v, const void* logits, int64_t stride, bool bf16,
                                                   const int32_t* token, int32_t k, Outputs o, Segments seg) {
   __shared__ float s_value[64 * kMaxAlternatives];
@@ -607,22 +612,62 @@ struct GradRow {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const float lp = (x[i] - m) - log_s, p = __builtin_amdgcn_exp2f(lp * kLog2e);
-      const float c = with_entropy && ge != 0.0f ? fmaf(ge, fmaxf(lp, kLeast) + h, g) : g;
+      const float c = with_entropy && ge != 0.0f ? fmaf(ge, fmaxf(lp, kUnseen) + h, g) : g;
       x[i] = zero ? 0.0f : fmaf(-p, c, hot == i ? g : 0.0f);
     }
   }
 };
 
-// a row to G lanes
-template <typename T, int G>
-__global__ __launch_bounds__(256) void grad_short_kernel(int64_t n, int32_t v, const T* logits, int64_t stride,
-                                                         Gradient a, T* grad, int64_t grad_stride) {
-  constexpr int V = kVec<T>, kRows = 256 / G;
-  const int64_t step = (int64_t)gridDim.x * kRows;
-  for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / G; row < n; row += step) {
+constexpr int kGradAhead = 4;        // vectors of a thread in flight
+// the longest row, in vectors, that shares a workgroup with others: 60,000 x 2,000 float32 168 us so and 188 a wavefront to
+// a row, but 100,000 x 1,025 bfloat16 103 and 87 (more to compute for a vector)
+template <typename T>
+constexpr int kGradShort = sizeof(T) == 4 ? 512 : 64;
+constexpr int kGradRow = 512;        // and the longest that a wavefront takes
+
+// Rows of `vecs` vectors laid end to end, a vector to a thread, whatever rows a wavefront's lie in, so no lane idles at a
+// row's end. magic = ceil(2^21 / vecs): i * magic >> 21 is i / vecs for i < vecs + 1024, vecs <= 1024.
+// Measured (us; a row to a power of two of lanes before): 300,000 x 293 bfloat16 105 (164), 450,209 x 34 float32 33
+// (44), 10^6 x 3 bfloat16 9.5 (13.9), 2^20 x 64 56 (56). Two or four vectors a thread take 5 to 30% longer (registers).
+template <typename T>
+__global__ __launch_bounds__(256) void grad_short_kernel(int64_t n, int32_t v, const T* logits, int64_t stride, Gradient a,
+                                                         T* grad, int64_t grad_stride, uint32_t vecs, uint32_t magic) {
+  constexpr int V = kVec<T>;
+  const int64_t chunks = (n * vecs + 255) / 256;
+  for (int64_t chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
+    const int64_t first = chunk * 256;
+    const int64_t row0 = first >> 32 ? first / vecs : (uint32_t)first / vecs;      // 32 bits: a sixth of the time
+    const uint32_t i = (uint32_t)(first - row0 * vecs) + threadIdx.x, down = i * magic >> 21;
+    const int64_t row = row0 + down;
+    if (row >= n) continue;
+    const int32_t j = (int32_t)(i - down * vecs) * V;
+    const u32x4 w = load_raw(logits + row * stride, j, v);
     GradRow r;
     r.load(a, row, v);
-    for (int j = V * (threadIdx.x % G); j < v; j += V * G) {
+    float x[V];
+    unpack(w, x);
+    r.gradient(x, j, a.g_entropy != nullptr);
+    T* out = grad + row * grad_stride + j;
+    if (j + V <= v) {
+      store16(out, pack(x));
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (j + e < v) out[e] = (T)x[e];
+    }
+  }
+}
+
+// a wavefront to a row
+template <typename T>
+__global__ __launch_bounds__(256) void grad_row_kernel(int64_t n, int32_t v, const T* logits, int64_t stride, Gradient a,
+                                                       T* grad, int64_t grad_stride) {
+  constexpr int V = kVec<T>;
+  const int lane = threadIdx.x & 63;
+  for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < n; row += (int64_t)gridDim.x * 4) {
+    GradRow r;
+    r.load(a, row, v);
+    for (int j = V * lane; j < v; j += V * 64) {
       float x[V];
       load_vec(logits + row * stride, j, v, x);
       r.gradient(x, j, a.g_entropy != nullptr);
@@ -637,8 +682,6 @@ __global__ __launch_bounds__(256) void grad_short_kernel(int64_t n, int32_t v, c
     }
   }
 }
-
-constexpr int kGradAhead = 4;        // vectors of a thread in flight
 
 // a workgroup takes 256 kGradAhead vectors of a row
 template <typename T>
@@ -735,23 +778,17 @@ maestro_status launch(int64_t n, int32_t v, const T* x, int64_t stride, const in
   return launch_status();
 }
 
-template <typename T, int G>
-void launch_grad_short(int64_t n, int32_t v, const T* x, int64_t stride, const Gradient& a, T* grad, int64_t grad_stride,
-                       hipStream_t stream) {
-  const int64_t blocks = cdiv(n, 256 / G);
-  grad_short_kernel<T, G><<<(unsigned)least(blocks, kCus * 64), 256, 0, stream>>>(n, v, x, stride, a, grad, grad_stride);
-}
-
 template <typename T>
 maestro_status launch_grad(int64_t n, int32_t v, const T* x, int64_t stride, const Gradient& a, T* grad,
                            int64_t grad_stride, hipStream_t stream) {
   const int64_t vecs = cdiv(v, kVec<T>);
-  if (vecs <= 2) launch_grad_short<T, 2>(n, v, x, stride, a, grad, grad_stride, stream);
-  else if (vecs <= 8) launch_grad_short<T, 8>(n, v, x, stride, a, grad, grad_stride, stream);
-  else if (vecs <= 16) launch_grad_short<T, 16>(n, v, x, stride, a, grad, grad_stride, stream);
-  else if (vecs <= 32) launch_grad_short<T, 32>(n, v, x, stride, a, grad, grad_stride, stream);
-  else if (vecs <= 512) launch_grad_short<T, 64>(n, v, x, stride, a, grad, grad_stride, stream);
-  else {
+  if (vecs <= kGradShort<T>)
+    grad_short_kernel<T><<<(unsigned)least(cdiv(n * vecs, 256), kCus * 64), 256, 0, stream>>>(
+        n, v, x, stride, a, grad, grad_stride, (uint32_t)vecs, (uint32_t)cdiv(1 << 21, vecs));
+  else if (vecs <= kGradRow) {
+    if constexpr (kGradShort<T> < kGradRow)
+      grad_row_kernel<T><<<(unsigned)least(cdiv(n, 4), kCus * 64), 256, 0, stream>>>(n, v, x, stride, a, grad, grad_stride);
+  } else {
     const int32_t parts = (int32_t)cdiv(vecs, 256 * kGradAhead);
     grad_long_kernel<T><<<(unsigned)least(n * parts, kCus * 64), 256, 0, stream>>>(n, v, x, stride, a, grad, grad_stride, parts);
   }
