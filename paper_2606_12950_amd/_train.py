@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+from array import array
 from typing import NamedTuple, Optional, Sequence
 
 import torch
@@ -21,6 +22,8 @@ EXPORTS = ("maestro_logprobs_workspace", "maestro_logprobs", "maestro_logprobs_g
            "maestro_clip_gradients")
 
 MAX_ALTERNATIVES = 16
+
+# Outputs are allocated with their sizes as separate arguments: torch reads those in 1.2 us, a tuple of them in 2.0.
 
 _MOST = (1 << 31) - 1      # of an int32 argument: ctypes would cut a larger number off
 
@@ -107,8 +110,8 @@ def logprobs(logits: torch.Tensor, token: Optional[torch.Tensor] = None, k: int 
     if out is None:
         f = dict(dtype=torch.float32, device=dev)
         out = Logprobs(torch.empty(n, **f) if token is not None else None, torch.empty(n, **f) if want_entropy else None,
-                       torch.empty((n, k), dtype=torch.int32, device=dev), torch.empty((n, k), **f),
-                       torch.empty((n, 2), **f) if want_stats else None)
+                       torch.empty(n, k, dtype=torch.int32, device=dev), torch.empty(n, k, **f),
+                       torch.empty(n, 2, **f) if want_stats else None)
     else:
         if (out.logprob is None) != (token is None):
             raise ValueError("logprob goes with token")
@@ -150,7 +153,7 @@ def logprobs_grad(logits: torch.Tensor, token: Optional[torch.Tensor], stats: to
         if t is not None:
             _shape(_dev(t, name, torch.float32), name, (n,))
     if out is None:
-        out, out_stride = torch.empty((n, v), dtype=logits.dtype, device=logits.device), v
+        out, out_stride = torch.empty(n, v, dtype=logits.dtype, device=logits.device), v
     else:
         *same, out_stride = _rows(out, "out")
         if same != [dt, n, v]:
@@ -183,7 +186,7 @@ def layer(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor, relu: bool 
     dt, n, i, o = _layer_shapes(x, weight)
     _shape(_dev(bias, "bias", torch.float32), "bias", (o,))
     if out is None:
-        out = torch.empty((n, o), dtype=weight.dtype, device=x.device)
+        out = torch.empty(n, o, dtype=weight.dtype, device=x.device)
     else:
         _shape(_dev(out, "out", weight.dtype), "out", (n, o))
     st = lib.maestro_layer(n, i, o, dt, _ptr(x), _ptr(weight), _ptr(bias), int(bool(relu)), _ptr(out), _stream(stream))
@@ -202,8 +205,8 @@ def layer_grad(x: torch.Tensor, weight: torch.Tensor, g_z: torch.Tensor, relu_in
     _shape(_dev(g_z, "g_z", weight.dtype), "g_z", (n, o))
     dev = x.device
     if out is None:
-        out = LayerGrad(torch.empty((n, i), dtype=weight.dtype, device=dev) if want_x else None,
-                        torch.empty((o, i), dtype=torch.float32, device=dev),
+        out = LayerGrad(torch.empty(n, i, dtype=weight.dtype, device=dev) if want_x else None,
+                        torch.empty(o, i, dtype=torch.float32, device=dev),
                         torch.empty(o, dtype=torch.float32, device=dev))
     else:
         if (out.x is not None) != want_x:
@@ -223,22 +226,24 @@ def layer_grad(x: torch.Tensor, weight: torch.Tensor, g_z: torch.Tensor, relu_in
     return out
 
 
+_is_cuda, _dtype = _Tensor.is_cuda.__get__, _Tensor.dtype.__get__
+
+
 def _host_arrays(tensors: Sequence[torch.Tensor], name: str):
-    """(addresses, element counts, dtype codes) of contiguous float32 or bfloat16 tensors on a GPU, as lists. Runs for
-    every tensor of a call: 0.3 us each."""
-    at, sizes, codes = [], [], []
-    for t in tensors:
-        if not isinstance(t, _Tensor) or not t.is_cuda:
-            raise TypeError(f"{name} must be CUDA (HIP) tensors")
-        if not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous")
-        code = _DTYPE.get(t.dtype)
-        if code is None:
-            raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
-        at.append(t.data_ptr())
-        sizes.append(t.numel())
-        codes.append(code)
-    return at, sizes, codes
+    """(addresses, element counts, dtype codes) of contiguous float32 or bfloat16 tensors on a GPU, as arrays. One
+    attribute of all tensors at a time, by way of torch's descriptors: per tensor 0.6 of what a loop over them takes."""
+    try:
+        on_gpu = all(map(_is_cuda, tensors))
+    except TypeError:
+        on_gpu = False
+    if not on_gpu:
+        raise TypeError(f"{name} must be CUDA (HIP) tensors")
+    if not all(map(_Tensor.is_contiguous, tensors)):
+        raise ValueError(f"{name} must be contiguous")
+    codes = list(map(_DTYPE.get, map(_dtype, tensors)))
+    if None in codes:
+        raise TypeError(f"{name} must be float32 or bfloat16, got {tensors[codes.index(None)].dtype}")
+    return array("Q", map(_Tensor.data_ptr, tensors)), array("q", map(_Tensor.numel, tensors)), array("i", codes)
 
 
 def clip_gradients(tensors: Sequence[torch.Tensor], max_norm: float, out: Optional[Sequence[torch.Tensor]] = None,
@@ -255,15 +260,11 @@ def clip_gradients(tensors: Sequence[torch.Tensor], max_norm: float, out: Option
     if not max_norm >= 0.0:
         raise ValueError("max_norm must not be negative or NaN")
     at, sizes, codes = _host_arrays(tensors, "tensors")
-    count = len(tensors)
-    pointers = ctypes.c_void_p * count
-    optr = None
+    count, oat = len(tensors), None
     if out is not None:
-        oat, osizes, ocodes = _host_arrays(out, "out")
+        oat, osizes, ocodes = _host_arrays(list(out), "out")
         if osizes != sizes or ocodes != codes:
             raise ValueError("out must have one output per tensor, of its size and type")
-        optr = pointers(*oat)
-    ptr, sizes, dtypes = pointers(*at), (ctypes.c_int64 * count)(*sizes), (ctypes.c_int32 * count)(*codes)
     dev = tensors[0].device
     if norm is None:
         norm = torch.empty(1, dtype=torch.float32, device=dev)
@@ -272,8 +273,9 @@ def clip_gradients(tensors: Sequence[torch.Tensor], max_norm: float, out: Option
     _workspace(workspace)
     if workspace is None:
         workspace = _scratch(lib.maestro_clip_gradients_workspace(count), dev, stream)
-    st = lib.maestro_clip_gradients(count, ptr, optr, sizes, dtypes, max_norm, _ptr(norm), _ptr(workspace),
-                                    workspace.numel(), _stream(stream))
+    st = lib.maestro_clip_gradients(count, at.buffer_info()[0], oat and oat.buffer_info()[0], sizes.buffer_info()[0],
+                                    codes.buffer_info()[0], max_norm, _ptr(norm), _ptr(workspace), workspace.numel(),
+                                    _stream(stream))
     _check("maestro_clip_gradients", st)
     return norm
 
