@@ -321,26 +321,37 @@ __device__ __forceinline__ void store_rows(const Out& out, const Product& g, uns
   }
 }
 
+// Sizes of a product's tile, and its LDS.
+template <int WP, int WQ, int kDepth, int kBufs, class Out>
+struct Tile {
+  static constexpr int TP = 64 * WP, TQ = 64 * WQ;          // four wavefronts
+  static constexpr int kStage = (TP + TQ) * 2 * kDepth;
+  static constexpr bool kStores = !std::is_same<Out, WeightGrad>::value;      // by way of LDS
+  static constexpr int kBiasLoads = Out::kBias ? (WP + 1) / 2 : 0;
+  static constexpr int kBiasBytes = 2 * 4 * 256 * kBiasLoads;                 // two places for each wavefront
+  static constexpr int kBytes = kBufs * kStage + (kStores ? 4 * Staging<WP>::kBytes : 0) + kBiasBytes;
+  static constexpr int kResident = WP * WQ > 8 ? 1 : WP * WQ > 2 ? 2 : 4;     // workgroups of a CU
+};
+
+// The share of workgroup `block` of `blocks` (a multiple of 8) in a product.
 template <int WP, int WQ, int kDepth, int kBufs, bool kPT, bool kQT, class Out>
-__global__ __launch_bounds__(kThreads, WP * WQ > 8 ? 1 : WP * WQ > 2 ? 2 : 4) void product_kernel(Product g, Out out) {
-  constexpr int NP = 2, NQ = 2;                             // four wavefronts
-  constexpr int TP = 32 * WP * NP, TQ = 32 * WQ * NQ;
-  constexpr int kStage = (TP + TQ) * 2 * kDepth, kLoads = (TP + TQ) * kDepth / 2048, kHalves = kDepth / 16;
+__device__ __forceinline__ void product(const Product& g, const Out& out, unsigned char* lds, uint32_t block, uint32_t blocks) {
+  using L = Tile<WP, WQ, kDepth, kBufs, Out>;
+  constexpr int NP = 2, TP = L::TP, TQ = L::TQ;
+  constexpr int kStage = L::kStage, kLoads = (TP + TQ) * kDepth / 2048, kHalves = kDepth / 16;
   constexpr int kQ = TP * 2 * kDepth;                       // Q's place in a stage
   constexpr bool kSums = kQT;                               // the weights' gradient sums Q too (the biases')
-  constexpr int kBiasLoads = Out::kBias ? (WP + 1) / 2 : 0;
+  constexpr int kBiasLoads = L::kBiasLoads;
   constexpr int kStores = kSums ? 0 : 2 * WP * WQ + kBiasLoads;      // between two tiles, exactly
-  static_assert(kLoads * (kBufs - 2) + kStores < 64, "vmcnt range");
-  constexpr int kBiasBytes = 2 * 4 * 256 * kBiasLoads;      // two places for each wavefront
-  __shared__ __attribute__((aligned(16))) unsigned char lds[kBufs * kStage + (kSums ? 0 : 4 * Staging<WP>::kBytes) + kBiasBytes];
+  static_assert(kSums != L::kStores && kLoads * (kBufs - 2) + kStores < 64, "vmcnt range");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wp = wave % NP, wq = wave / NP;
 
   // XCD x (of 8; workgroups go round them) takes a contiguous share of the items, so that the tiles that read
   // the same rows of Q run side by side on one L2
-  const int64_t share = (g.items + 7) / 8, xcd = blockIdx.x & 7, step = gridDim.x >> 3;
+  const int64_t share = (g.items + 7) / 8, xcd = block & 7, step = blocks >> 3;
   const int64_t last = (xcd + 1) * share < g.items ? (xcd + 1) * share : g.items;
-  const int64_t first = xcd * share + (blockIdx.x >> 3);
+  const int64_t first = xcd * share + (block >> 3);
   if (first >= last) return;
 
   struct Item {
@@ -547,6 +558,22 @@ __global__ __launch_bounds__(kThreads, WP * WQ > 8 ? 1 : WP * WQ > 2 ? 2 : 4) vo
   wait_loads<0>();                                          // no load into LDS outlives the workgroup
 }
 
+template <int WP, int WQ, int kDepth, int kBufs, bool kPT, bool kQT, class Out>
+__global__ __launch_bounds__(kThreads, (Tile<WP, WQ, kDepth, kBufs, Out>::kResident)) void product_kernel(Product g, Out out) {
+  __shared__ __attribute__((aligned(16))) unsigned char lds[Tile<WP, WQ, kDepth, kBufs, Out>::kBytes];
+  product<WP, WQ, kDepth, kBufs, kPT, kQT>(g, out, lds, blockIdx.x, gridDim.x);
+}
+
+// Both gradients in one launch: the first `blocks` workgroups make the input's, in 64 x 64 tiles, the others the weights'.
+template <int WP, int WQ>
+__global__ __launch_bounds__(kThreads, 2) void pair_kernel(Product gx, InputGrad x, uint32_t blocks, Product gw, WeightGrad w) {
+  using X = Tile<1, 1, 64, 2, InputGrad>;
+  using W = Tile<WP, WQ, 64, 2, WeightGrad>;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[X::kBytes > W::kBytes ? X::kBytes : W::kBytes];
+  if (blockIdx.x < blocks) product<1, 1, 64, 2, true, false>(gx, x, lds, blockIdx.x, blocks);
+  else product<WP, WQ, 64, 2, true, true>(gw, w, lds, blockIdx.x - blocks, gridDim.x - blocks);
+}
+
 // g_w and g_b from their shares, summed in a fixed order. A quad of values to each of 256 / G neighbouring threads, its
 // shares dealt out over G groups of them, each with the loads of eight shares issued before the first is added. G = 16
 // where there are few values for the chip: the gradients of 91,341 x 32 -> 48 float32 (357 shares) take 31 us so and 45 in
@@ -595,16 +622,27 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const float* gw_parts, i
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int64_t kCus = 256;
 
+// the rest of a product's numbers, and its workgroups
+template <class Tile>
+uint32_t plan(Product& g) {
+  g.p_tiles = (int32_t)cdiv(g.np, Tile::TP);
+  g.splits = (int32_t)cdiv(g.nk, g.k_split);
+  g.items = cdiv(g.nq, Tile::TQ) * g.p_tiles * g.splits;
+  const int64_t want = cdiv(g.items, 8) * 8, most = kCus * Tile::kResident;
+  return (uint32_t)(want < most ? want : most);
+}
+
 template <int WP, int WQ, int kDepth, int kBufs, bool kPT, bool kQT, class Out>
 maestro_status launch(Product g, const Out& out, hipStream_t stream) {
-  constexpr int TP = 64 * WP, TQ = 64 * WQ;
-  constexpr int64_t kResident = WP * WQ > 8 ? 1 : WP * WQ > 2 ? 2 : 4;     // workgroups of a CU
-  g.p_tiles = (int32_t)cdiv(g.np, TP);
-  g.splits = (int32_t)cdiv(g.nk, g.k_split);
-  g.items = cdiv(g.nq, TQ) * g.p_tiles * g.splits;
-  const auto kernel = product_kernel<WP, WQ, kDepth, kBufs, kPT, kQT, Out>;
-  const int64_t want = cdiv(g.items, 8) * 8, most = kCus * kResident;
-  kernel<<<(unsigned)(want < most ? want : most), kThreads, 0, stream>>>(g, out);
+  const uint32_t blocks = plan<Tile<WP, WQ, kDepth, kBufs, Out>>(g);
+  product_kernel<WP, WQ, kDepth, kBufs, kPT, kQT, Out><<<blocks, kThreads, 0, stream>>>(g, out);
+  return launch_status();
+}
+
+template <int WP, int WQ>
+maestro_status launch_pair(Product gx, const InputGrad& x, Product gw, const WeightGrad& w, hipStream_t stream) {
+  const uint32_t blocks = plan<Tile<1, 1, 64, 2, InputGrad>>(gx), more = plan<Tile<WP, WQ, 64, 2, WeightGrad>>(gw);
+  pair_kernel<WP, WQ><<<blocks + more, kThreads, 0, stream>>>(gx, x, blocks, gw, w);
   return launch_status();
 }
 
@@ -624,8 +662,9 @@ template <bool kPT, class Out>
 maestro_status launch_rows(const Product& g, const Out& out, hipStream_t stream) {
   const int tile = tile_of(g.np, g.nq);
   if (tile == 256) return launch<4, 4, 64, 2, kPT, false>(g, out, stream);
-  if (tile == 128) return launch<2, 2, 64, 2, kPT, false>(g, out, stream);
-  return launch<1, 1, 64, 2, kPT, false>(g, out, stream);
+  if constexpr (!kPT)                                       // the input's gradient of this size: pair_kernel
+    if (tile == 64) return launch<1, 1, 64, 2, kPT, false>(g, out, stream);
+  return launch<2, 2, 64, 2, kPT, false>(g, out, stream);
 }
 
 // How the weights' gradient is cut: tile, k of one split, splits of the n rows, and workgroups that share the
@@ -671,20 +710,25 @@ maestro_status launch_layer_grad_bf16(int64_t n, int32_t d_in, int32_t d_out, co
                                       const void* g_z, bool relu_input, void* g_x, float* g_weight, float* g_bias,
                                       void* workspace, hipStream_t stream) {
   const __bf16 *xb = static_cast<const __bf16*>(x), *gz = static_cast<const __bf16*>(g_z);
-  if (g_x) {
-    Product g{static_cast<const __bf16*>(weight), gz, d_in, d_out, d_in, n, d_out, d_out, 1, 0, 0};
-    const maestro_status st =
-        launch_rows<true>(g, InputGrad{xb, static_cast<__bf16*>(g_x), relu_input}, stream);
-    if (st != MAESTRO_OK) return st;
-  }
   const Cut c = cut_of(n, d_in, d_out);
   float* parts = static_cast<float*>(workspace);
   float* gb_parts = parts + c.splits * d_in * d_out;
-  Product g{xb, gz, d_in, d_out, d_in, d_out, n, c.k_split, 1, 0, 0};
-  const WeightGrad out{c.splits > 1 ? parts : g_weight, c.splits > 1 ? gb_parts : g_bias, c.parts};
-  const maestro_status st = c.tq == 256   ? launch<4, 4, 32, 4, true, true>(g, out, stream)
-                            : c.tp == 256 ? launch<4, 1, 64, 2, true, true>(g, out, stream)
-                                          : launch<2, 2, 64, 2, true, true>(g, out, stream);
+  const Product gw{xb, gz, d_in, d_out, d_in, d_out, n, c.k_split, 1, 0, 0};
+  const WeightGrad w{c.splits > 1 ? parts : g_weight, c.splits > 1 ? gb_parts : g_bias, c.parts};
+  const Product gx{static_cast<const __bf16*>(weight), gz, d_in, d_out, d_in, n, d_out, d_out, 1, 0, 0};
+  const InputGrad x_out{xb, static_cast<__bf16*>(g_x), relu_input};
+  maestro_status st = MAESTRO_OK;
+  // Little work: a launch less, and the two products side by side. 300 x 256 -> 512 11.8 us (14.6 in two launches),
+  // 2,000 x 512 -> 512 16.7 (22.6), 30,000 x 64 -> 128 18.7 (20.2)
+  if (g_x && tile_of(d_in, n) == 64) {
+    st = c.tp == 256 ? launch_pair<4, 1>(gx, x_out, gw, w, stream) : launch_pair<2, 2>(gx, x_out, gw, w, stream);
+  } else {
+    if (g_x) st = launch_rows<true>(gx, x_out, stream);
+    if (st != MAESTRO_OK) return st;
+    st = c.tq == 256   ? launch<4, 4, 32, 4, true, true>(gw, w, stream)
+         : c.tp == 256 ? launch<4, 1, 64, 2, true, true>(gw, w, stream)
+                       : launch<2, 2, 64, 2, true, true>(gw, w, stream);
+  }
   if (st != MAESTRO_OK || c.splits == 1) return st;
   return launch_join(parts, (int32_t)c.splits, g_weight, (int64_t)d_in * d_out, gb_parts, (int32_t)(c.splits * c.parts * 2),
                      g_bias, d_out, stream);
