@@ -2,13 +2,14 @@
 
 Argument marshalling only, in the manner of ``_native``: the tensors are checked, outputs and
 workspaces allocated where the caller passes none, and every computation runs in the HIP kernels of
-libmaestro.so on the current stream. There is no fallback.
+libmaestro.so on the current stream. Where Python would take longer than the GPU (hundreds of tensors,
+several outputs) the native module ``_tensors`` does it. There is no fallback.
 """
 from __future__ import annotations
 
 import ctypes
 import math
-from array import array
+import os
 from typing import NamedTuple, Optional, Sequence
 
 import torch
@@ -22,6 +23,8 @@ EXPORTS = ("maestro_logprobs_workspace", "maestro_logprobs", "maestro_logprobs_g
            "maestro_clip_gradients")
 
 MAX_ALTERNATIVES = 16
+
+TENSORS_PATH = os.path.join(os.path.dirname(_native.LIBRARY_PATH), "_tensors.so")
 
 # Outputs are allocated with their sizes as separate arguments: torch reads those in 1.2 us, a tuple of them in 2.0.
 
@@ -48,15 +51,19 @@ class LayerGrad(NamedTuple):
     bias: torch.Tensor
 
 
-_lib = None
+_lib = _tensors = None
 
 
 def load():
-    """libmaestro.so with the argument types of the training operators set."""
-    global _lib
+    """libmaestro.so with the argument types of the training operators set, and the binding's host half."""
+    global _lib, _tensors
     if _lib is not None:
         return _lib
     lib = _native.load()
+    if not os.path.exists(TENSORS_PATH):
+        raise RuntimeError(f"{TENSORS_PATH} is missing: build it first (python -m paper_2606_12950_amd.build)")
+    from . import _tensors as module
+    _tensors = module
     P, i32, i64, f32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
     lib.maestro_logprobs_workspace.argtypes = [i64, i32, i32, i32]
     lib.maestro_logprobs.argtypes = [i64, i32, P, i64, i32, P, i32, P, P, P, P, P, P, sz, P]
@@ -108,10 +115,9 @@ def logprobs(logits: torch.Tensor, token: Optional[torch.Tensor] = None, k: int 
     if token is not None:
         _shape(_dev(token, "token", torch.int32), "token", (n,))
     if out is None:
-        f = dict(dtype=torch.float32, device=dev)
-        out = Logprobs(torch.empty(n, **f) if token is not None else None, torch.empty(n, **f) if want_entropy else None,
-                       torch.empty(n, k, dtype=torch.int32, device=dev), torch.empty(n, k, **f),
-                       torch.empty(n, 2, **f) if want_stats else None)
+        row = ((n,), False)
+        out = Logprobs._make(_tensors.empties(logits, row if token is not None else None, row if want_entropy else None,
+                                              ((n, k), True), ((n, k), False), ((n, 2), False) if want_stats else None))
     else:
         if (out.logprob is None) != (token is None):
             raise ValueError("logprob goes with token")
@@ -226,26 +232,6 @@ def layer_grad(x: torch.Tensor, weight: torch.Tensor, g_z: torch.Tensor, relu_in
     return out
 
 
-_is_cuda, _dtype = _Tensor.is_cuda.__get__, _Tensor.dtype.__get__
-
-
-def _host_arrays(tensors: Sequence[torch.Tensor], name: str):
-    """(addresses, element counts, dtype codes) of contiguous float32 or bfloat16 tensors on a GPU, as arrays. One
-    attribute of all tensors at a time, by way of torch's descriptors: per tensor 0.6 of what a loop over them takes."""
-    try:
-        on_gpu = all(map(_is_cuda, tensors))
-    except TypeError:
-        on_gpu = False
-    if not on_gpu:
-        raise TypeError(f"{name} must be CUDA (HIP) tensors")
-    if not all(map(_Tensor.is_contiguous, tensors)):
-        raise ValueError(f"{name} must be contiguous")
-    codes = list(map(_DTYPE.get, map(_dtype, tensors)))
-    if None in codes:
-        raise TypeError(f"{name} must be float32 or bfloat16, got {tensors[codes.index(None)].dtype}")
-    return array("Q", map(_Tensor.data_ptr, tensors)), array("q", map(_Tensor.numel, tensors)), array("i", codes)
-
-
 def clip_gradients(tensors: Sequence[torch.Tensor], max_norm: float, out: Optional[Sequence[torch.Tensor]] = None,
                    norm: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                    stream=None) -> torch.Tensor:
@@ -259,10 +245,10 @@ def clip_gradients(tensors: Sequence[torch.Tensor], max_norm: float, out: Option
     max_norm = float(max_norm)
     if not max_norm >= 0.0:
         raise ValueError("max_norm must not be negative or NaN")
-    at, sizes, codes = _host_arrays(tensors, "tensors")
+    at, sizes, codes = _tensors.table(tensors, "tensors")
     count, oat = len(tensors), None
     if out is not None:
-        oat, osizes, ocodes = _host_arrays(list(out), "out")
+        oat, osizes, ocodes = _tensors.table(list(out), "out")
         if osizes != sizes or ocodes != codes:
             raise ValueError("out must have one output per tensor, of its size and type")
     dev = tensors[0].device
@@ -273,9 +259,8 @@ def clip_gradients(tensors: Sequence[torch.Tensor], max_norm: float, out: Option
     _workspace(workspace)
     if workspace is None:
         workspace = _scratch(lib.maestro_clip_gradients_workspace(count), dev, stream)
-    st = lib.maestro_clip_gradients(count, at.buffer_info()[0], oat and oat.buffer_info()[0], sizes.buffer_info()[0],
-                                    codes.buffer_info()[0], max_norm, _ptr(norm), _ptr(workspace), workspace.numel(),
-                                    _stream(stream))
+    st = lib.maestro_clip_gradients(count, at, oat, sizes, codes, max_norm, _ptr(norm), _ptr(workspace),
+                                    workspace.numel(), _stream(stream))
     _check("maestro_clip_gradients", st)
     return norm
 

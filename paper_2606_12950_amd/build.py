@@ -1,5 +1,6 @@
 """Build libmaestro.so (gfx950) in-tree with hipcc, and beside it libmaestro_calibrate.so, the
-measurement-only matrix-core ceiling kernel that bench.py --mfma-ceiling times.
+measurement-only matrix-core ceiling kernel that bench.py --mfma-ceiling times, and _tensors.so, the host
+half of the training operators' binding (g++).
 
 Usage: python -m paper_2606_12950_amd.build [-v]
 """
@@ -9,6 +10,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 import tempfile
 from concurrent.futures import ThreadPoolExecutor
 
@@ -21,6 +23,9 @@ SOURCES = ("api.hip", "predict.hip", "predict_split.hip", "roles.hip", "route.hi
            "train_api.hip", "logprobs.hip", "layers.hip", "layers_bf16.hip", "clip.hip")
 CALIBRATE_LIB = os.path.join(PKG, "libmaestro_calibrate.so")
 CALIBRATE_SOURCE = "calibrate.hip"
+# the host half of the binding, against torch's C++ interface
+TENSORS_LIB = os.path.join(PKG, "_tensors.so")
+TENSORS_SOURCE = "tensors.cpp"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
@@ -56,12 +61,36 @@ def _compile(src: str, outdir: str, verbose: bool) -> str:
     return obj
 
 
+def _compile_tensors(outdir: str, verbose: bool) -> str:
+    import torch
+    from torch.utils import cpp_extension
+
+    out = os.path.join(outdir, os.path.basename(TENSORS_LIB))
+    include = [*cpp_extension.include_paths(), sysconfig.get_paths()["include"]]
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *(f"-I{p}" for p in include),
+           os.path.join(CSRC, TENSORS_SOURCE), "-o", out, *(f"-L{p}" for p in cpp_extension.library_paths()),
+           "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{cmd[0]} failed for {TENSORS_SOURCE}:\n{r.stdout}{r.stderr}")
+    return out
+
+
+def _install(built: str, lib: str) -> None:
+    shutil.copyfile(built, lib + ".tmp")
+    os.replace(lib + ".tmp", lib)
+
+
 def build(verbose: bool = False) -> str:
-    """Compile every HIP source for gfx950 and link libmaestro.so next to this file."""
+    """Compile every HIP source for gfx950 and link libmaestro.so next to this file, and the binding's host half."""
     if not os.path.exists(HIPCC):
         raise RuntimeError(f"hipcc not found at {HIPCC}")
     with tempfile.TemporaryDirectory(prefix="maestro_build_") as tmp:
-        with ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        with ThreadPoolExecutor(max_workers=len(SOURCES) + 2) as ex:
+            tensors = ex.submit(_compile_tensors, tmp, verbose)
             objs = list(ex.map(lambda s: _compile(s, tmp, verbose), SOURCES + (CALIBRATE_SOURCE,)))
         for lib, lib_objs in ((LIB, objs[:-1]), (CALIBRATE_LIB, objs[-1:])):
             out = os.path.join(tmp, os.path.basename(lib))
@@ -69,8 +98,8 @@ def build(verbose: bool = False) -> str:
             if verbose:
                 print(" ".join(cmd), flush=True)
             subprocess.run(cmd, check=True)
-            shutil.copyfile(out, lib + ".tmp")
-            os.replace(lib + ".tmp", lib)
+            _install(out, lib)
+        _install(tensors.result(), TENSORS_LIB)
     return LIB
 
 
