@@ -349,9 +349,10 @@ struct Segments {
 // the cache; hardly more than k of them, by all threads together), and of these only the logits that reach it are ranked. Where more than
 // kCandidates do (long runs of equal logits), k scans find them instead.
 //
-// A wavefront to a row (no barriers, 64 threads) where rows are many and short, 512 threads where they are few and long, else 256.
-// Measured (us): 16,384 x 4,096 bfloat16 36 with 64 threads and 110 with 256, 4,096 x 20,000 39 and 48, but
-// 2,048 x 131,072 171 and 111; one row of 32,000 with eight alternatives 8.6 with 256 and 7.8 with 512, one of 5,000
+// A wavefront to a row (no barriers, 64 threads) where rows are short (8 KB, any number of them) or many, 512 threads where they
+// are few and long, else 256. Measured (us): 16,384 x 4,096 bfloat16 36 with 64 threads and 110 with 256, 4,096 x 20,000 39 and
+// 48, 2,500 x 8,000 16.4 and 18.6, but 4,082 x 16,000 float32 60 and 51, 1,000 x 4,000 9.3 and 8.1, 2,048 x 131,072
+// bfloat16 171 and 111; 4,082 x 2,000 float32 11.0 and 22.7, 3 of them 6.2 and 6.0; one row of 32,000 with eight alternatives 8.6 with 256 and 7.8 with 512, one of 5,000
 // 6.6 and 7.5. Against short_kernel's widest form 64 threads take 88 to 106 at 65,536 x 2,048 bfloat16, 190 to 98 at
 // 131,072 x 1,000.
 template <typename T, int kThreads>
@@ -766,7 +767,8 @@ maestro_status launch(int64_t n, int32_t v, const T* x, int64_t stride, const in
       seg.id = reinterpret_cast<int32_t*>(seg.value + n * seg.count * k);
     }
     const int64_t jobs = n * seg.count;
-    if (jobs >= 4096 && seg.length * (int64_t)sizeof(T) <= 65536)
+    const int64_t bytes = seg.length * (int64_t)sizeof(T);
+    if (bytes <= 8192 || (bytes <= 40960 && jobs >= 2048))
       long_kernel<T, 64><<<(unsigned)least(jobs, kCus * 32), 64, 0, stream>>>(n, v, x, stride, token, k, o, seg);
     else if (jobs <= 2 * kCus && seg.length >= 16384)
       long_kernel<T, 512><<<(unsigned)jobs, 512, 0, stream>>>(n, v, x, stride, token, k, o, seg);
