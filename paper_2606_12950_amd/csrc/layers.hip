@@ -187,17 +187,24 @@ void launch(Product g, const Out& out, hipStream_t stream) {
   product_kernel<W, kPT, kQT><<<blocks, kThreads, 0, stream>>>(g, out);
 }
 
-// 128 x 128 tiles where there are two rounds of them, else 64 x 64.
+// 128 x 128 tiles where there are two rounds of them, else 64 x 64. Activations take the larger ones only where k is long
+// and 128 columns fit no worse than 64. Measured (us, 128 / 64): activations of 150,000 x 80 -> 160 75 / 53, 128 -> 128 64 /
+// 59, 192 -> 192 167 / 135, 256 -> 256 233 / 235, 60,000 x 1024 -> 1024 1163 / 1215; input's gradients of 150,000 x 256 ->
+// 256 210 / 257, 60,000 x 1024 -> 1024 1074 / 1658.
 bool wide(int64_t np, int64_t nq) { return np > 64 && nq > 64 && cdiv(np, 128) * cdiv(nq, 128) >= 2 * kCus; }
+bool wide_forward(int64_t np, int64_t nq, int64_t nk) { return wide(np, nq) && nk >= 192 && cdiv(np, 64) % 2 == 0; }
 
-// The weights' gradient: the rows split so that there are about two workgroups a CU, none with fewer than 256 rows
+// The weights' gradient: the rows split so that there are about two workgroups a CU, none with fewer than 256 rows. 128 x 128
+// tiles for many rows where they hold at most 1.2 times what 64 x 64 ones do: 150,000 x 192 -> 192 191 us (150 with 64), 256 ->
+// 256 203 (246), 96 -> 96 58 (68).
 struct Cut {
   bool wide;
   int64_t k_split, splits;
 };
 Cut cut_of(int64_t n, int64_t d_in, int64_t d_out) {
   Cut c;
-  c.wide = d_in > 64 && d_out > 64 && n >= 32768;
+  const int64_t large = 4 * cdiv(d_in, 128) * cdiv(d_out, 128), small = cdiv(d_in, 64) * cdiv(d_out, 64);
+  c.wide = d_in > 64 && d_out > 64 && n >= 32768 && 5 * large <= 6 * small;
   const int64_t t = c.wide ? 128 : 64, tiles = cdiv(d_in, t) * cdiv(d_out, t);
   int64_t splits = 2 * kCus / tiles;
   if (splits > cdiv(n, 256)) splits = cdiv(n, 256);
@@ -214,7 +221,7 @@ maestro_status launch_layer(int64_t n, int32_t d_in, int32_t d_out, int32_t dtyp
   if (dtype == MAESTRO_BF16) return launch_layer_bf16(n, d_in, d_out, x, weight, bias, relu, y, stream);
   const Product g{static_cast<const float*>(weight), static_cast<const float*>(x), d_in, d_in, d_out, n, d_in, d_in, 1, 0, 0};
   const Forward out{bias, static_cast<float*>(y), relu};
-  if (wide(d_out, n)) launch<2, false, false>(g, out, stream);
+  if (wide_forward(d_out, n, d_in)) launch<2, false, false>(g, out, stream);
   else launch<1, false, false>(g, out, stream);
   return launch_status();
 }
