@@ -195,3 +195,23 @@ def test_refusals():
                      (lambda: M.layer_grad(x, w, gz.float()), TypeError)):
         with pytest.raises(err):
             bad()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,i,o", [(338, 128, 128), (512, 32, 32), (513, 32, 32), (2000, 512, 512), (8192, 256, 64), (40000, 192, 192),
+                                   (40001, 80, 160), (40000, 256, 144), (91341, 32, 48), (33000, 208, 256)])
+def test_forms(n, i, o, dtype):
+    """Both gradients in one launch or two, one or many shares of the rows, tiles that the widths do not fill."""
+    print(f"forms n={n} {i}->{o} {dtype}", flush=True)
+    x, w, b, gz = draw(n, i, o, dtype, n + 7 * i + o)
+    xd, wd, gd = x.double(), w.double(), gz.double()
+    z = xd @ wd.t() + b.double()
+    near(M.layer(x.cuda(), w.cuda(), b.cuda(), relu=False), z,
+         bound(xd, wd.t()) + 2.0 ** -23 * b.double().abs() + ROUND[dtype] * z.abs(), "z")
+    gx = gd @ wd
+    for want_x in (True, False):
+        got = M.layer_grad(x.cuda(), w.cuda(), gz.cuda(), want_x=want_x)
+        near(got.weight, gd.t() @ xd, bound(gd.t(), xd) + 1e-38, "weight")
+        near(got.bias, gd.sum(0), bound(gd.t(), torch.ones(n, 1, dtype=torch.float64))[:, 0] + 1e-38, "bias")
+        if want_x:
+            near(got.x, gx, bound(gd, wd) + ROUND[dtype] * gx.abs(), "x")

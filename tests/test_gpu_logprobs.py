@@ -376,3 +376,41 @@ def test_refusals():
                      (lambda: M.logprobs_grad(x, t, s, f, f, out=x.bfloat16()), ValueError)):
         with pytest.raises(err):
             bad()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,v", [(450, 34), (3000, 3), (2500, 293), (1025, 9), (700, 505), (90, 520), (61, 2044), (21, 2049), (40, 4096)])
+def test_grad_rows_end_to_end(n, v, dtype):
+    """Workgroups that hold parts of rows, and both sides of the lines between the forms."""
+    print(f"logprobs_grad n={n} v={v} {dtype}", flush=True)
+    x, token = draw(n, v, dtype, n * v, masked=0.2 if v > 4 else 0.0, pad=3)
+    r = torch.Generator().manual_seed(v)
+    run_grad(x, token, torch.randn(n, generator=r), torch.randn(n, generator=r))
+
+
+def test_grad_more_vectors_than_threads():
+    n, v = 2_200_003, 7
+    x, token = draw(n, v, torch.float32, 4)
+    r = torch.Generator().manual_seed(9)
+    run_grad(x, token, torch.randn(n, generator=r), torch.randn(n, generator=r))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("v", [40, 3000, 20000])
+def test_grad_of_masked_logits_with_large_coefficients(v, dtype):
+    x, token = draw(12, v, dtype, v, masked=0.5)
+    token.fill_(-1)
+    ge = torch.full((12,), 1e30)
+    run_grad(x, token, None, ge)
+    dev = x.cuda()
+    fw = M.logprobs(dev)
+    got = M.logprobs_grad(dev, None, fw.stats, fw.entropy, None, ge.cuda())
+    assert (got.cpu()[x == -INF] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,v", [(5, 2047), (5, 2049), (2049, 4100), (2047, 4100), (2050, 20001), (3, 20481)])
+def test_rows_by_a_wavefront_or_more(n, v, dtype):
+    """Both sides of the lines between 64 and more threads for a row."""
+    print(f"logprobs n={n} v={v} {dtype}", flush=True)
+    check(*draw(n, v, dtype, n + 3 * v, masked=0.1), 6)
