@@ -4,8 +4,8 @@ them back into the predictor).
 A step takes the batch's features through the layers (activations kept), reads the log probability of
 every stage's observed length bin, takes the gradient of their mean back through the layers, clips it
 by its global norm and moves float32 master weights by it (momentum), from which the predictor's own
-weights are rounded. All but the update runs in the library's kernels; nothing in a step synchronises
-or, with the buffers a ``Fit`` holds, allocates. The weights are the ones ``predict`` takes.
+weights are rounded. All but the update runs in the library's kernels, in the buffers a ``Fit`` holds;
+nothing in a step synchronises. The weights are the ones ``predict`` takes.
 
     python -m paper_2606_12950_amd.fit --workload c1 --stages 65536 --steps 50
 """
@@ -65,10 +65,13 @@ class Fit:
             h = layer(h, w, b, relu=l + 1 < len(self.weights), out=self.hidden[l])
         return logprobs(h, bins, out=self.out, workspace=self.workspace)
 
+    def _given(self, bins: torch.Tensor) -> torch.Tensor:
+        return (bins >= 0) & (bins < self.hidden[-1].shape[1])
+
     def gradients(self, x: torch.Tensor, bins: torch.Tensor) -> Tuple[List[torch.Tensor], List[torch.Tensor]]:
         """Gradients of minus the mean log probability of the observed bins (less the entropy bonus), of
         weights and biases, after ``score``."""
-        given = ((bins >= 0) & (bins < self.hidden[-1].shape[1])).float()
+        given = self._given(bins).float()
         g = given / -given.sum().clamp_min(1.0)
         ge = None if self.g_entropy is None else -self.g_entropy
         logprobs_grad(self.hidden[-1], bins, self.out.stats, self.out.entropy, g, ge, out=self.g_z[-1])
@@ -84,7 +87,7 @@ class Fit:
         """One update. Returns the mean log probability before it and the gradient's norm before clipping, on
         the device."""
         out = self.score(x, bins)
-        mean = out.logprob.sum() / (bins >= 0).sum().clamp_min(1)
+        mean = out.logprob.sum() / self._given(bins).sum().clamp_min(1)
         self.gradients(x, bins)
         grads = [*self.g_weights, *self.g_biases]
         clip_gradients(grads, max_norm, norm=self.norm, workspace=self.workspace)

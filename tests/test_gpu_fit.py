@@ -148,3 +148,12 @@ def test_nothing_observed_moves_nothing():
     assert mean.item() == 0.0 and norm.item() == 0.0
     for a, b in zip((*ws, *bs), before):
         assert torch.equal(a, b)
+
+
+def test_bins_outside_the_table_count_as_none():
+    ws, bs = network((32, 16), torch.float32, 3)
+    x = torch.randn(6, 32, device="cuda")
+    inside = torch.tensor([0, 3, -1, -1, 15, -1], dtype=torch.int32, device="cuda")
+    outside = torch.tensor([0, 3, 16, -7, 15, 1 << 30], dtype=torch.int32, device="cuda")
+    means = [F.Fit([w.clone() for w in ws], [b.clone() for b in bs], 6).step(x, t, 0.1)[0] for t in (inside, outside)]
+    assert torch.equal(*means)
