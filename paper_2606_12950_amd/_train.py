@@ -26,8 +26,6 @@ MAX_ALTERNATIVES = 16
 
 TENSORS_PATH = os.path.join(os.path.dirname(_native.LIBRARY_PATH), "_tensors.so")
 
-# Outputs are allocated with their sizes as separate arguments: torch reads those in 1.2 us, a tuple of them in 2.0.
-
 _MOST = (1 << 31) - 1      # of an int32 argument: ctypes would cut a larger number off
 
 _DTYPE = {torch.float32: MAESTRO_F32, torch.bfloat16: MAESTRO_BF16}
@@ -115,9 +113,9 @@ def logprobs(logits: torch.Tensor, token: Optional[torch.Tensor] = None, k: int 
     if token is not None:
         _shape(_dev(token, "token", torch.int32), "token", (n,))
     if out is None:
-        row = ((n,), False)
+        row = ((n,), 0)
         out = Logprobs._make(_tensors.empties(logits, row if token is not None else None, row if want_entropy else None,
-                                              ((n, k), True), ((n, k), False), ((n, 2), False) if want_stats else None))
+                                              ((n, k), 1), ((n, k), 0), ((n, 2), 0) if want_stats else None))
     else:
         if (out.logprob is None) != (token is None):
             raise ValueError("logprob goes with token")
@@ -159,7 +157,7 @@ def logprobs_grad(logits: torch.Tensor, token: Optional[torch.Tensor], stats: to
         if t is not None:
             _shape(_dev(t, name, torch.float32), name, (n,))
     if out is None:
-        out, out_stride = torch.empty(n, v, dtype=logits.dtype, device=logits.device), v
+        (out,), out_stride = _tensors.empties(logits, ((n, v), 2)), v
     else:
         *same, out_stride = _rows(out, "out")
         if same != [dt, n, v]:
@@ -192,7 +190,7 @@ def layer(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor, relu: bool 
     dt, n, i, o = _layer_shapes(x, weight)
     _shape(_dev(bias, "bias", torch.float32), "bias", (o,))
     if out is None:
-        out = torch.empty(n, o, dtype=weight.dtype, device=x.device)
+        out, = _tensors.empties(x, ((n, o), 2))
     else:
         _shape(_dev(out, "out", weight.dtype), "out", (n, o))
     st = lib.maestro_layer(n, i, o, dt, _ptr(x), _ptr(weight), _ptr(bias), int(bool(relu)), _ptr(out), _stream(stream))
@@ -211,9 +209,7 @@ def layer_grad(x: torch.Tensor, weight: torch.Tensor, g_z: torch.Tensor, relu_in
     _shape(_dev(g_z, "g_z", weight.dtype), "g_z", (n, o))
     dev = x.device
     if out is None:
-        out = LayerGrad(torch.empty(n, i, dtype=weight.dtype, device=dev) if want_x else None,
-                        torch.empty(o, i, dtype=torch.float32, device=dev),
-                        torch.empty(o, dtype=torch.float32, device=dev))
+        out = LayerGrad._make(_tensors.empties(x, ((n, i), 2) if want_x else None, ((o, i), 0), ((o,), 0)))
     else:
         if (out.x is not None) != want_x:
             raise ValueError("out.x goes with want_x")
@@ -253,7 +249,7 @@ def clip_gradients(tensors: Sequence[torch.Tensor], max_norm: float, out: Option
             raise ValueError("out must have one output per tensor, of its size and type")
     dev = tensors[0].device
     if norm is None:
-        norm = torch.empty(1, dtype=torch.float32, device=dev)
+        norm, = _tensors.empties(tensors[0], ((1,), 0))
     else:
         _shape(_dev(norm, "norm", torch.float32), "norm", (1,))
     _workspace(workspace)

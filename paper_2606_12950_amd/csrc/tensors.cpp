@@ -45,31 +45,33 @@ PyObject* table(PyObject*, PyObject* args) {
   END_HANDLE_TH_ERRORS
 }
 
-// empties(like: tensor, *(shape: tuple, int32: bool) or None) -> tuple of uninitialised float32 (or int32) tensors on
-// like's device, None where None was given
+// empties(like: tensor, *(shape: tuple, type: int) or None) -> tuple of uninitialised tensors on like's device, None where
+// None was given; type 0: float32, 1: int32, 2: like's
 PyObject* empties(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (n < 1 || !THPVariable_Check(args[0])) return PyErr_Format(PyExc_TypeError, "a tensor is needed");
   HANDLE_TH_ERRORS
   THPObjectPtr out(PyTuple_New(n - 1));
   if (!out) return nullptr;
-  const at::TensorOptions like = at::TensorOptions().device(THPVariable_Unpack(args[0]).device());
+  const at::Tensor& like = THPVariable_Unpack(args[0]);
+  const at::TensorOptions on = at::TensorOptions().device(like.device());
   for (Py_ssize_t i = 1; i < n; ++i) {
     if (args[i] == Py_None) {
       Py_INCREF(Py_None);
       PyTuple_SET_ITEM(out.get(), i - 1, Py_None);
       continue;
     }
-    PyObject* shape;
-    int whole;
-    if (!PyTuple_Check(args[i])) return PyErr_Format(PyExc_TypeError, "(shape, int32) is needed");
-    if (!PyArg_ParseTuple(args[i], "O!p", &PyTuple_Type, &shape, &whole)) return nullptr;
+    if (!PyTuple_Check(args[i]) || PyTuple_GET_SIZE(args[i]) != 2 || !PyTuple_Check(PyTuple_GET_ITEM(args[i], 0)))
+      return PyErr_Format(PyExc_TypeError, "(shape, type) is needed");
+    PyObject* shape = PyTuple_GET_ITEM(args[i], 0);
+    const long type = PyLong_AsLong(PyTuple_GET_ITEM(args[i], 1));
     const Py_ssize_t dims = PyTuple_GET_SIZE(shape);
     if (dims > 2) return PyErr_Format(PyExc_ValueError, "at most two dimensions");
     int64_t size[2];
     for (Py_ssize_t d = 0; d < dims; ++d) size[d] = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, d));
     if (PyErr_Occurred()) return nullptr;
-    PyObject* t = THPVariable_Wrap(
-        at::empty(c10::IntArrayRef(size, static_cast<size_t>(dims)), like.dtype(whole ? at::kInt : at::kFloat)));
+    if (type < 0 || type > 2) return PyErr_Format(PyExc_ValueError, "type must be 0, 1 or 2");
+    const at::ScalarType dtype = type == 0 ? at::kFloat : type == 1 ? at::kInt : like.scalar_type();
+    PyObject* t = THPVariable_Wrap(at::empty(c10::IntArrayRef(size, static_cast<size_t>(dims)), on.dtype(dtype)));
     if (!t) return nullptr;
     PyTuple_SET_ITEM(out.get(), i - 1, t);
   }

@@ -57,3 +57,13 @@ def test_missing_module_is_named(tmp_path, monkeypatch):
     monkeypatch.setattr(_train, "_lib", None)
     with pytest.raises(RuntimeError, match="missing.so"):
         _train.load()
+
+
+def test_empties_types(tensors):
+    like = torch.zeros(1, dtype=torch.bfloat16)
+    assert [t.dtype for t in tensors.empties(like, ((1,), 0), ((1,), 1), ((1,), 2))] == [torch.float32, torch.int32, torch.bfloat16]
+    for bad in (((1,), 3), ((1,), -1)):
+        with pytest.raises(ValueError):
+            tensors.empties(like, bad)
+    with pytest.raises(TypeError):
+        tensors.empties(like, ((1,),))
