@@ -41,14 +41,16 @@ __device__ __forceinline__ void unpack(const u32x4& w, float (&x)[8]) {
 }
 
 // the vector at x[j] as it lies in memory, what lies past v filled with -inf
-__device__ __forceinline__ u32x4 load_raw(const float* x, int32_t j, int32_t v) {
+template <class I>
+__device__ __forceinline__ u32x4 load_raw(const float* x, I j, I v) {
   if (j + 4 <= v) return load16(x + j);
   u32x4 w;
 #pragma unroll
   for (int i = 0; i < 4; ++i) w[i] = j + i < v ? __float_as_uint(x[j + i]) : 0xFF800000u;
   return w;
 }
-__device__ __forceinline__ u32x4 load_raw(const __bf16* x, int32_t j, int32_t v) {
+template <class I>
+__device__ __forceinline__ u32x4 load_raw(const __bf16* x, I j, I v) {
   if (j + 8 <= v) return load16(x + j);
   u32x4 w;
 #pragma unroll
@@ -375,27 +377,39 @@ __global__ __launch_bounds__(kThreads) void long_kernel(int64_t n, int32_t v, co
 
     Part p{-INFINITY, 0.0f, 0.0f};
     float b = 0.0f;
-    for (int64_t at = 0; at < vecs; at += kAhead * kThreads) {
-      float z[kAhead][V];
-      if ((at + kAhead * kThreads) * V <= len) {
-        u32x4 w[kAhead];
+    // some values of this thread
+    auto take = [&](const auto& z) {
+      constexpr int N = sizeof(z) / sizeof(float);
+      float m = z[0];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) w[u] = load16(x + (at + u * kThreads + tid) * V);
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) unpack(w[u], z[u]);
-      } else {
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) load_vec(x, (at + u * kThreads + tid) * V, len, z[u]);
-      }
-      float m = z[0][0];
-#pragma unroll
-      for (int i = 1; i < kAhead * V; ++i) m = maximum(m, z[i / V][i % V]);
+      for (int i = 1; i < N; ++i) m = maximum(m, z[i]);
       if (!(m <= p.m)) {
         rebase(p, maximum(p.m, m));
         b = base_of(p.m);
       }
 #pragma unroll
-      for (int i = 0; i < kAhead * V; ++i) add(p, z[i / V][i % V], b);
+      for (int i = 0; i < N; ++i) add(p, z[i], b);
+    };
+    for (int64_t at = 0; at < vecs; at += kAhead * kThreads) {
+      u32x4 w[kAhead];                                      // unpacked when all are on their way
+      if ((at + kAhead * kThreads) * V <= len) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) w[u] = load16(x + (at + u * kThreads + tid) * V);
+        float z[kAhead * V];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) unpack(w[u], *reinterpret_cast<float(*)[V]>(&z[u * V]));
+        take(z);
+      } else {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) w[u] = load_raw<int64_t>(x, (at + u * kThreads + tid) * V, len);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+          if (at + u * kThreads < vecs) {                   // nothing is computed for vectors that no thread has
+            float z[V];
+            unpack(w[u], z);
+            take(z);
+          }
+      }
     }
     const float own = p.m;
     p = group_join<64>(p);
