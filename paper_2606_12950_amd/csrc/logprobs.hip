@@ -355,8 +355,7 @@ struct Segments {
 // are few and long, else 256. Measured (us): 16,384 x 4,096 bfloat16 36 with 64 threads and 110 with 256, 4,096 x 20,000 39 and
 // 48, 2,500 x 8,000 16.4 and 18.6, but 4,082 x 16,000 float32 60 and 51, 1,000 x 4,000 9.3 and 8.1, 2,048 x 131,072
 // bfloat16 171 and 111; 4,082 x 2,000 float32 11.0 and 22.7, 3 of them 6.2 and 6.0; one row of 32,000 with eight alternatives 8.6 with 256 and 7.8 with 512, one of 5,000
-// 6.6 and 7.5. Against short_kernel's widest form 64 threads take 88 to 106 at 65,536 x 2,048 bfloat16, 190 to 98 at
-// 131,072 x 1,000.
+// 6.6 and 7.5.
 template <typename T, int kThreads>
 __global__ __launch_bounds__(kThreads) void long_kernel(int64_t n, int32_t v, const T* logits, int64_t stride,
                                                         const int32_t* token, int32_t k, Outputs o, Segments seg) {
@@ -754,6 +753,12 @@ int64_t segments_of(int64_t n, int64_t bytes) {
   return least(least(64, cdiv(2 * kCus, n)), bytes / 16384);
 }
 
+// Alternatives up to which a row of 129 to 256 vectors stays in a wavefront's registers: each costs a pass over them there,
+// of 64-bit keys for float32. Measured (us, short / long with 0, 2, 5 alternatives): 41,004 x 700 float32 25 / 31,
+// 43 / 49, 65 / 58; 60,000 x 2,048 bfloat16 43 / 50, 67 / 75, 90 / 90; 20,000 x 1,100 22 / 22, 31 / 32, 38 / 36.
+template <typename T>
+constexpr int32_t kWideShort = sizeof(T) == 4 ? 2 : 4;
+
 template <typename T, int G, int R>
 void launch_short(int64_t n, int32_t v, const T* x, int64_t stride, const int32_t* token, int32_t k, const Outputs& o,
                   hipStream_t stream) {
@@ -771,6 +776,7 @@ maestro_status launch(int64_t n, int32_t v, const T* x, int64_t stride, const in
   else if (vecs <= 32) launch_short<T, 8, 4>(n, v, x, stride, token, k, o, stream);
   else if (vecs <= 64) launch_short<T, 16, 4>(n, v, x, stride, token, k, o, stream);
   else if (vecs <= 128) launch_short<T, 32, 4>(n, v, x, stride, token, k, o, stream);
+  else if (vecs <= 256 && k <= kWideShort<T>) launch_short<T, 64, 4>(n, v, x, stride, token, k, o, stream);
   else {
     Segments seg{nullptr, nullptr, nullptr, (int32_t)segments_of(n, (int64_t)v * sizeof(T)), v};
     if (seg.count > 1) {

@@ -414,3 +414,15 @@ def test_rows_by_a_wavefront_or_more(n, v, dtype):
     """Both sides of the lines between 64 and more threads for a row."""
     print(f"logprobs n={n} v={v} {dtype}", flush=True)
     check(*draw(n, v, dtype, n + 3 * v, masked=0.1), 6)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("k", [0, 1, 2, 3, 4, 5])
+@pytest.mark.parametrize("n,v", [(37, 513), (5, 700), (37, 1023), (9, 1025), (37, 1100), (9, 2047), (5, 2048)])
+def test_rows_in_a_wavefronts_registers(n, v, k, dtype):
+    print(f"logprobs n={n} v={v} k={k} {dtype}", flush=True)
+    check(*draw(n, v, dtype, n + v + k, masked=0.2, pad=1), k)
+    x, token = draw(n, v, dtype, n + v + k)
+    x.copy_(x.round())                                          # ties
+    x[0], x[1, :-1], x[2, v // 2], x[3, 1] = -INF, -INF, INF, math.nan
+    check(x, token, k)
