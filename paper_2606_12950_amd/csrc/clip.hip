@@ -17,16 +17,18 @@ namespace maestro {
 namespace {
 
 constexpr int kTensors = 96;         // 96 * 32 bytes of table: within the 4 KB of kernel arguments
+constexpr int kFew = 12;             // a smaller table, which is sooner copied to the arguments: six tensors 9.3 us a call (9.8)
 constexpr int kThreads = 256;
 constexpr int kAhead = 8;            // 16-byte vectors of a thread in flight
 constexpr int64_t kChunk = 16 * kThreads * kAhead;        // bytes of one unit of work
 constexpr int kBlocks = 2048;        // the most workgroups, and so partial sums, of a launch
 
+template <int N>
 struct Table {
-  const void* in[kTensors];
-  void* out[kTensors];
-  int64_t size[kTensors];
-  int64_t chunk[kTensors];           // first chunk of each tensor, over all of the launch's
+  const void* in[N];
+  void* out[N];
+  int64_t size[N];
+  int64_t chunk[N];                  // first chunk of each tensor, over all of the launch's
   uint64_t bf16[2];
   int64_t chunks;
   int32_t count;
@@ -47,7 +49,8 @@ __device__ __forceinline__ void store16(float* p, const u32x4& w) { *reinterpret
 __device__ __forceinline__ void store16(__bf16* p, const u32x4& w) { *reinterpret_cast<u32x4_at2*>(p) = w; }
 
 // the tensor that chunk c lies in: the last one whose first chunk is not past it
-__device__ __forceinline__ int tensor_of(const Table& t, int64_t c) {
+template <int N>
+__device__ __forceinline__ int tensor_of(const Table<N>& t, int64_t c) {
   int lo = 0, hi = t.count;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
@@ -142,7 +145,8 @@ __device__ __forceinline__ void scale(const T* x, T* y, int64_t lo, int64_t hi, 
   }
 }
 
-__global__ __launch_bounds__(kThreads) void square_kernel(Table t, double* partial) {
+template <int N>
+__global__ __launch_bounds__(kThreads) void square_kernel(Table<N> t, double* partial) {
   double s = 0.0;
   for (int64_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
     const int i = tensor_of(t, c);
@@ -169,7 +173,8 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(const double* partial, i
 }
 
 // norm: written by the first launch's first workgroup, NULL in the others
-__global__ __launch_bounds__(kThreads) void scale_kernel(Table t, const double* partial, int64_t n, double max_norm,
+template <int N>
+__global__ __launch_bounds__(kThreads) void scale_kernel(Table<N> t, const double* partial, int64_t n, double max_norm,
                                                          bool in_place, float* norm) {
   const double all = sqrt(total(partial, n));
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) norm[0] = (float)all;
@@ -194,8 +199,9 @@ struct Call {
   const int32_t* dtypes;
 };
 
-// The table of the tensors [from, to): at most kTensors that are not empty.
-void fill(Table& t, const Call& c, int32_t from, int32_t to) {
+// The table of the tensors [from, to): at most N that are not empty.
+template <int N>
+void fill(Table<N>& t, const Call& c, int32_t from, int32_t to) {
   t.count = 0;
   t.chunks = 0;
   t.bf16[0] = t.bf16[1] = 0;
@@ -215,10 +221,35 @@ void fill(Table& t, const Call& c, int32_t from, int32_t to) {
 int32_t launches_of(int32_t n) { return (int32_t)(((int64_t)n + kTensors - 1) / kTensors); }
 
 // Workgroups of a launch: fewer where there are many launches, so that the partial sums stay soon added up.
-unsigned grid_of(const Table& t, int32_t launches) {
+template <int N>
+unsigned grid_of(const Table<N>& t, int32_t launches) {
   int64_t most = 2 * kBlocks / launches;
   most = most < 64 ? 64 : most > kBlocks ? kBlocks : most;
   return (unsigned)(t.chunks < most ? t.chunks : most);
+}
+
+template <int N>
+maestro_status launch(const Call& c, int32_t launches, float max_norm, float* norm, double* partial, hipStream_t stream) {
+  int64_t sums = 0;
+  Table<N> t;
+  for (int32_t l = 0; l < launches; ++l) {
+    fill(t, c, l * N, l == launches - 1 ? c.n : (l + 1) * N);
+    if (t.count == 0) continue;
+    const unsigned grid = grid_of(t, launches);
+    square_kernel<<<grid, kThreads, 0, stream>>>(t, partial + sums);
+    sums += grid;
+  }
+  if (max_norm == INFINITY || sums == 0) {
+    norm_kernel<<<1, kThreads, 0, stream>>>(partial, sums, norm);
+    return launch_status();
+  }
+  for (int32_t l = launches - 1; l >= 0; --l) {             // backwards: see the top
+    if (launches > 1) fill(t, c, l * N, l == launches - 1 ? c.n : (l + 1) * N);
+    if (t.count == 0) continue;
+    scale_kernel<<<grid_of(t, 1), kThreads, 0, stream>>>(t, partial, sums, max_norm, !c.out, norm);
+    norm = nullptr;
+  }
+  return launch_status();
 }
 
 }  // namespace
@@ -230,28 +261,9 @@ size_t clip_workspace_bytes(int32_t n_tensors) {
 maestro_status launch_clip(int32_t n_tensors, void* const* tensors, void* const* out, const int64_t* sizes,
                            const int32_t* dtypes, float max_norm, float* norm, void* workspace, hipStream_t stream) {
   const Call c{n_tensors, tensors, out, sizes, dtypes};
-  const int32_t launches = launches_of(n_tensors);
   double* partial = static_cast<double*>(workspace);
-  int64_t sums = 0;
-  Table t;
-  for (int32_t l = 0; l < launches; ++l) {
-    fill(t, c, l * kTensors, l == launches - 1 ? n_tensors : (l + 1) * kTensors);
-    if (t.count == 0) continue;
-    const unsigned grid = grid_of(t, launches);
-    square_kernel<<<grid, kThreads, 0, stream>>>(t, partial + sums);
-    sums += grid;
-  }
-  if (max_norm == INFINITY || sums == 0) {
-    norm_kernel<<<1, kThreads, 0, stream>>>(partial, sums, norm);
-    return launch_status();
-  }
-  for (int32_t l = launches - 1; l >= 0; --l) {             // backwards: see the top
-    if (launches > 1) fill(t, c, l * kTensors, l == launches - 1 ? n_tensors : (l + 1) * kTensors);
-    if (t.count == 0) continue;
-    scale_kernel<<<grid_of(t, 1), kThreads, 0, stream>>>(t, partial, sums, max_norm, !out, norm);
-    norm = nullptr;
-  }
-  return launch_status();
+  if (n_tensors <= kFew) return launch<kFew>(c, n_tensors > 0, max_norm, norm, partial, stream);
+  return launch<kTensors>(c, launches_of(n_tensors), max_norm, norm, partial, stream);
 }
 
 }  // namespace maestro
