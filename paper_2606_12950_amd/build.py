@@ -66,7 +66,7 @@ def _compile_tensors(outdir: str, verbose: bool) -> str:
     from torch.utils import cpp_extension
 
     out = os.path.join(outdir, os.path.basename(TENSORS_LIB))
-    include = [*cpp_extension.include_paths(), sysconfig.get_paths()["include"]]
+    include = [*cpp_extension.include_paths(), sysconfig.get_paths()["include"], INCLUDE]
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *(f"-I{p}" for p in include),
            os.path.join(CSRC, TENSORS_SOURCE), "-o", out, *(f"-L{p}" for p in cpp_extension.library_paths()),

@@ -67,3 +67,50 @@ def test_empties_types(tensors):
             tensors.empties(like, bad)
     with pytest.raises(TypeError):
         tensors.empties(like, ((1,),))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_whole_calls_and_the_binding_agree(tensors, dtype):
+    """What the native module takes whole gives the bits that the binding's own path (outputs given) gives."""
+    import paper_2606_12950_amd as M
+    r = torch.Generator().manual_seed(3)
+    d = lambda *s: torch.randn(*s, generator=r).cuda()
+    x, w, b, gz = d(37, 64).to(dtype), d(48, 64).to(dtype), d(48), d(37, 48).to(dtype)
+    assert torch.equal(M.layer(x, w, b), M.layer(x, w, b, out=torch.empty_like(gz)))
+    one = M.layer_grad(x, w, gz, relu_input=True)
+    two = M.layer_grad(x, w, gz, relu_input=True, out=M.LayerGrad(torch.empty_like(x), torch.empty(48, 64, device="cuda"), torch.empty(48, device="cuda")))
+    assert type(one) is M.LayerGrad and all(map(torch.equal, one, two))
+    assert M.layer_grad(x, w, gz, want_x=False).x is None
+    t = torch.arange(37, dtype=torch.int32, device="cuda")
+    for k, token in ((0, None), (3, t), (16, t)):
+        one = M.logprobs(gz, token, k=k)
+        two = M.logprobs(gz, token, k=k, out=M.Logprobs(*(None if u is None else torch.full_like(u, 7) for u in one)))
+        assert type(one) is M.Logprobs and (one.logprob is None) == (token is None)
+        assert all(u is v is None or torch.equal(u, v) for u, v in zip(one, two))
+    g = d(37)
+    for token, gl, ge in ((t, g, g), (t, g, None), (None, None, g)):
+        one = M.logprobs_grad(gz, token, two.stats, two.entropy, gl, ge)
+        assert torch.equal(one, M.logprobs_grad(gz, token, two.stats, two.entropy, gl, ge, out=torch.empty_like(gz)))
+    grads = [x, w, b]
+    one, two = [torch.empty_like(u) for u in grads], [torch.empty_like(u) for u in grads]
+    norms = M.clip_gradients(grads, 0.5, out=one), M.clip_gradients(grads, 0.5, out=two, norm=torch.empty(1, device="cuda"))
+    assert torch.equal(*norms) and all(map(torch.equal, one, two))
+
+
+@pytest.mark.gpu
+def test_calls_that_are_not_plain_are_left_to_the_binding(tensors):
+    x, w, b = torch.zeros(8, 32, device="cuda"), torch.zeros(16, 32, device="cuda"), torch.zeros(16, device="cuda")
+    t = torch.zeros(8, dtype=torch.int32, device="cuda")
+    for bad in ((x.cpu(), w, b), (x, w.bfloat16(), b), (x[:, ::2], w[:, ::2], b), (x, w, b[:8]), (x, w, b.double()), (x, w, None),
+                (x[:, :24], w[:, :24].contiguous(), b), (3, w, b), (x, w.to_sparse(), b)):
+        assert tensors.layer(*bad, True, 0) is None
+    for bad in ((x, w, x), (x, w[:8], w), (x, None, x)):
+        assert tensors.layer_grad(*bad, True, True, 0) is None
+    for bad in ((x.t(), None, 0), (x, t[:7], 0), (x, t.long(), 0), (x, t, 17), (x, t, -1), (x, t, "2"), (x[0], None, 0), (x.half(), t, 0)):
+        assert tensors.logprobs(*bad, True, True, 0) is None
+    s, e = torch.zeros(8, 2, device="cuda"), torch.zeros(8, device="cuda")
+    for bad in ((x, t, s, e, None, e), (x, None, s, e, None, None), (x, None, s, None, None, e), (x, t, s[:4], e, e, e), (x, t, None, e, e, e)):
+        assert tensors.logprobs_grad(*bad, 0) is None
+    for bad in (([], 1.0, None), ([x.cpu()], 1.0, None), ([x], 1, None), ([x], 1.0, []), ([x], 1.0, [x[:4]]), ([x], -1.0, None), ((x,), 1.0, None)):
+        assert tensors.clip(*bad, 0) is None
