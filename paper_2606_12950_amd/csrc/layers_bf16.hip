@@ -13,8 +13,8 @@
 // tile's last products and its stores, and its stores under the next tile's products.
 //
 // Bound by the matrix cores on wide layers, by HBM on narrow ones. Measured: 262,139 x 1024 -> 1024
-// (0.55 TFLOP a product) activations 522 us = 1.05 PFLOP/s, input's gradient 564, weights' 505; a
-// 16,384-cubed library product reaches 1.55 on the same card, and the library's products of these shapes 555, 618
+// (0.55 TFLOP a product) activations 522 to 540 us = 1.02 to 1.05 PFLOP/s, input's gradient 564, weights' 505; a
+// 16,384-cubed library product reaches 1.31 to 1.35 on the same card, and the library's products of these shapes 555, 618
 // and 1,230 us. 512 -> 256: activations 95 us for 403 MB, input's gradient 132 us for 671 MB = 5.1 TB/s, what a copy reaches.
 #include <type_traits>
 

@@ -354,8 +354,8 @@ struct Segments {
 // A wavefront to a row (no barriers, 64 threads) where rows are short (8 KB, any number of them) or many, 512 threads where they
 // are few and long, else 256. Measured (us): 16,384 x 4,096 bfloat16 36 with 64 threads and 110 with 256, 4,096 x 20,000 39 and
 // 48, 2,500 x 8,000 16.4 and 18.6, but 4,082 x 16,000 float32 60 and 51, 1,000 x 4,000 9.3 and 8.1, 2,048 x 131,072
-// bfloat16 171 and 111; 4,082 x 2,000 float32 11.0 and 22.7, 3 of them 6.2 and 6.0; one row of 32,000 with eight alternatives 8.6 with 256 and 7.8 with 512, one of 5,000
-// 6.6 and 7.5.
+// bfloat16 171 and 111; 4,082 x 2,000 float32 11.0 and 22.7, 3 of them 6.2 and 6.0; one row of 32,000 with eight
+// alternatives 8.6 with 256 and 7.8 with 512 (9.5 with 1,024), one of 5,000 6.6 and 7.5.
 template <typename T, int kThreads>
 __global__ __launch_bounds__(kThreads) void long_kernel(int64_t n, int32_t v, const T* logits, int64_t stride,
                                                         const int32_t* token, int32_t k, Outputs o, Segments seg) {
