@@ -85,7 +85,7 @@ MAESTRO_API maestro_status maestro_layer_grad(int64_t n, int32_t d_in, int32_t d
  * of the sum of squares, accumulated in float64; where it exceeds max_norm, every tensor is scaled by
  * max_norm / norm. max_norm = INFINITY computes the norm alone (out must be NULL).
  *   tensors, sizes, dtypes  HOST arrays [n_tensors], read during the call: device pointers (aligned to an
- *                           element, NULL allowed for size 0), element counts, maestro_dtype
+ *                           element, NULL allowed for size 0), element counts (up to 2^39 bytes), maestro_dtype
  *   out                     HOST array [n_tensors] of device pointers the result is written to, scaled
  *                           or not, each of its tensor's type and size; NULL: in place, where nothing is
  *                           written unless the norm exceeds max_norm. out[i] is tensors[i] itself or overlaps none

@@ -7,7 +7,7 @@
 // product rounded to float32 (and then to the tensor's type), so no factor is too small for a float32.
 //
 // Bound by HBM. The second pass goes through the tensors backwards: what the first read last is still in the memory-side
-// cache. 320 bfloat16 tensors of 403 million values (805 MB, read twice and written once) 519 us = 4.65 TB/s, their norm
+// cache. 320 bfloat16 tensors of 403 million values (805 MB, read twice and written once) 490 us = 4.9 TB/s, their norm
 // alone 175 us; two float32 tensors of 145 million 345 us = 5.1; small sets are bound by the two launches.
 #include <math.h>
 
@@ -16,7 +16,7 @@
 namespace maestro {
 namespace {
 
-constexpr int kTensors = 96;         // 96 * 32 bytes of table: within the 4 KB of kernel arguments
+constexpr int kTensors = 160;        // 160 * 22 bytes of table: within the 4 KB of kernel arguments. 400 small tensors 31 us a call (50 with 96 in a table)
 constexpr int kFew = 12;             // a smaller table, which is sooner copied to the arguments: six tensors 9.3 us a call (9.8)
 constexpr int kThreads = 256;
 constexpr int kAhead = 8;            // 16-byte vectors of a thread in flight
@@ -27,12 +27,12 @@ template <int N>
 struct Table {
   const void* in[N];
   void* out[N];
-  int64_t size[N];
-  int64_t chunk[N];                  // first chunk of each tensor, over all of the launch's
-  uint64_t bf16[2];
-  int64_t chunks;
+  uint32_t chunk[N];                 // first chunk of each tensor, over all of the launch's
+  uint16_t last[N];                  // values in its last chunk (at most 2^14), and 2^15 for bfloat16
+  uint32_t chunks;                   // < 2^32: a tensor has at most 2^24 (kClipMaxBytes)
   int32_t count;
 };
+static_assert(sizeof(Table<kTensors>) <= 3600, "kernel arguments");
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 __attribute__((aligned(2))) u32x4_at2;        // tensors start anywhere
@@ -50,7 +50,7 @@ __device__ __forceinline__ void store16(__bf16* p, const u32x4& w) { *reinterpre
 
 // the tensor that chunk c lies in: the last one whose first chunk is not past it
 template <int N>
-__device__ __forceinline__ int tensor_of(const Table<N>& t, int64_t c) {
+__device__ __forceinline__ int tensor_of(const Table<N>& t, uint32_t c) {
   int lo = 0, hi = t.count;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
@@ -58,6 +58,24 @@ __device__ __forceinline__ int tensor_of(const Table<N>& t, int64_t c) {
     else hi = mid;
   }
   return lo;
+}
+
+// chunk c: its tensor, type, and values [lo, hi)
+struct Chunk {
+  int i;
+  bool bf16;
+  int64_t lo, hi;
+};
+template <int N>
+__device__ __forceinline__ Chunk chunk_of(const Table<N>& t, uint32_t c) {
+  Chunk k;
+  k.i = tensor_of(t, c);
+  const uint32_t last = t.last[k.i], end = k.i + 1 < t.count ? t.chunk[k.i + 1] : t.chunks;
+  k.bf16 = last >> 15;
+  const int64_t most = kChunk / (k.bf16 ? 2 : 4);
+  k.lo = (c - t.chunk[k.i]) * most;
+  k.hi = k.lo + (c + 1 == end ? last & 0x7FFF : most);
+  return k;
 }
 
 __device__ __forceinline__ double block_sum(double s) {
@@ -149,12 +167,9 @@ template <int N>
 __global__ __launch_bounds__(kThreads) void square_kernel(Table<N> t, double* partial) {
   double s = 0.0;
   for (int64_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
-    const int i = tensor_of(t, c);
-    const bool bf16 = (t.bf16[i >> 6] >> (i & 63)) & 1;
-    const int64_t most = kChunk / (bf16 ? 2 : 4), lo = (c - t.chunk[i]) * most;
-    const int64_t hi = lo + most < t.size[i] ? lo + most : t.size[i];
-    if (bf16) s += square_sum(static_cast<const __bf16*>(t.in[i]), lo, hi);
-    else s += square_sum(static_cast<const float*>(t.in[i]), lo, hi);
+    const Chunk k = chunk_of(t, (uint32_t)c);
+    if (k.bf16) s += square_sum(static_cast<const __bf16*>(t.in[k.i]), k.lo, k.hi);
+    else s += square_sum(static_cast<const float*>(t.in[k.i]), k.lo, k.hi);
   }
   s = block_sum(s);
   if (threadIdx.x == 0) partial[blockIdx.x] = s;
@@ -181,13 +196,10 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(Table<N> t, const doubl
   const bool over = all > max_norm && all < INFINITY;
   if (!over && in_place) return;
   const double f = over ? max_norm / all : 1.0;
-  for (int64_t c = t.chunks - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
-    const int i = tensor_of(t, c);
-    const bool bf16 = (t.bf16[i >> 6] >> (i & 63)) & 1;
-    const int64_t most = kChunk / (bf16 ? 2 : 4), lo = (c - t.chunk[i]) * most;
-    const int64_t hi = lo + most < t.size[i] ? lo + most : t.size[i];
-    if (bf16) scale(static_cast<const __bf16*>(t.in[i]), static_cast<__bf16*>(t.out[i]), lo, hi, f);
-    else scale(static_cast<const float*>(t.in[i]), static_cast<float*>(t.out[i]), lo, hi, f);
+  for (int64_t c = (int64_t)t.chunks - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
+    const Chunk k = chunk_of(t, (uint32_t)c);
+    if (k.bf16) scale(static_cast<const __bf16*>(t.in[k.i]), static_cast<__bf16*>(t.out[k.i]), k.lo, k.hi, f);
+    else scale(static_cast<const float*>(t.in[k.i]), static_cast<float*>(t.out[k.i]), k.lo, k.hi, f);
   }
 }
 
@@ -204,17 +216,16 @@ template <int N>
 void fill(Table<N>& t, const Call& c, int32_t from, int32_t to) {
   t.count = 0;
   t.chunks = 0;
-  t.bf16[0] = t.bf16[1] = 0;
   for (int32_t j = from; j < to; ++j) {
     if (c.sizes[j] == 0) continue;
     const int i = t.count++;
     t.in[i] = c.tensors[j];
     t.out[i] = c.out ? c.out[j] : c.tensors[j];
-    t.size[i] = c.sizes[j];
     t.chunk[i] = t.chunks;
-    const int64_t most = kChunk / (c.dtypes[j] == MAESTRO_BF16 ? 2 : 4);
-    t.chunks += (c.sizes[j] + most - 1) / most;
-    if (c.dtypes[j] == MAESTRO_BF16) t.bf16[i >> 6] |= 1ull << (i & 63);
+    const bool bf16 = c.dtypes[j] == MAESTRO_BF16;
+    const int64_t most = kChunk / (bf16 ? 2 : 4), chunks = (c.sizes[j] + most - 1) / most;
+    t.last[i] = (uint16_t)(c.sizes[j] - (chunks - 1) * most + (bf16 ? 0x8000 : 0));
+    t.chunks += (uint32_t)chunks;
   }
 }
 

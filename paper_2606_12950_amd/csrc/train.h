@@ -34,6 +34,7 @@ maestro_status launch_layer_grad_bf16(int64_t n, int32_t d_in, int32_t d_out, co
 maestro_status launch_join(const float* gw_parts, int32_t n_gw, float* gw, int64_t size, const float* gb_parts,
                            int32_t n_gb, float* gb, int32_t d_out, hipStream_t stream);
 
+constexpr int64_t kClipMaxBytes = (int64_t)1 << 39;      // of a tensor to clip: 2^24 units of work
 size_t clip_workspace_bytes(int32_t n_tensors);
 maestro_status launch_clip(int32_t n_tensors, void* const* tensors, void* const* out, const int64_t* sizes,
                            const int32_t* dtypes, float max_norm, float* norm, void* workspace, hipStream_t stream);

@@ -120,7 +120,8 @@ maestro_status maestro_clip_gradients(int32_t n_tensors, void* const* tensors, v
   if (max_norm == INFINITY && out) return MAESTRO_ERR_INVALID_ARG;
   if (n_tensors > 0 && (!tensors || !sizes || !dtypes)) return MAESTRO_ERR_INVALID_ARG;
   for (int32_t i = 0; i < n_tensors; ++i) {
-    if (sizes[i] < 0 || sizes[i] > kMaxRows || !typed(dtypes[i])) return MAESTRO_ERR_INVALID_ARG;
+    if (!typed(dtypes[i]) || sizes[i] < 0 || sizes[i] > maestro::kClipMaxBytes / (int64_t)element(dtypes[i]))
+      return MAESTRO_ERR_INVALID_ARG;
     if (sizes[i] == 0) continue;
     if (!tensors[i] || !aligned(tensors[i], element(dtypes[i]))) return MAESTRO_ERR_INVALID_ARG;
     if (out && (!out[i] || !aligned(out[i], element(dtypes[i])))) return MAESTRO_ERR_INVALID_ARG;

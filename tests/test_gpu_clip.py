@@ -161,3 +161,20 @@ def test_refusals():
                      (lambda: M.clip_gradients([f], 1.0, out=[f.bfloat16()]), ValueError)):
         with pytest.raises(err):
             bad()
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("count", [12, 13, 159, 160, 161, 321])
+def test_tables_just_full(count, in_place):
+    """Counts around the tables' sizes; lengths around a unit of work (8,192 float32, 16,384 bfloat16)."""
+    lengths = [1, 8191, 8192, 8193, 16383, 16384, 16385, 0, 32769, 77]
+    ts = make([lengths[i % 10] for i in range(count)], count)
+    print(f"clip tables of {count}", flush=True)
+    total = math.sqrt(sum(float(t.double().square().sum()) for t in ts))
+    dev = [t.cuda() for t in ts]
+    out = None if in_place else [torch.empty_like(t) for t in dev]
+    norm = M.clip_gradients(dev, total / 3, out=out)
+    assert abs(float(norm) - total) <= 2.0 ** -22 * total
+    for t, o in zip(ts, dev if in_place else out):
+        want = t.double() / 3
+        assert ((o.cpu().double() - want).abs() <= (2.0 ** -8 if t.dtype == torch.bfloat16 else 2.0 ** -22) * want.abs() + 1e-38).all()

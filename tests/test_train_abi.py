@@ -127,3 +127,7 @@ def test_clip_refuses(lib, bad):
 def test_clip_workspace(lib):
     assert _clip(lib, ws_bytes=lib.maestro_clip_gradients_workspace(2) - 1) == WORKSPACE
     assert lib.maestro_clip_gradients(-1, None, None, None, None, 1.0, A, A, 1 << 20, None) == INVALID
+
+
+def test_clip_tensors_past_half_a_tebibyte(lib):
+    assert _clip(lib, sizes=((1 << 37) + 1, 0)) == INVALID and _clip(lib, dtypes=(BF16, BF16), sizes=((1 << 38) + 1, 0)) == INVALID
