@@ -180,10 +180,27 @@ def _scratch(n_bytes: int, device, stream) -> torch.Tensor:
     to later work of the same stream only, and it is not one that another stream's work still uses."""
     if stream is None:
         return torch.empty(n_bytes, dtype=torch.uint8, device=device)
-    if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
-    with torch.cuda.stream(stream):
+    with torch.cuda.stream(_torch_stream(stream, device)):
         return torch.empty(n_bytes, dtype=torch.uint8, device=device)
+
+
+def _torch_stream(stream, device):
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+
+
+def _outputs(allocate, device, stream):
+    """The tensors (some may be None) that ``allocate()`` makes for a call on ``stream`` to write: from that
+    stream's pool, as ``_scratch``, and lent to the current stream, on which the caller goes on with them. Dropped, a
+    block is given to that stream's later work only, and not before what the current one was given has run."""
+    if stream is None:
+        return allocate()
+    with torch.cuda.stream(_torch_stream(stream, device)):
+        out = allocate()
+    current = torch.cuda.current_stream(device)
+    for t in out:
+        if t is not None:
+            t.record_stream(current)
+    return out
 
 
 def _may_allocate(stream) -> bool:

@@ -15,7 +15,7 @@ from typing import NamedTuple, Optional, Sequence
 import torch
 
 from . import _native
-from ._native import MAESTRO_BF16, MAESTRO_F32, _check, _dev, _ptr, _scratch, _shape, _stream, _Tensor, _workspace
+from ._native import MAESTRO_BF16, MAESTRO_F32, _check, _dev, _outputs, _ptr, _scratch, _shape, _stream, _Tensor, _workspace
 
 # Every function declared in include/maestro_train.h.
 EXPORTS = ("maestro_logprobs_workspace", "maestro_logprobs", "maestro_logprobs_grad", "maestro_layer",
@@ -107,6 +107,11 @@ def _rows(t: torch.Tensor, name: str):
     return code, n, v, stride
 
 
+def _empties(stream, like: torch.Tensor, *specs):
+    """The native module's ``empties`` for a call on ``stream``."""
+    return _outputs(lambda: _tensors.empties(like, *specs), like.device, stream)
+
+
 def logprobs(logits: torch.Tensor, token: Optional[torch.Tensor] = None, k: int = 0, want_entropy: bool = True,
              want_stats: bool = True, out: Optional[Logprobs] = None, workspace: Optional[torch.Tensor] = None,
              stream=None) -> Logprobs:
@@ -126,8 +131,8 @@ def logprobs(logits: torch.Tensor, token: Optional[torch.Tensor] = None, k: int 
         _shape(_dev(token, "token", torch.int32), "token", (n,))
     if out is None:
         row = ((n,), 0)
-        out = Logprobs._make(_tensors.empties(logits, row if token is not None else None, row if want_entropy else None,
-                                              ((n, k), 1), ((n, k), 0), ((n, 2), 0) if want_stats else None))
+        out = Logprobs._make(_empties(stream, logits, row if token is not None else None, row if want_entropy else None,
+                                      ((n, k), 1), ((n, k), 0), ((n, 2), 0) if want_stats else None))
     else:
         if (out.logprob is None) != (token is None):
             raise ValueError("logprob goes with token")
@@ -173,7 +178,7 @@ def logprobs_grad(logits: torch.Tensor, token: Optional[torch.Tensor], stats: to
         if t is not None:
             _shape(_dev(t, name, torch.float32), name, (n,))
     if out is None:
-        (out,), out_stride = _tensors.empties(logits, ((n, v), 2)), v
+        (out,), out_stride = _empties(stream, logits, ((n, v), 2)), v
     else:
         *same, out_stride = _rows(out, "out")
         if same != [dt, n, v]:
@@ -210,7 +215,7 @@ def layer(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor, relu: bool 
     dt, n, i, o = _layer_shapes(x, weight)
     _shape(_dev(bias, "bias", torch.float32), "bias", (o,))
     if out is None:
-        out, = _tensors.empties(x, ((n, o), 2))
+        out, = _empties(stream, x, ((n, o), 2))
     else:
         _shape(_dev(out, "out", weight.dtype), "out", (n, o))
     st = lib.maestro_layer(n, i, o, dt, _ptr(x), _ptr(weight), _ptr(bias), int(bool(relu)), _ptr(out), _stream(stream))
@@ -233,7 +238,7 @@ def layer_grad(x: torch.Tensor, weight: torch.Tensor, g_z: torch.Tensor, relu_in
     _shape(_dev(g_z, "g_z", weight.dtype), "g_z", (n, o))
     dev = x.device
     if out is None:
-        out = LayerGrad._make(_tensors.empties(x, ((n, i), 2) if want_x else None, ((o, i), 0), ((o,), 0)))
+        out = LayerGrad._make(_empties(stream, x, ((n, i), 2) if want_x else None, ((o, i), 0), ((o,), 0)))
     else:
         if (out.x is not None) != want_x:
             raise ValueError("out.x goes with want_x")
@@ -278,7 +283,7 @@ def clip_gradients(tensors: Sequence[torch.Tensor], max_norm: float, out: Option
             raise ValueError("out must have one output per tensor, of its size and type")
     dev = tensors[0].device
     if norm is None:
-        norm, = _tensors.empties(tensors[0], ((1,), 0))
+        norm, = _empties(stream, tensors[0], ((1,), 0))
     else:
         _shape(_dev(norm, "norm", torch.float32), "norm", (1,))
     _workspace(workspace)
