@@ -271,8 +271,8 @@ def predict(x: torch.Tensor, weights: Sequence[torch.Tensor], biases: Sequence[t
     if kv_bytes_per_token.dim() != 1:
         raise ValueError("kv_bytes_per_token must be [n_models]")
     if out is None:
-        out = (torch.empty(n, dtype=torch.float32, device=x.device),
-               torch.empty(n, dtype=torch.float64, device=x.device))
+        out = _outputs(lambda: (torch.empty(n, dtype=torch.float32, device=x.device),
+                                torch.empty(n, dtype=torch.float64, device=x.device)), x.device, stream)
     pred, kv = out
     _shape(_dev(pred, "pred_len", torch.float32), "pred_len", (n,))
     _shape(_dev(kv, "kv_bytes", torch.float64), "kv_bytes", (n,))
@@ -321,8 +321,9 @@ def predict_two_phase(x: torch.Tensor, weights: Sequence[torch.Tensor], biases: 
     tp.iso_y = iso_y.data_ptr()
     tp.max_len = float(max_len)
     if out is None:
-        out = (torch.empty(n, dtype=torch.float32, device=x.device), torch.empty(n, dtype=torch.float32, device=x.device),
-               torch.empty(n, dtype=torch.float64, device=x.device))
+        out = _outputs(lambda: (torch.empty(n, dtype=torch.float32, device=x.device),
+                                torch.empty(n, dtype=torch.float32, device=x.device),
+                                torch.empty(n, dtype=torch.float64, device=x.device)), x.device, stream)
     pt, pred, kv = out
     if pt is not None:
         _shape(_dev(pt, "p_tool", torch.float32), "p_tool", (n,))
@@ -433,8 +434,8 @@ def route(model_id: torch.Tensor, pred_len: torch.Tensor, kv_bytes: torch.Tensor
     if queue_s.shape != (M,):
         raise ValueError("per-node inputs must have the same length")
     if out is None:
-        out = (torch.empty((n, k), dtype=torch.int32, device=model_id.device),
-               torch.empty((n, k), dtype=torch.float32, device=model_id.device))
+        out = _outputs(lambda: (torch.empty((n, k), dtype=torch.int32, device=model_id.device),
+                                torch.empty((n, k), dtype=torch.float32, device=model_id.device)), model_id.device, stream)
     idx, sc = out
     _shape(_dev(idx, "node_idx", torch.int32), "node_idx", (n, k))
     _shape(_dev(sc, "score", torch.float32), "score", (n, k))
@@ -523,8 +524,8 @@ def route_fitness(model_id: torch.Tensor, src_id: torch.Tensor, class_id: torch.
     if class_weights.dim() != 2 or class_weights.shape[1] != 3 or bounds.numel() != 6:
         raise ValueError("class_weights must be [n_classes][3] and bounds hold 6 values")
     if out is None:
-        out = (torch.empty((n, k), dtype=torch.int32, device=model_id.device),
-               torch.empty((n, k), dtype=torch.float32, device=model_id.device))
+        out = _outputs(lambda: (torch.empty((n, k), dtype=torch.int32, device=model_id.device),
+                                torch.empty((n, k), dtype=torch.float32, device=model_id.device)), model_id.device, stream)
     idx, fit = out
     _shape(_dev(idx, "node_idx", torch.int32), "node_idx", (n, k))
     _shape(_dev(fit, "fitness", torch.float32), "fitness", (n, k))
@@ -575,8 +576,10 @@ def degradation_plans(engine_offset: torch.Tensor, engine_level: torch.Tensor, e
     if engine_freed_bytes.shape != (E,) or engine_cost_ms.shape != (E,):
         raise ValueError("per-engine inputs must have the same length")
     if out is None:
-        out = DegradationPlans(torch.empty((M, PLAN_BYTES), dtype=torch.uint8, device=engine_offset.device),
-                               torch.empty((max(E, 1), STEP_BYTES), dtype=torch.uint8, device=engine_offset.device))
+        dev = engine_offset.device
+        out = _outputs(lambda: DegradationPlans(torch.empty((M, PLAN_BYTES), dtype=torch.uint8, device=dev),
+                                                torch.empty((max(E, 1), STEP_BYTES), dtype=torch.uint8, device=dev)),
+                       dev, stream)
     _dev(out.records, "plans.records", torch.uint8)
     _dev(out.steps, "plans.steps", torch.uint8)
     if tuple(out.records.shape) != (M, PLAN_BYTES):
@@ -607,7 +610,7 @@ def activation_latency(tier: torch.Tensor, model_bytes: torch.Tensor, tier_bw: t
         raise ValueError("tier [n_nodes][n_models], model_bytes [n_models], tier_bw and tier_setup_ms [5]")
     M, K = tier.shape
     if out is None:
-        out = torch.empty((M, K), dtype=torch.float32, device=tier.device)
+        out, = _outputs(lambda: (torch.empty((M, K), dtype=torch.float32, device=tier.device),), tier.device, stream)
     _shape(_dev(out, "act_ms", torch.float32), "act_ms", (M, K))
     st = lib.maestro_activation_latency(M, K, _ptr(tier) if M else None, _ptr(model_bytes), _ptr(tier_bw),
                                         _ptr(tier_setup_ms), float(unit), _ptr(out) if M else None, _stream(stream))
@@ -637,8 +640,8 @@ def adaptive_rho(kv_actual: torch.Tensor, kv_pred: torch.Tensor, beta: float, q:
     if kv_actual.dim() != 1 or kv_pred.shape != (m,):
         raise ValueError("kv_actual and kv_pred must have the same length")
     if out is None:
-        out = (torch.empty(m, dtype=torch.float32, device=kv_actual.device),
-               torch.empty(1, dtype=torch.float32, device=kv_actual.device))
+        out = _outputs(lambda: (torch.empty(m, dtype=torch.float32, device=kv_actual.device),
+                                torch.empty(1, dtype=torch.float32, device=kv_actual.device)), kv_actual.device, stream)
     ew, rho = out
     _shape(_dev(ew, "ewma", torch.float32), "ewma", (m,))
     _shape(_dev(rho, "rho", torch.float32), "rho", (1,))
@@ -658,7 +661,7 @@ def quantiles(values: torch.Tensor, q_lo: float = 0.05, q_hi: float = 0.95,
     lib = load()
     _dev(values, "values", torch.float32)
     if out is None:
-        out = torch.empty(2, dtype=torch.float32, device=values.device)
+        out, = _outputs(lambda: (torch.empty(2, dtype=torch.float32, device=values.device),), values.device, stream)
     _shape(_dev(out, "out", torch.float32), "out", (2,))
     ws = _select_workspace(values.numel(), workspace, values.device, stream)
     st = lib.maestro_quantiles(_ptr(values), values.numel(), float(q_lo), float(q_hi), _ptr(out), _ptr(ws),
@@ -700,7 +703,8 @@ def route_sort_nodes(free_bytes: torch.Tensor, queue_s: torch.Tensor, cold_s: Op
             raise ValueError("per-node inputs must have the same length")
     need = route_lists_bytes(n_models, M)
     if lists is None:
-        lists = torch.empty(max(need, 16), dtype=torch.uint8, device=free_bytes.device)
+        lists, = _outputs(lambda: (torch.empty(max(need, 16), dtype=torch.uint8, device=free_bytes.device),),
+                          free_bytes.device, stream)
     _workspace(lists)
     st = lib.maestro_route_sort_nodes(n_models, M, _ptr(free_bytes), _ptr(queue_s),
                                       _ptr(cold_s) if act_s is None else None,
@@ -726,8 +730,8 @@ def route_walk(model_id: torch.Tensor, pred_len: torch.Tensor, kv_bytes: torch.T
         raise ValueError("per-stage inputs must be one-dimensional and of the same length")
     _workspace(lists)
     if out is None:
-        out = (torch.empty((n, k), dtype=torch.int32, device=model_id.device),
-               torch.empty((n, k), dtype=torch.float32, device=model_id.device))
+        out = _outputs(lambda: (torch.empty((n, k), dtype=torch.int32, device=model_id.device),
+                                torch.empty((n, k), dtype=torch.float32, device=model_id.device)), model_id.device, stream)
     idx, sc = out
     _shape(_dev(idx, "node_idx", torch.int32), "node_idx", (n, k))
     _shape(_dev(sc, "score", torch.float32), "score", (n, k))
@@ -767,9 +771,9 @@ def prioritize(chain_offset: torch.Tensor, stage_latency_s: torch.Tensor, deadli
             raise ValueError("one cursor per workflow")
     dev = chain_offset.device
     if out is None:
-        out = (torch.empty(S, dtype=torch.int64, device=dev) if want_remaining else None,
-               torch.empty(W, dtype=torch.int32, device=dev),
-               torch.empty(W, dtype=torch.int32, device=dev))
+        out = _outputs(lambda: (torch.empty(S, dtype=torch.int64, device=dev) if want_remaining else None,
+                                torch.empty(W, dtype=torch.int32, device=dev),
+                                torch.empty(W, dtype=torch.int32, device=dev)), dev, stream)
     rem, key, order = out
     if rem is not None:
         _shape(_dev(rem, "remaining_us", torch.int64), "remaining_us", (S,))
