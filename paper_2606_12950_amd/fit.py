@@ -59,7 +59,8 @@ class Fit:
         self.workspace = torch.empty(max(need), dtype=torch.uint8, device=dev)
 
     def score(self, x: torch.Tensor, bins: torch.Tensor) -> Logprobs:
-        """The layers forward and the observed bins' log probabilities (0 where none was observed)."""
+        """The layers forward and the observed bins' log probabilities (0 where none was observed), in the Fit's buffers:
+        the next call writes them again."""
         h = x
         for l, (w, b) in enumerate(zip(self.weights, self.biases)):
             h = layer(h, w, b, relu=l + 1 < len(self.weights), out=self.hidden[l])
@@ -70,7 +71,7 @@ class Fit:
 
     def gradients(self, x: torch.Tensor, bins: torch.Tensor) -> Tuple[List[torch.Tensor], List[torch.Tensor]]:
         """Gradients of minus the mean log probability of the observed bins (less the entropy bonus), of
-        weights and biases, after ``score``."""
+        weights and biases, after ``score``, in the Fit's buffers: the next call writes them again."""
         given = self._given(bins).float()
         g = given / -given.sum().clamp_min(1.0)
         ge = None if self.g_entropy is None else -self.g_entropy
@@ -85,7 +86,8 @@ class Fit:
     def step(self, x: torch.Tensor, bins: torch.Tensor, rate: float, max_norm: float = 1.0,
              momentum: float = 0.9) -> Tuple[torch.Tensor, torch.Tensor]:
         """One update. Returns the mean log probability before it and the gradient's norm before clipping, on
-        the device."""
+        the device, in tensors of their own (the ones that ``score`` and ``gradients`` return are the Fit's buffers,
+        which the next call writes)."""
         out = self.score(x, bins)
         mean = out.logprob.sum() / self._given(bins).sum().clamp_min(1)
         self.gradients(x, bins)
@@ -96,7 +98,7 @@ class Fit:
             p.add_(v, alpha=-rate)
         for w, p in zip(self.weights, self.masters):
             w.copy_(p)
-        return mean, self.norm
+        return mean, self.norm.clone()
 
 
 def main(argv: Optional[Sequence[str]] = None) -> dict:
