@@ -56,7 +56,7 @@ MAESTRO_API maestro_status maestro_logprobs(int64_t n, int32_t v, const void* lo
  * g_logprob may be NULL together, g_entropy may be NULL (entropy is then not read), not all three. A row without a
  * token takes no part in g_logprob. Rows whose two coefficients are zero, and rows masked
  * throughout, get zeros, whatever they hold; masked logits get 0 (the token's own apart: its
- * derivative is g_logprob). grad may be the logits themselves with the same stride, and must not
+ * derivative is g_logprob), for all finite coefficients. A p_j below float32's least normal number may count as 0. grad may be the logits themselves with the same stride, and must not
  * overlap them otherwise. */
 MAESTRO_API maestro_status maestro_logprobs_grad(int64_t n, int32_t v, const void* logits, int64_t row_stride,
                              int32_t dtype, const int32_t* token, const float* stats, const float* entropy,

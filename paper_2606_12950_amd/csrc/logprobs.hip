@@ -15,7 +15,6 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLeast = -1e30f;     // below any log probability in range; times 0 it is 0
-constexpr float kUnseen = -1e3f;     // below any whose probability is not 0 in float32; times a large coefficient still finite
 constexpr int kMaxAlternatives = MAESTRO_MAX_ALTERNATIVES;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -605,7 +604,8 @@ struct Gradient {
   const float* g_entropy;
 };
 
-// the row's own numbers, and a vector's gradient: hot_j - p_j (g + ge (ln p_j + entropy))
+// the row's own numbers, and a vector's gradient: hot_j - p_j g - ge (p_j (ln p_j + entropy)), the product with p_j first: it
+// is in range where ge ln p_j is not, and 0 where p_j is
 struct GradRow {
   float m, log_s, g, ge, h;
   int32_t t;
@@ -615,19 +615,22 @@ struct GradRow {
     g = (uint32_t)t < (uint32_t)v ? a.g_logprob[row] : 0.0f;
     ge = a.g_entropy ? a.g_entropy[row] : 0.0f;
     h = a.g_entropy ? a.entropy[row] : 0.0f;
+    h = ge != 0.0f ? h : 0.0f;
     const float2 s = *reinterpret_cast<const float2*>(a.stats + 2 * row);
     m = s.x;
     log_s = s.y;
     zero = m == -INFINITY || (g == 0.0f && ge == 0.0f);
   }
-  template <int V>
-  __device__ __forceinline__ void gradient(float (&x)[V], int64_t j, bool with_entropy) const {
+  // without kEntropy: for rows whose ge is 0
+  template <bool kEntropy = true, int V>
+  __device__ __forceinline__ void gradient(float (&x)[V], int64_t j) const {
     const int64_t hot = t - j;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const float lp = (x[i] - m) - log_s, p = __builtin_amdgcn_exp2f(lp * kLog2e);
-      const float c = with_entropy && ge != 0.0f ? fmaf(ge, fmaxf(lp, kUnseen) + h, g) : g;
-      x[i] = zero ? 0.0f : fmaf(-p, c, hot == i ? g : 0.0f);
+      float d = fmaf(-p, g, hot == i ? g : 0.0f);
+      if constexpr (kEntropy) d = fmaf(-ge, p * (fmaxf(lp, kLeast) + h), d);
+      x[i] = zero ? 0.0f : d;
     }
   }
 };
@@ -643,7 +646,7 @@ constexpr int kGradRow = 512;        // and the longest that a wavefront takes
 // row's end. magic = ceil(2^21 / vecs): i * magic >> 21 is i / vecs for i < vecs + 1024, vecs <= 1024.
 // Measured (us; a row to a power of two of lanes before): 300,000 x 293 bfloat16 105 (164), 450,209 x 34 float32 33
 // (44), 10^6 x 3 bfloat16 9.5 (13.9), 2^20 x 64 56 (56). Two or four vectors a thread take 5 to 30% longer (registers).
-template <typename T>
+template <typename T, bool kEntropy>
 __global__ __launch_bounds__(256) void grad_short_kernel(int64_t n, int32_t v, const T* logits, int64_t stride, Gradient a,
                                                          T* grad, int64_t grad_stride, uint32_t vecs, uint32_t magic) {
   constexpr int V = kVec<T>;
@@ -660,7 +663,7 @@ __global__ __launch_bounds__(256) void grad_short_kernel(int64_t n, int32_t v, c
     r.load(a, row, v);
     float x[V];
     unpack(w, x);
-    r.gradient(x, j, a.g_entropy != nullptr);
+    r.template gradient<kEntropy>(x, j);
     T* out = grad + row * grad_stride + j;
     if (j + V <= v) {
       store16(out, pack(x));
@@ -684,7 +687,7 @@ __global__ __launch_bounds__(256) void grad_row_kernel(int64_t n, int32_t v, con
     for (int j = V * lane; j < v; j += V * 64) {
       float x[V];
       load_vec(logits + row * stride, j, v, x);
-      r.gradient(x, j, a.g_entropy != nullptr);
+      r.gradient(x, j);
       T* out = grad + row * grad_stride + j;
       if (j + V <= v) {
         store16(out, pack(x));
@@ -718,14 +721,14 @@ __global__ __launch_bounds__(256) void grad_long_kernel(int64_t n, int32_t v, co
         const int64_t j = first + (u * 256 + threadIdx.x) * V;
         float x[V];
         unpack(w[u], x);
-        r.gradient(x, j, a.g_entropy != nullptr);
+        r.gradient(x, j);
         store16(out + j, pack(x));
       }
     } else {
       for (int64_t j = first + threadIdx.x * V; j < v; j += 256 * V) {
         float x[V];
         load_vec(in, j, v, x);
-        r.gradient(x, j, a.g_entropy != nullptr);
+        r.gradient(x, j);
         if (j + V <= v) {
           store16(out + j, pack(x));
         } else {
@@ -804,10 +807,11 @@ template <typename T>
 maestro_status launch_grad(int64_t n, int32_t v, const T* x, int64_t stride, const Gradient& a, T* grad,
                            int64_t grad_stride, hipStream_t stream) {
   const int64_t vecs = cdiv(v, kVec<T>);
-  if (vecs <= kGradShort<T>)
-    grad_short_kernel<T><<<(unsigned)least(cdiv(n * vecs, 256), kCus * 64), 256, 0, stream>>>(
+  if (vecs <= kGradShort<T>) {
+    auto kernel = a.g_entropy ? grad_short_kernel<T, true> : grad_short_kernel<T, false>;
+    kernel<<<(unsigned)least(cdiv(n * vecs, 256), kCus * 64), 256, 0, stream>>>(
         n, v, x, stride, a, grad, grad_stride, (uint32_t)vecs, (uint32_t)cdiv(1 << 21, vecs));
-  else if (vecs <= kGradRow) {
+  } else if (vecs <= kGradRow) {
     if constexpr (kGradShort<T> < kGradRow)
       grad_row_kernel<T><<<(unsigned)least(cdiv(n, 4), kCus * 64), 256, 0, stream>>>(n, v, x, stride, a, grad, grad_stride);
   } else {
