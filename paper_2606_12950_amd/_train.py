@@ -15,7 +15,7 @@ from typing import NamedTuple, Optional, Sequence
 import torch
 
 from . import _native
-from ._native import MAESTRO_BF16, MAESTRO_F32, _check, _dev, _outputs, _ptr, _scratch, _shape, _stream, _Tensor, _workspace
+from ._native import MAESTRO_BF16, MAESTRO_F32, MaestroError, _check, _dev, _outputs, _ptr, _scratch, _shape, _stream, _Tensor, _workspace
 
 # Every function declared in include/maestro_train.h.
 EXPORTS = ("maestro_logprobs_workspace", "maestro_logprobs", "maestro_logprobs_grad", "maestro_layer",
@@ -74,15 +74,16 @@ def load():
         getattr(lib, f).restype = sz if f.endswith("_workspace") else ctypes.c_int
     module.bind(*(ctypes.cast(getattr(lib, f), P).value for f in (
         "maestro_layer", "maestro_layer_grad_workspace", "maestro_layer_grad", "maestro_logprobs_workspace", "maestro_logprobs",
-        "maestro_logprobs_grad", "maestro_clip_gradients_workspace", "maestro_clip_gradients")))
+        "maestro_logprobs_grad", "maestro_clip_gradients_workspace", "maestro_clip_gradients")), MaestroError)
     _tensors = module
     _lib = lib
     return lib
 
 
 # The calls below go to the native module first where the outputs, the workspace and the stream are the binding's to choose: it
-# takes a plain call whole and gives None for any other, whose errors are raised here. Host time, launch included (us, and
-# without it): log probabilities of one token 8.3 (10.7), their gradient 4.5 (8.1), a layer 4.9 (7.0), its gradients 6.0 (9.0).
+# takes a plain call whole and gives None for any other, and for one that the entry point's checks refuse; their errors are raised
+# here. Host time, launch included (us, and without it): log probabilities of one token 8.3 (10.7), their gradient 4.5 (8.1), a
+# layer 4.9 (7.0), its gradients 6.0 (9.0).
 
 
 def _rows(t: torch.Tensor, name: str):

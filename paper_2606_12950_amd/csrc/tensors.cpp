@@ -1,8 +1,9 @@
 // The binding's host half, the module `_tensors` of the package: a table of many tensors, several outputs allocated at
 // once, and the training operators' calls whole (checks, outputs, workspace, entry point) for the plain case, in which a
-// small call's time is the host's. A call that is not plain (an argument of another type, shape, layout or device, or a
-// status other than MAESTRO_OK) gives None and leaves nothing behind: the Python binding then takes it, and says what is
-// wrong with it. Plain host code against torch's C++ interface.
+// small call's time is the host's. A call that is not plain (an argument of another type, shape, layout or device), or that
+// the entry point's checks refuse, gives None and leaves nothing behind: the Python binding then takes it, and says what is
+// wrong with it. A failed launch raises the binding's error here and is not made again: part of its work may be on the
+// stream. Plain host code against torch's C++ interface.
 #include <Python.h>
 
 #include <ATen/ops/empty.h>
@@ -96,15 +97,19 @@ struct Entries {
   decltype(&maestro_clip_gradients_workspace) clip_workspace;
   decltype(&maestro_clip_gradients) clip;
 } entries;
+PyObject* error;                     // the binding's exception of (entry point, status)
 
-// bind(layer, layer_grad_workspace, ...): the addresses of libmaestro.so's entry points, in the order of Entries
+// bind(layer, layer_grad_workspace, ..., error): the addresses of libmaestro.so's entry points, in the order of Entries,
+// and the exception that a failed launch raises
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
   void* at[8];
   static_assert(sizeof(at) == sizeof(entries), "one address an entry point");
-  if (n != 8) return PyErr_Format(PyExc_TypeError, "eight addresses are needed");
+  if (n != 9 || !PyExceptionClass_Check(args[8])) return PyErr_Format(PyExc_TypeError, "eight addresses and an exception are needed");
   for (int i = 0; i < 8; ++i) at[i] = PyLong_AsVoidPtr(args[i]);
   if (PyErr_Occurred()) return nullptr;
   memcpy(&entries, at, sizeof(at));
+  Py_INCREF(args[8]);
+  Py_XSETREF(error, args[8]);
   Py_RETURN_NONE;
 }
 
@@ -141,6 +146,14 @@ maestro_status unlocked(const F& f) {
   return st;
 }
 
+// The result of a call that `entry` did not take: None, for the binding, where its checks refused it.
+PyObject* refused(const char* entry, maestro_status st) {
+  if (st == MAESTRO_ERR_INVALID_ARG || st == MAESTRO_ERR_UNSUPPORTED || st == MAESTRO_ERR_WORKSPACE) Py_RETURN_NONE;
+  THPObjectPtr e(PyObject_CallFunction(error, "si", entry, static_cast<int>(st)));
+  if (e) PyErr_SetObject(error, e.get());
+  return nullptr;
+}
+
 // x [n][d_in] and weight [d_out][d_in] of one type
 bool layer_shapes(const at::Tensor* x, const at::Tensor* w) {
   if (!strided(x) || !strided(w) || x->dim() != 2 || w->dim() != 2 || code_of(*w) < 0) return false;
@@ -161,7 +174,8 @@ PyObject* layer(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   const at::Tensor y = fresh(*x, x->scalar_type(), {n, o});
   void *xp = at_of(x), *wp = at_of(w), *yp = at_of(&y);
   const float* bp = static_cast<float*>(at_of(b));
-  if (unlocked([&] { return entries.layer(n, i, o, code_of(*w), xp, wp, bp, relu, yp, stream); }) != MAESTRO_OK) Py_RETURN_NONE;
+  const maestro_status st = unlocked([&] { return entries.layer(n, i, o, code_of(*w), xp, wp, bp, relu, yp, stream); });
+  if (st != MAESTRO_OK) return refused("maestro_layer", st);
   return wrap(y);
   END_HANDLE_TH_ERRORS
 }
@@ -183,8 +197,8 @@ PyObject* layer_grad(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   const at::Tensor work = scratch(*x, need);
   void *xp = at_of(x), *wp = at_of(w), *gp = at_of(gz), *gxp = at_of(&gx), *workp = at_of(&work);
   float *gwp = static_cast<float*>(at_of(&gw)), *gbp = static_cast<float*>(at_of(&gb));
-  if (unlocked([&] { return entries.layer_grad(n, i, o, code, xp, wp, gp, relu, gxp, gwp, gbp, workp, need, stream); }) != MAESTRO_OK)
-    Py_RETURN_NONE;
+  const maestro_status st = unlocked([&] { return entries.layer_grad(n, i, o, code, xp, wp, gp, relu, gxp, gwp, gbp, workp, need, stream); });
+  if (st != MAESTRO_OK) return refused("maestro_layer_grad", st);
   return Py_BuildValue("NNN", wrap(gx), wrap(gw), wrap(gb));
   END_HANDLE_TH_ERRORS
 }
@@ -223,8 +237,8 @@ PyObject* logprobs(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   const int32_t* tp = static_cast<int32_t*>(at_of(token));
   int32_t* idp = static_cast<int32_t*>(at_of(&id));
   float *lpp = f(lp), *hp = f(h), *topp = f(top), *sp = f(stats);
-  if (unlocked([&] { return entries.logprobs(n, v, xp, stride, code, tp, k, lpp, hp, idp, topp, sp, workp, need, stream); }) != MAESTRO_OK)
-    Py_RETURN_NONE;
+  const maestro_status st = unlocked([&] { return entries.logprobs(n, v, xp, stride, code, tp, k, lpp, hp, idp, topp, sp, workp, need, stream); });
+  if (st != MAESTRO_OK) return refused("maestro_logprobs", st);
   return Py_BuildValue("NNNNN", wrap(lp), wrap(h), wrap(id), wrap(top), wrap(stats));
   END_HANDLE_TH_ERRORS
 }
@@ -248,8 +262,8 @@ PyObject* logprobs_grad(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   void *xp = at_of(x), *op = at_of(&out);
   const int32_t* tp = static_cast<int32_t*>(at_of(token));
   const float *sp = f(stats), *hp = f(h), *gp = f(g), *gep = f(ge);
-  if (unlocked([&] { return entries.logprobs_grad(n, v, xp, stride, code_of(*x), tp, sp, hp, gp, gep, op, v, stream); }) != MAESTRO_OK)
-    Py_RETURN_NONE;
+  const maestro_status st = unlocked([&] { return entries.logprobs_grad(n, v, xp, stride, code_of(*x), tp, sp, hp, gp, gep, op, v, stream); });
+  if (st != MAESTRO_OK) return refused("maestro_logprobs_grad", st);
   return wrap(out);
   END_HANDLE_TH_ERRORS
 }
@@ -288,8 +302,8 @@ PyObject* clip(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   float* np = static_cast<float*>(at_of(&norm));
   void* workp = at_of(&work);
   void* const* op = a[2] != Py_None ? out.at.data() : nullptr;
-  if (unlocked([&] { return entries.clip(n, in.at.data(), op, in.size.data(), in.code.data(), max_norm, np, workp, need, stream); }) != MAESTRO_OK)
-    Py_RETURN_NONE;
+  const maestro_status st = unlocked([&] { return entries.clip(n, in.at.data(), op, in.size.data(), in.code.data(), max_norm, np, workp, need, stream); });
+  if (st != MAESTRO_OK) return refused("maestro_clip_gradients", st);
   return wrap(norm);
   END_HANDLE_TH_ERRORS
 }
