@@ -4,14 +4,15 @@ them back into the predictor).
 A step takes the batch's features through the layers (activations kept), reads the log probability of
 every stage's observed length bin, takes the gradient of their mean back through the layers, clips it
 by its global norm and moves float32 master weights by it (momentum), from which the predictor's own
-weights are rounded. All but the update runs in the library's kernels, in the buffers a ``Fit`` holds;
-nothing in a step synchronises. The weights are the ones ``predict`` takes.
+weights are rounded; a batch whose gradient's norm is not finite moves nothing. All but the update runs in the
+library's kernels, in the buffers a ``Fit`` holds; nothing in a step synchronises. The weights are the ones ``predict`` takes.
 
     python -m paper_2606_12950_amd.fit --workload c1 --stages 65536 --steps 50
 """
 from __future__ import annotations
 
 import argparse
+import math
 from typing import List, Optional, Sequence, Tuple
 
 import torch
@@ -41,12 +42,17 @@ class Fit:
         dt, dev = weights[0].dtype, weights[0].device
         widths = [weights[0].shape[1]] + [w.shape[0] for w in weights]
         f = dict(dtype=torch.float32, device=dev)
-        self.masters = [w.float().clone() for w in weights]
-        self.velocity = [torch.zeros_like(p) for p in (*self.masters, *self.biases)]
+        # masters, gradients and velocities each end to end, weights first (16-byte aligned: widths are multiples of 16), so
+        # that an update takes few launches
+        L, size = len(weights), sum(t.numel() for t in (*weights, *biases))
+        views = lambda flat, like: [v.view(t.shape) for v, t in zip(flat.split([t.numel() for t in like]), like)]
+        self._master = torch.cat([w.reshape(-1).float() for w in weights])
+        self._gradient, self._velocity = torch.zeros(size, **f), torch.zeros(size, **f)
+        self.masters, self.velocity = views(self._master, weights), views(self._velocity, [*weights, *biases])
+        gradients = views(self._gradient, [*weights, *biases])
+        self.g_weights, self.g_biases = gradients[:L], gradients[L:]
         self.hidden = [torch.empty(n, w, dtype=dt, device=dev) for w in widths[1:]]      # the last: logits
         self.g_z = [torch.empty_like(h) for h in self.hidden]
-        self.g_weights = [torch.empty(tuple(w.shape), **f) for w in weights]
-        self.g_biases = [torch.empty_like(b) for b in biases]
         self.out = Logprobs(torch.empty(n, **f), torch.empty(n, **f), torch.empty(n, 0, dtype=torch.int32, device=dev),
                             torch.empty(n, 0, **f), torch.empty(n, 2, **f))
         self.entropy_bonus = entropy_bonus
@@ -85,17 +91,22 @@ class Fit:
 
     def step(self, x: torch.Tensor, bins: torch.Tensor, rate: float, max_norm: float = 1.0,
              momentum: float = 0.9) -> Tuple[torch.Tensor, torch.Tensor]:
-        """One update. Returns the mean log probability before it and the gradient's norm before clipping, on
-        the device, in tensors of their own (the ones that ``score`` and ``gradients`` return are the Fit's buffers,
-        which the next call writes)."""
+        """One update; where the gradient's norm is not finite, weights, biases and velocities stay as they are. Returns
+        the mean log probability before it and the norm before clipping, on the device, in tensors of their own (the
+        ones that ``score`` and ``gradients`` return are the Fit's buffers, which the next call writes)."""
         out = self.score(x, bins)
         mean = out.logprob.sum() / self._given(bins).sum().clamp_min(1)
         self.gradients(x, bins)
         grads = [*self.g_weights, *self.g_biases]
         clip_gradients(grads, max_norm, norm=self.norm, workspace=self.workspace)
-        for p, v, g in zip((*self.masters, *self.biases), self.velocity, grads):
-            v.mul_(momentum).add_(g)
-            p.add_(v, alpha=-rate)
+        finite, v = self.norm < math.inf, self._velocity * momentum       # a NaN is not less
+        v.add_(self._gradient)
+        by, at = torch.where(finite, v, 0.0), self._master.numel()
+        torch.where(finite, v, self._velocity, out=self._velocity)
+        self._master.add_(by[:at], alpha=-rate)
+        for b in self.biases:
+            b.add_(by[at:at + b.numel()], alpha=-rate)
+            at += b.numel()
         for w, p in zip(self.weights, self.masters):
             w.copy_(p)
         return mean, self.norm.clone()

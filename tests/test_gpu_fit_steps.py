@@ -1,4 +1,7 @@
-"""What Fit.step gives back and leaves behind: every step's own norm."""
+"""What Fit.step gives back and leaves behind: every step's own norm, weights that a batch without finite gradients does not
+touch."""
+import math
+
 import pytest
 import torch
 
@@ -15,6 +18,10 @@ def batch(dims, dtype, n, seed):
     return x, torch.randint(-1, dims[-1], (n,), generator=g, dtype=torch.int32).cuda()
 
 
+def state(f):
+    return [t.clone() for t in (*f.weights, *f.biases, *f.masters, *f.velocity)]
+
+
 def test_every_step_has_its_own_norm():
     dims, dtype = NETWORKS[0]
     f = F.Fit(*network(dims, dtype, 1), 100)
@@ -24,3 +31,22 @@ def test_every_step_has_its_own_norm():
         kept.append((mean, norm))
         seen.append((mean.item(), norm.item()))
     assert [(m.item(), n.item()) for m, n in kept] == seen and len(set(seen)) == 4
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("dims,dtype", NETWORKS)
+def test_a_step_without_finite_gradients_changes_nothing(dims, dtype, bad):
+    n, fits = 100, []
+    for with_bad in (False, True):
+        f = F.Fit(*network(dims, dtype, 2), n)
+        f.step(*batch(dims, dtype, n, 1), 0.1)
+        if with_bad:
+            before = state(f)
+            x, bins = batch(dims, dtype, n, 2)
+            x[5], bins[5] = bad, 3
+            mean, norm = f.step(x, bins, 0.1)
+            assert not math.isfinite(mean.item()) and not math.isfinite(norm.item())
+            assert all(map(torch.equal, state(f), before))
+        f.step(*batch(dims, dtype, n, 3), 0.1)
+        fits.append(state(f))
+    assert all(map(torch.equal, *fits)) and all(t.isfinite().all() for t in fits[0])
