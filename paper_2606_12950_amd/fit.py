@@ -72,14 +72,19 @@ class Fit:
             h = layer(h, w, b, relu=l + 1 < len(self.weights), out=self.hidden[l])
         return logprobs(h, bins, out=self.out, workspace=self.workspace)
 
-    def _given(self, bins: torch.Tensor) -> torch.Tensor:
-        return (bins >= 0) & (bins < self.hidden[-1].shape[1])
+    def _given(self, bins: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+        """Which stages' bins were observed, and how many (1 where none)."""
+        given = (bins >= 0) & (bins < self.hidden[-1].shape[1])
+        return given, given.sum().clamp_min(1)
 
     def gradients(self, x: torch.Tensor, bins: torch.Tensor) -> Tuple[List[torch.Tensor], List[torch.Tensor]]:
         """Gradients of minus the mean log probability of the observed bins (less the entropy bonus), of
-        weights and biases, after ``score``, in the Fit's buffers: the next call writes them again."""
-        given = self._given(bins).float()
-        g = given / -given.sum().clamp_min(1.0)
+        weights and biases, after ``score``, in the Fit's buffers: the next call writes them again. Features
+        have to be finite, also those of stages without an observed bin."""
+        return self._gradients(x, bins, *self._given(bins))
+
+    def _gradients(self, x, bins, given, count):
+        g = given.float() / -count
         ge = None if self.g_entropy is None else -self.g_entropy
         logprobs_grad(self.hidden[-1], bins, self.out.stats, self.out.entropy, g, ge, out=self.g_z[-1])
         for l in reversed(range(len(self.weights))):
@@ -93,10 +98,18 @@ class Fit:
              momentum: float = 0.9) -> Tuple[torch.Tensor, torch.Tensor]:
         """One update; where the gradient's norm is not finite, weights, biases and velocities stay as they are. Returns
         the mean log probability before it and the norm before clipping, on the device, in tensors of their own (the
-        ones that ``score`` and ``gradients`` return are the Fit's buffers, which the next call writes)."""
+        ones that ``score`` and ``gradients`` return are the Fit's buffers, which the next call writes). Stages without
+        an observed bin take no part, whatever their features hold (with an entropy bonus they take part in that, and
+        their features have to be finite)."""
+        width = self.weights[0].shape[1]
+        _native._shape(_native._dev(x, "x", self.weights[0].dtype), "x", (self.n, width))
+        _native._shape(_native._dev(bins, "bins", torch.int32), "bins", (self.n,))
+        given, count = self._given(bins)
+        if not self.entropy_bonus:
+            x = torch.where(given[:, None], x, 0.0)        # 0 times a NaN would be one in the weights' gradient
         out = self.score(x, bins)
-        mean = out.logprob.sum() / self._given(bins).sum().clamp_min(1)
-        self.gradients(x, bins)
+        mean = out.logprob.sum() / count
+        self._gradients(x, bins, given, count)
         grads = [*self.g_weights, *self.g_biases]
         clip_gradients(grads, max_norm, norm=self.norm, workspace=self.workspace)
         finite, v = self.norm < math.inf, self._velocity * momentum       # a NaN is not less

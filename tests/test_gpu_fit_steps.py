@@ -1,5 +1,5 @@
 """What Fit.step gives back and leaves behind: every step's own norm, weights that a batch without finite gradients does not
-touch."""
+touch, and stages without an observed length that take no part whatever their features hold."""
 import math
 
 import pytest
@@ -50,3 +50,27 @@ def test_a_step_without_finite_gradients_changes_nothing(dims, dtype, bad):
         f.step(*batch(dims, dtype, n, 3), 0.1)
         fits.append(state(f))
     assert all(map(torch.equal, *fits)) and all(t.isfinite().all() for t in fits[0])
+
+
+@pytest.mark.parametrize("dims,dtype", NETWORKS)
+def test_unobserved_stages_take_no_part(dims, dtype):
+    n, got = 200, []
+    for features in (0.0, 1.0, math.nan, math.inf):
+        f = F.Fit(*network(dims, dtype, 3), n)
+        x, bins = batch(dims, dtype, n, 4)
+        bins[17], bins[150] = -1, dims[-1]
+        x[17], x[150, 3] = features, features
+        x[150, :3] = 0.0
+        mean, norm = f.step(x, bins, 0.1)
+        got.append([mean, norm, *state(f)])
+    for other in got[1:]:
+        assert all(map(torch.equal, other, got[0]))
+    assert all(t.isfinite().all() for t in got[0])
+
+
+def test_shapes_of_a_step():
+    f = F.Fit(*network((32, 16), torch.float32, 3), 6)
+    bins = torch.zeros(6, dtype=torch.int32, device="cuda")
+    for x, b in ((torch.zeros(1, 32), bins), (torch.zeros(6, 16), bins), (torch.zeros(6, 32), bins[:1])):
+        with pytest.raises(ValueError):
+            f.step(x.cuda(), b, 0.1)
