@@ -136,6 +136,8 @@ def main(argv: Optional[Sequence[str]] = None) -> dict:
     ap.add_argument("--rate", type=float, default=0.2)
     ap.add_argument("--max-norm", type=float, default=1.0)
     a = ap.parse_args(argv)
+    if a.steps < 1:
+        ap.error("--steps must be at least 1")
     if W.SPECS[a.workload].n_workflows:
         ap.error("a workload of single stages is needed")
     wl = W.workload(a.workload, **({} if a.stages is None else dict(n_stages=a.stages)))
