@@ -60,7 +60,14 @@ def load():
     lib = _native.load()
     if not os.path.exists(TENSORS_PATH):
         raise RuntimeError(f"{TENSORS_PATH} is missing: build it first (python -m paper_2606_12950_amd.build)")
-    from . import _tensors as module
+    try:
+        from . import _tensors as module
+        built = module.torch_version
+    except (ImportError, AttributeError) as e:         # a symbol that this torch does not have, or an older build
+        built = str(e)
+    if built != torch.__version__:
+        raise RuntimeError(f"{TENSORS_PATH} was built against another torch ({built}) than {torch.__version__}: "
+                           "build it again (python -m paper_2606_12950_amd.build)")
     P, i32, i64, f32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
     lib.maestro_logprobs_workspace.argtypes = [i64, i32, i32, i32]
     lib.maestro_logprobs.argtypes = [i64, i32, P, i64, i32, P, i32, P, P, P, P, P, P, sz, P]

@@ -1,6 +1,6 @@
 """Build libmaestro.so (gfx950) in-tree with hipcc, and beside it libmaestro_calibrate.so, the
 measurement-only matrix-core ceiling kernel that bench.py --mfma-ceiling times, and _tensors.so, the host
-half of the training operators' binding (g++).
+half of the training operators' binding (the host's C++ compiler and torch's headers).
 
 Usage: python -m paper_2606_12950_amd.build [-v]
 """
@@ -61,14 +61,20 @@ def _compile(src: str, outdir: str, verbose: bool) -> str:
     return obj
 
 
+def _host_compiler() -> str:
+    """$CXX, else g++, else the clang++ that hipcc runs."""
+    return os.environ.get("CXX") or shutil.which("g++") or os.path.join(os.path.dirname(HIPCC), "amdclang++")
+
+
 def _compile_tensors(outdir: str, verbose: bool) -> str:
     import torch
     from torch.utils import cpp_extension
 
     out = os.path.join(outdir, os.path.basename(TENSORS_LIB))
     include = [*cpp_extension.include_paths(), sysconfig.get_paths()["include"], INCLUDE]
-    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *(f"-I{p}" for p in include),
+    cmd = [_host_compiler(), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           f'-DMAESTRO_TORCH_VERSION="{torch.__version__}"', *(f"-I{p}" for p in include),
            os.path.join(CSRC, TENSORS_SOURCE), "-o", out, *(f"-L{p}" for p in cpp_extension.library_paths()),
            "-ltorch_python", "-ltorch_cpu", "-lc10"]
     if verbose:
@@ -92,14 +98,16 @@ def build(verbose: bool = False) -> str:
         with ThreadPoolExecutor(max_workers=len(SOURCES) + 2) as ex:
             tensors = ex.submit(_compile_tensors, tmp, verbose)
             objs = list(ex.map(lambda s: _compile(s, tmp, verbose), SOURCES + (CALIBRATE_SOURCE,)))
+        built = {TENSORS_LIB: tensors.result()}
         for lib, lib_objs in ((LIB, objs[:-1]), (CALIBRATE_LIB, objs[-1:])):
-            out = os.path.join(tmp, os.path.basename(lib))
+            built[lib] = out = os.path.join(tmp, os.path.basename(lib))
             cmd = [HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", *lib_objs, "-o", out]
             if verbose:
                 print(" ".join(cmd), flush=True)
             subprocess.run(cmd, check=True)
+        # all or none: the host half calls the library's entry points by address, as this source declares them
+        for lib, out in built.items():
             _install(out, lib)
-        _install(tensors.result(), TENSORS_LIB)
     return LIB
 
 

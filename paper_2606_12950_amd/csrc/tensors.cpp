@@ -318,4 +318,9 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, n
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__tensors() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__tensors() {
+  PyObject* m = PyModule_Create(&module);
+  // the torch whose interface this was compiled against: the binding refuses another
+  if (m && PyModule_AddStringConstant(m, "torch_version", MAESTRO_TORCH_VERSION) < 0) Py_CLEAR(m);
+  return m;
+}
