@@ -88,7 +88,8 @@ MAESTRO_API maestro_status maestro_layer_grad(int64_t n, int32_t d_in, int32_t d
  *                           element, NULL allowed for size 0), element counts (up to 2^39 bytes), maestro_dtype
  *   out                     HOST array [n_tensors] of device pointers the result is written to, scaled
  *                           or not, each of its tensor's type and size; NULL: in place, where nothing is
- *                           written unless the norm exceeds max_norm. out[i] is tensors[i] itself or overlaps none
+ *                           written unless the norm exceeds max_norm. out[i] is tensors[i] itself or overlaps none;
+ *                           no two tensors overlap
  * A norm that is not finite in float64 (an input is NaN or infinite) scales nothing; one past float32 is
  * written as infinity and scales all the same. Workspace: maestro_clip_gradients_workspace() bytes. */
 MAESTRO_API size_t maestro_clip_gradients_workspace(int32_t n_tensors);

@@ -4,6 +4,9 @@ Argument marshalling only, in the manner of ``_native``: the tensors are checked
 workspaces allocated where the caller passes none, and every computation runs in the HIP kernels of
 libmaestro.so on the current stream. Where Python would take longer than the GPU (hundreds of tensors,
 several outputs) the native module ``_tensors`` does it. There is no fallback.
+
+Nothing here is recorded for autograd: a tensor that requires gradients is read as any other, and the results
+are detached. ``logprobs_grad`` and ``layer_grad`` are the gradients.
 """
 from __future__ import annotations
 
@@ -270,7 +273,8 @@ def clip_gradients(tensors: Sequence[torch.Tensor], max_norm: float, out: Option
                    stream=None) -> torch.Tensor:
     """maestro_clip_gradients: scales all ``tensors`` (float32 or bfloat16, contiguous) by max_norm / norm where
     the norm of all their values together exceeds ``max_norm``, in place or into ``out``. Returns the
-    norm before clipping, float32 [1] on the device. A norm that is not finite scales nothing."""
+    norm before clipping, float32 [1] on the device. A norm that is not finite scales nothing. ``max_norm`` past
+    float32's range (math.inf) computes the norm alone and takes no ``out``. No two tensors overlap."""
     lib = load()
     tensors = list(tensors)
     if not tensors:

@@ -5,7 +5,8 @@
 // here in 32x32x2 float32 MFMAs, four wavefronts of 32 W x 32 W each. Stages of 16 k come through
 // registers into two LDS buffers laid out [k][p], so every operand is turned (or not) as it is written, and a product
 // reads one word a lane. Bound by the float32 matrix cores (64 operations a cycle and SIMD, 1/16 of bfloat16) on wide
-// layers, by launches on the small ones it is for. Measured: 4,096 x 64 -> 128 7 us; see wide and cut_of for the rest.
+// layers, by launches on the small ones it is for. Measured: 4,096 x 64 -> 128 5.5 us, 60,000 x 1024 -> 1024
+// 1,061 (floor 833), 150,000 x 256 -> 256 195 (130): one 16-k stage ahead does not cover a load; see wide and cut_of for the rest.
 #include "mlp.h"
 #include "train.h"
 

@@ -13,9 +13,11 @@
 // tile's last products and its stores, and its stores under the next tile's products.
 //
 // Bound by the matrix cores on wide layers, by HBM on narrow ones. Measured: 262,139 x 1024 -> 1024
-// (0.55 TFLOP a product) activations 522 to 540 us = 1.02 to 1.05 PFLOP/s, input's gradient 564, weights' 505; a
-// 16,384-cubed library product reaches 1.31 to 1.35 on the same card, and the library's products of these shapes 555, 618
-// and 1,230 us. 512 -> 256: activations 95 us for 403 MB, input's gradient 132 us for 671 MB = 5.1 TB/s, what a copy reaches.
+// (0.55 TFLOP a product) activations 523 us in the first launches, 550 in a long run and up to 680 in between, while the
+// clock settles to the matrix cores' power; input's gradient 535 and 560, weights' 447 and 475, 20 more to join its shares
+// (as calls, over changing inputs: 533, and 1,047 for both gradients). A 16,384-cubed library product reaches 1.31 to 1.35
+// PFLOP/s on the same card, and the library's products of these shapes 555, 618 and 1,230 us. 512 -> 256: activations 96 us for
+// 403 MB, input's gradient 131 to 140 us for 671 MB = 4.8 to 5.1 TB/s, what a copy reaches.
 #include <type_traits>
 
 #include "mlp.h"
@@ -330,7 +332,9 @@ struct Tile {
   static constexpr int kBiasLoads = Out::kBias ? (WP + 1) / 2 : 0;
   static constexpr int kBiasBytes = 2 * 4 * 256 * kBiasLoads;                 // two places for each wavefront
   static constexpr int kBytes = kBufs * kStage + (kStores ? 4 * Staging<WP>::kBytes : 0) + kBiasBytes;
-  static constexpr int kResident = WP * WQ > 8 ? 1 : WP * WQ > 2 ? 2 : 4;     // workgroups of a CU
+  // workgroups of a CU that a launch plans for, and that registers allow. LDS lets three run of the activations' 64 x 64
+  // (43,008 bytes of 160 KB) and two of pair_kernel<4, 1> (81,920, the larger tile's, in all of them).
+  static constexpr int kResident = WP * WQ > 8 ? 1 : WP * WQ > 2 ? 2 : 4;
 };
 
 // The share of workgroup `block` of `blocks` (a multiple of 8) in a product.

@@ -2,12 +2,14 @@
 //
 // With m the row's maximum and u_j = (x_j - m) log2 e: S = sum 2^u_j, T = sum 2^u_j u_j, ln p_t = (x_t - m) - ln S and
 // entropy = ln 2 (log2 S - T / S). The difference comes first, so large logits lose nothing to a rounded
-// product; the hardware's 2^x and log2 are good to an ulp.
+// product; the hardware's 2^x and log2 are good to an ulp. A long row's S and T are chains of v / 64 to v / 512 additions, a chain
+// a thread, and then a tree.
 //
 // A pass reads every logit once and is bound by HBM, but for short rows with alternatives, which are bound by the
-// vector ALU. Measured (a copy reaches 5.0 TB/s): 4,096 rows of 50,257 float32 with 5 alternatives 158 us = 5.2 TB/s,
-// 2,048 of 131,072 bfloat16 with 8 111 us = 4.8; 2^20 rows of 64 bfloat16 30 us without alternatives, 40 with one
-// and 52 with four (floor 38). Gradient: 2^20 x 64 bfloat16 56 us = 5.1 TB/s, 2,048 x 131,072 187 us = 5.7.
+// vector ALU. Measured, passes back to back over changing inputs (a copy reaches 5.1 TB/s): 4,096 rows of 50,257 float32 with 5
+// alternatives 160 us = 5.1 TB/s, 2,048 of 131,072 bfloat16 with 8 117 us = 4.6; 2^20 rows of 64 bfloat16 37 us without
+// alternatives (30 where the logits are still in the memory-side cache), 41 with one and 53 with four (floors 30, 32 and 37).
+// Gradient: 2^20 x 64 bfloat16 55 us = 5.2 TB/s, 2,048 x 131,072 187 us = 5.7.
 #include "train.h"
 
 namespace maestro {
