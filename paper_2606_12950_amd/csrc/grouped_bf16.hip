@@ -1,0 +1,185 @@
+// The bfloat16 products (products_bf16.h) of a grouped layer and its gradients.
+//
+// Rows of a group make tiles of their own, each against the group's weights; workgroups are persistent and find a tile's group
+// in a table of the groups' rows that each builds in LDS. The weights' gradients cut every group's rows into shares of
+// k_split; a group of one share writes its gradient, of more its shares, which a second launch adds in order.
+#include "groups.h"
+#include "layers.h"
+#include "products_bf16.h"
+
+namespace maestro {
+namespace {
+
+// Tiles of TQ rows of a group (q), all p tiles of one after the other.
+template <int TP, int TQ, int kDepth>
+struct GroupedRows {
+  const Product& g;
+  const GroupTable& table;
+  int32_t n_groups;
+  __device__ __forceinline__ int64_t items() const { return table.first_unit(n_groups) * g.p_tiles; }
+  __device__ __forceinline__ Item item(int64_t i) const {
+    Item t;
+    const int64_t unit = i / g.p_tiles;
+    t.group = table.group_of(unit, n_groups);
+    t.p = g.p + t.group * (g.np * g.nk);
+    t.q = g.q;
+    t.q0 = table.first_row(t.group) + (unit - table.first_unit(t.group)) * TQ;
+    t.q_end = table.first_row(t.group + 1);
+    t.p0 = i % g.p_tiles * TP;
+    t.k0 = 0;
+    t.kn = g.nk;
+    t.stages = (g.nk + kDepth - 1) / kDepth;
+    t.slot = 0;
+    t.whole = true;
+    return t;
+  }
+};
+
+// Tiles of a group's weights' gradient over one of its shares of rows (k).
+template <int TP, int TQ, int kDepth>
+struct GroupedSums {
+  const Product& g;
+  const GroupTable& table;
+  int32_t n_groups;
+  __device__ __forceinline__ int64_t tiles() const { return (g.nq + TQ - 1) / TQ * g.p_tiles; }
+  __device__ __forceinline__ int64_t items() const { return table.first_unit(n_groups) * tiles(); }
+  __device__ __forceinline__ Item item(int64_t i) const {
+    Item t;
+    t.slot = i / tiles();
+    const int64_t tile = i % tiles();
+    t.group = table.group_of(t.slot, n_groups);
+    t.p = g.p;
+    t.q = g.q;
+    t.q0 = tile / g.p_tiles * TQ;
+    t.q_end = g.nq;
+    t.p0 = tile % g.p_tiles * TP;
+    t.k0 = table.first_row(t.group) + (t.slot - table.first_unit(t.group)) * g.k_split;
+    const int64_t left = table.first_row(t.group + 1) - t.k0;
+    t.kn = left < g.k_split ? left : g.k_split;
+    t.stages = (t.kn + kDepth - 1) / kDepth;
+    t.whole = true;
+    return t;
+  }
+};
+
+struct GroupedWeightGrad {
+  static constexpr bool kBias = false, kInt8 = false;
+  float *gw, *gb, *gw_parts, *gb_parts;
+  int32_t parts;                     // 1
+  const GroupTable* table;
+  __device__ __forceinline__ bool direct(const Item& t) const {
+    return table->first_unit(t.group + 1) - table->first_unit(t.group) == 1;
+  }
+  __device__ __forceinline__ float* weights(const Product& g, const Item& t) const {
+    return direct(t) ? gw + t.group * (g.nq * g.np) : gw_parts + t.slot * g.nq * g.np;
+  }
+  __device__ __forceinline__ float* biases(const Product& g, const Item& t, int64_t, int) const {
+    return direct(t) ? gb + t.group * g.nq : gb_parts + t.slot * g.nq;
+  }
+};
+
+template <int WP, int WQ, int kDepth, int kBufs, bool kPT, class Out>
+__global__ __launch_bounds__(kThreads, (Tile<WP, WQ, kDepth, kBufs, Out>::kResident)) void rows_kernel(
+    Product g, Out out, const int64_t* offsets, int32_t n_groups, int64_t n) {
+  using L = Tile<WP, WQ, kDepth, kBufs, Out>;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[L::kBytes];
+  __shared__ GroupTable table;
+  table.build(offsets, n_groups, n, L::TQ);
+  product<WP, WQ, kDepth, kBufs, kPT, false>(g, out, GroupedRows<L::TP, L::TQ, kDepth>{g, table, n_groups}, lds, blockIdx.x, gridDim.x);
+}
+
+template <int WP, int WQ, int kDepth, int kBufs>
+__global__ __launch_bounds__(kThreads, (Tile<WP, WQ, kDepth, kBufs, GroupedWeightGrad>::kResident)) void sums_kernel(
+    Product g, GroupedWeightGrad out, const int64_t* offsets, int32_t n_groups, int64_t n) {
+  using L = Tile<WP, WQ, kDepth, kBufs, GroupedWeightGrad>;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[L::kBytes];
+  __shared__ GroupTable table;
+  table.build(offsets, n_groups, n, g.k_split);
+  out.table = &table;
+  product<WP, WQ, kDepth, kBufs, true, true>(g, out, GroupedSums<L::TP, L::TQ, kDepth>{g, table, n_groups}, lds, blockIdx.x, gridDim.x);
+}
+
+uint32_t blocks_of(int64_t items, int64_t resident) {
+  const int64_t want = cdiv(items, 8) * 8, most = kCus * resident;
+  return (uint32_t)(want < most ? want : most);
+}
+
+template <int W, bool kPT, class Out>
+void launch_tiles(Product g, const Out& out, const int64_t* offsets, int32_t n_groups, int64_t n, hipStream_t stream) {
+  using L = Tile<W, W, 64, 2, Out>;
+  g.p_tiles = (int32_t)cdiv(g.np, L::TP);
+  const uint32_t blocks = blocks_of((n / L::TQ + n_groups) * g.p_tiles, L::kResident);
+  rows_kernel<W, W, 64, 2, kPT><<<blocks, kThreads, 0, stream>>>(g, out, offsets, n_groups, n);
+}
+
+template <bool kPT, class Out>
+void launch_rows(const Product& g, const Out& out, const int64_t* offsets, int32_t n_groups, int64_t n, hipStream_t stream) {
+  if (g.np > 128 && cdiv(g.np, 256) * (n / 256) >= 2 * kCus) launch_tiles<4, kPT>(g, out, offsets, n_groups, n, stream);
+  else if (cdiv(g.np, 128) * (n / 128) >= kCus) launch_tiles<2, kPT>(g, out, offsets, n_groups, n, stream);
+  else launch_tiles<1, kPT>(g, out, offsets, n_groups, n, stream);
+}
+
+template <int WP, int WQ, int kDepth, int kBufs>
+void launch_sums(Product g, const GroupedWeightGrad& out, const int64_t* offsets, int32_t n_groups, int64_t n, hipStream_t stream) {
+  using L = Tile<WP, WQ, kDepth, kBufs, GroupedWeightGrad>;
+  g.p_tiles = (int32_t)cdiv(g.np, L::TP);
+  const uint32_t blocks = blocks_of((n / g.k_split + n_groups) * g.p_tiles * cdiv(g.nq, L::TQ), L::kResident);
+  sums_kernel<WP, WQ, kDepth, kBufs><<<blocks, kThreads, 0, stream>>>(g, out, offsets, n_groups, n);
+}
+
+// Tile of the weights' gradient and rows of a share, as for a layer of one group.
+struct Cut {
+  int32_t tp, tq;
+  int64_t k_split, most;
+};
+Cut cut_of(int64_t n, int64_t n_groups, int64_t d_in, int64_t d_out) {
+  Cut c;
+  c.tp = d_in > 128 ? 256 : 128;
+  c.tq = c.tp == 128 ? 128 : d_out > 128 && n >= 131072 ? 256 : 64;
+  const int64_t tiles = cdiv(d_in, c.tp) * cdiv(d_out, c.tq), resident = c.tq == 256 ? 1 : 2;
+  int64_t splits = kCus * resident / tiles;
+  if (splits > cdiv(n, 512)) splits = cdiv(n, 512);
+  if (splits < 1) splits = 1;
+  c.k_split = cdiv(cdiv(n, splits), 64) * 64;
+  c.most = n / c.k_split + n_groups;
+  return c;
+}
+
+}  // namespace
+
+maestro_status launch_layer_grouped_bf16(int64_t n, int32_t n_groups, int32_t d_in, int32_t d_out, const void* x,
+                                         const void* weight, const float* bias, const int64_t* offsets, bool relu, void* y,
+                                         hipStream_t stream) {
+  const Product g{static_cast<const __bf16*>(weight), static_cast<const __bf16*>(x), d_in, d_in, d_out, n, d_in, d_in, 1, 0, 0};
+  launch_rows<false>(g, Forward{bias, static_cast<__bf16*>(y), relu}, offsets, n_groups, n, stream);
+  return launch_status();
+}
+
+size_t grouped_grad_bf16_workspace_bytes(int64_t n, int32_t n_groups, int32_t d_in, int32_t d_out) {
+  if (n == 0) return 0;
+  return sizeof(float) * (size_t)(cut_of(n, n_groups, d_in, d_out).most * ((int64_t)d_in + 1) * d_out);
+}
+
+maestro_status launch_grouped_grad_bf16(int64_t n, int32_t n_groups, int32_t d_in, int32_t d_out, const void* x,
+                                        const void* weight, const void* g_z, const int64_t* offsets, bool relu_input,
+                                        void* g_x, float* g_weight, float* g_bias, void* workspace, hipStream_t stream) {
+  const int64_t size = (int64_t)d_in * d_out;
+  if (n == 0) return launch_join_groups(0, n_groups, offsets, 1, nullptr, g_weight, size, nullptr, g_bias, d_out, stream);
+  const __bf16 *xb = static_cast<const __bf16*>(x), *gz = static_cast<const __bf16*>(g_z);
+  const Cut c = cut_of(n, n_groups, d_in, d_out);
+  float *gw_parts = static_cast<float*>(workspace), *gb_parts = gw_parts + c.most * size;
+  if (g_x) {
+    const Product gx{static_cast<const __bf16*>(weight), gz, d_in, d_out, d_in, n, d_out, d_out, 1, 0, 0};
+    launch_rows<true>(gx, InputGrad{xb, static_cast<__bf16*>(g_x), relu_input}, offsets, n_groups, n, stream);
+  }
+  const Product gw{xb, gz, d_in, d_out, d_in, d_out, n, c.k_split, 1, 0, 0};
+  const GroupedWeightGrad out{g_weight, g_bias, gw_parts, gb_parts, 1, nullptr};
+  if (c.tq == 256) launch_sums<4, 4, 32, 4>(gw, out, offsets, n_groups, n, stream);
+  else if (c.tp == 256) launch_sums<4, 1, 64, 2>(gw, out, offsets, n_groups, n, stream);
+  else launch_sums<2, 2, 64, 2>(gw, out, offsets, n_groups, n, stream);
+  const maestro_status st = launch_status();
+  if (st != MAESTRO_OK) return st;
+  return launch_join_groups(n, n_groups, offsets, c.k_split, gw_parts, g_weight, size, gb_parts, g_bias, d_out, stream);
+}
+
+}  // namespace maestro

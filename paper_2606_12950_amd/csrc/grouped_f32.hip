@@ -1,0 +1,202 @@
+// The float32 products (products_f32.h) of a grouped layer and its gradients, and the join of a group's shares.
+//
+// Rows of a group make tiles of their own, each against the group's weights. The weights' gradients cut every group's
+// rows into shares of k_split; a group of one share writes its gradient, of more its shares, which a second launch adds in order.
+#include "groups.h"
+#include "layers.h"
+#include "products_f32.h"
+
+namespace maestro {
+namespace {
+
+// Tiles of T rows of a group (q), all p tiles of one after the other.
+template <int T>
+struct GroupedRows {
+  const Product& g;
+  const GroupTable& table;
+  int32_t n_groups;
+  __device__ __forceinline__ int64_t items() const { return table.first_unit(n_groups) * g.p_tiles; }
+  __device__ __forceinline__ Item item(int64_t i) const {
+    Item t;
+    const int64_t unit = i / g.p_tiles;
+    t.group = table.group_of(unit, n_groups);
+    t.q0 = table.first_row(t.group) + (unit - table.first_unit(t.group)) * T;
+    t.q_end = table.first_row(t.group + 1);
+    t.p0 = i % g.p_tiles * T;
+    t.k0 = 0;
+    t.k_end = g.nk;
+    t.slot = 0;
+    t.p_shift = t.group * (g.np * g.nk);
+    t.direct = true;
+    return t;
+  }
+};
+
+// Tiles of a group's weights' gradient over one of its shares of rows (k).
+template <int T>
+struct GroupedSums {
+  const Product& g;
+  const GroupTable& table;
+  int32_t n_groups;
+  __device__ __forceinline__ int64_t tiles() const { return (g.nq + T - 1) / T * g.p_tiles; }
+  __device__ __forceinline__ int64_t items() const { return table.first_unit(n_groups) * tiles(); }
+  __device__ __forceinline__ Item item(int64_t i) const {
+    Item t;
+    t.slot = i / tiles();
+    const int64_t tile = i % tiles();
+    t.group = table.group_of(t.slot, n_groups);
+    const int64_t first = table.first_unit(t.group);
+    t.q0 = tile / g.p_tiles * T;
+    t.q_end = g.nq;
+    t.p0 = tile % g.p_tiles * T;
+    t.k0 = table.first_row(t.group) + (t.slot - first) * g.k_split;
+    const int64_t end = table.first_row(t.group + 1);
+    t.k_end = t.k0 + g.k_split < end ? t.k0 + g.k_split : end;
+    t.p_shift = 0;
+    t.direct = table.first_unit(t.group + 1) - first == 1;
+    return t;
+  }
+};
+
+struct GroupedWeightGrad {
+  float *gw, *gb, *gw_parts, *gb_parts;
+  __device__ __forceinline__ void finish(const Item& t, int64_t np, int64_t nq, int64_t q, int64_t p, float4 c) const {
+    float* at = t.direct ? gw + t.group * nq * np : gw_parts + t.slot * nq * np;
+    *reinterpret_cast<float4*>(at + q * np + p) = c;
+  }
+  __device__ __forceinline__ float* bias(const Item& t, int64_t nq, int64_t q) const {
+    return (t.direct ? gb + t.group * nq : gb_parts + t.slot * nq) + q;
+  }
+};
+
+template <int W, bool kPT, class Out>
+__global__ __launch_bounds__(kThreads, 2) void rows_kernel(Product g, Out out, const int64_t* offsets, int32_t n_groups, int64_t n) {
+  __shared__ __attribute__((aligned(16))) Lds<W> lds;
+  __shared__ GroupTable table;
+  table.build(offsets, n_groups, n, 64 * W);
+  product<W, kPT, false>(g, out, GroupedRows<64 * W>{g, table, n_groups}, lds, blockIdx.x, gridDim.x);
+}
+
+template <int W>
+__global__ __launch_bounds__(kThreads, 2) void sums_kernel(Product g, GroupedWeightGrad out, const int64_t* offsets, int32_t n_groups,
+                                                           int64_t n) {
+  __shared__ __attribute__((aligned(16))) Lds<W> lds;
+  __shared__ GroupTable table;
+  table.build(offsets, n_groups, n, g.k_split);
+  product<W, true, true>(g, out, GroupedSums<64 * W>{g, table, n_groups}, lds, blockIdx.x, gridDim.x);
+}
+
+// Group blockIdx.y's shares added in order, a quad of values a thread; zeros where it has none.
+__global__ __launch_bounds__(kThreads) void join_groups_kernel(int64_t n, int32_t n_groups, const int64_t* offsets, int64_t k_split,
+                                                               const float* gw_parts, float* gw, int64_t size,
+                                                               const float* gb_parts, float* gb, int32_t d_out) {
+  __shared__ GroupTable table;
+  table.build(offsets, n_groups, n, k_split);
+  const int group = blockIdx.y;
+  const int64_t first = table.unit[group], last = table.unit[group + 1];
+  if (last - first == 1) return;
+  const int64_t quads = size / 4, all = quads + d_out / 4;
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < all; i += (int64_t)gridDim.x * kThreads) {
+    const bool w = i < quads;
+    const float4* at = w ? reinterpret_cast<const float4*>(gw_parts) + i : reinterpret_cast<const float4*>(gb_parts) + (i - quads);
+    const int64_t step = w ? quads : d_out / 4;
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    int64_t j = first;
+    for (; j + 7 < last; j += 8) {
+      float4 a[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) a[u] = at[(j + u) * step];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s.x += a[u].x, s.y += a[u].y, s.z += a[u].z, s.w += a[u].w;
+    }
+    for (; j < last; ++j) {
+      const float4 a = at[j * step];
+      s.x += a.x, s.y += a.y, s.z += a.z, s.w += a.w;
+    }
+    float4* to = w ? reinterpret_cast<float4*>(gw) + group * quads + i : reinterpret_cast<float4*>(gb) + group * step + (i - quads);
+    *to = s;
+  }
+}
+
+// 128 x 128 tiles where there are two rounds of them, else 64 x 64, as a layer of one group.
+bool wide(int64_t np, int64_t n) { return np > 64 && cdiv(np, 128) * (n / 128) >= 2 * kCus; }
+
+template <int W, bool kPT, class Out>
+void launch_rows(Product g, const Out& out, const int64_t* offsets, int32_t n_groups, int64_t n, hipStream_t stream) {
+  g.p_tiles = cdiv(g.np, 64 * W);
+  const int64_t most = (n / (64 * W) + n_groups) * g.p_tiles;
+  rows_kernel<W, kPT><<<(unsigned)(most < 65536 ? most : 65536), kThreads, 0, stream>>>(g, out, offsets, n_groups, n);
+}
+
+template <int W>
+void launch_sums(Product g, const GroupedWeightGrad& out, const int64_t* offsets, int32_t n_groups, int64_t n, hipStream_t stream) {
+  g.p_tiles = cdiv(g.np, 64 * W);
+  const int64_t most = (n / g.k_split + n_groups) * g.p_tiles * cdiv(g.nq, 64 * W);
+  sums_kernel<W><<<(unsigned)(most < 65536 ? most : 65536), kThreads, 0, stream>>>(g, out, offsets, n_groups, n);
+}
+
+struct Cut {
+  bool wide;
+  int64_t k_split, most;             // rows of a share, and the most shares
+};
+Cut cut_of(int64_t n, int64_t n_groups, int64_t d_in, int64_t d_out) {
+  Cut c;
+  const int64_t large = 4 * cdiv(d_in, 128) * cdiv(d_out, 128), small = cdiv(d_in, 64) * cdiv(d_out, 64);
+  c.wide = d_in > 64 && d_out > 64 && n >= 32768 && 5 * large <= 6 * small;
+  const int64_t t = c.wide ? 128 : 64, tiles = cdiv(d_in, t) * cdiv(d_out, t);
+  int64_t splits = 2 * kCus / tiles;
+  if (splits > cdiv(n, 256)) splits = cdiv(n, 256);
+  if (splits < 1) splits = 1;
+  c.k_split = cdiv(cdiv(n, splits), kDepth) * kDepth;
+  c.most = n / c.k_split + n_groups;
+  return c;
+}
+
+}  // namespace
+
+maestro_status launch_layer_grouped_f32(int64_t n, int32_t n_groups, int32_t d_in, int32_t d_out, const float* x,
+                                        const float* weight, const float* bias, const int64_t* offsets, bool relu, float* y,
+                                        hipStream_t stream) {
+  const Product g{{weight, d_in}, {x, d_in}, d_out, n, d_in, d_in, 1, 0, 0};
+  const Forward out{bias, y, relu};
+  if (wide(d_out, n) && d_in >= 192 && cdiv(d_out, 64) % 2 == 0) launch_rows<2, false>(g, out, offsets, n_groups, n, stream);
+  else launch_rows<1, false>(g, out, offsets, n_groups, n, stream);
+  return launch_status();
+}
+
+size_t grouped_grad_f32_workspace_bytes(int64_t n, int32_t n_groups, int32_t d_in, int32_t d_out) {
+  if (n == 0) return 0;
+  return sizeof(float) * (size_t)(cut_of(n, n_groups, d_in, d_out).most * ((int64_t)d_in + 1) * d_out);
+}
+
+maestro_status launch_grouped_grad_f32(int64_t n, int32_t n_groups, int32_t d_in, int32_t d_out, const float* x,
+                                       const float* weight, const float* g_z, const int64_t* offsets, bool relu_input,
+                                       float* g_x, float* g_weight, float* g_bias, void* workspace, hipStream_t stream) {
+  const int64_t size = (int64_t)d_in * d_out;
+  if (n == 0) return launch_join_groups(0, n_groups, offsets, 1, nullptr, g_weight, size, nullptr, g_bias, d_out, stream);
+  const Cut c = cut_of(n, n_groups, d_in, d_out);
+  float *gw_parts = static_cast<float*>(workspace), *gb_parts = gw_parts + c.most * size;
+  if (g_x) {
+    const Product gx{{weight, d_in}, {g_z, d_out}, d_in, n, d_out, d_out, 1, 0, 0};
+    const InputGrad out{x, g_x, relu_input};
+    if (wide(d_in, n)) launch_rows<2, true>(gx, out, offsets, n_groups, n, stream);
+    else launch_rows<1, true>(gx, out, offsets, n_groups, n, stream);
+  }
+  const Product gw{{x, d_in}, {g_z, d_out}, d_in, d_out, n, c.k_split, 1, 0, 0};
+  const GroupedWeightGrad out{g_weight, g_bias, gw_parts, gb_parts};
+  if (c.wide) launch_sums<2>(gw, out, offsets, n_groups, n, stream);
+  else launch_sums<1>(gw, out, offsets, n_groups, n, stream);
+  const maestro_status st = launch_status();
+  if (st != MAESTRO_OK) return st;
+  return launch_join_groups(n, n_groups, offsets, c.k_split, gw_parts, g_weight, size, gb_parts, g_bias, d_out, stream);
+}
+
+maestro_status launch_join_groups(int64_t n, int32_t n_groups, const int64_t* offsets, int64_t k_split, const float* gw_parts,
+                                  float* gw, int64_t size, const float* gb_parts, float* gb, int32_t d_out, hipStream_t stream) {
+  const int64_t blocks = cdiv(size / 4 + d_out / 4, kThreads);
+  join_groups_kernel<<<dim3((unsigned)(blocks < 4096 ? blocks : 4096), (unsigned)n_groups), kThreads, 0, stream>>>(
+      n, n_groups, offsets, k_split, gw_parts, gw, size, gb_parts, gb, d_out);
+  return launch_status();
+}
+
+}  // namespace maestro
