@@ -37,12 +37,12 @@ class Packed(NamedTuple):
     exponents: torch.Tensor
 
 
-_lib = None
+_lib = _tensors = None
 
 
 def load():
-    """libmaestro.so with the argument types of these operators set."""
-    global _lib
+    """libmaestro.so with the argument types of these operators set, and the native module given its entry points."""
+    global _lib, _tensors
     if _lib is not None:
         return _lib
     lib = _train.load()
@@ -58,8 +58,33 @@ def load():
     lib.maestro_layer_grad_packed.argtypes = [i64, i32, i32, i32, P, P, i32, P, P, i32, P, P, P, P, sz, P]
     for f in EXPORTS:
         getattr(lib, f).restype = sz if f.endswith("_workspace") else ctypes.c_int
+    module = _train._tensors
+    module.bind_layers(*(ctypes.cast(getattr(lib, f), P).value for f in EXPORTS))      # in the order of its LayerEntries
+    _tensors = module
     _lib = lib
     return lib
+
+
+# As in ``_train``, a call goes to the native module first where outputs, workspace and stream are the binding's to choose, and is
+# checked and made here only where that takes no part in it (None).
+
+
+def _here():
+    """The current device's number."""
+    get = getattr(torch._C, "_cuda_getDevice", None)
+    return get() if get else torch.cuda.current_device()
+
+
+def _current(**tensors: Optional[torch.Tensor]) -> None:
+    """Raise unless all are on the current device, where the kernels are launched."""
+    here = _here()
+    for name, t in tensors.items():
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"{name} must be on the current device ({here}), is on {t.device}")
+
+
+def _named(out: LayerGrad) -> dict:
+    return {"out.x": out.x, "out.weight": out.weight, "out.bias": out.bias}
 
 
 def _code(dtype, name: str) -> int:
@@ -109,12 +134,17 @@ def layer_grouped(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor, off
     [groups][d_out][d_in] (float32 or bfloat16) and ``bias`` [groups][d_out] (float32); ``offsets`` int64 [groups + 1] on
     the device. Rows of no group are left as they are in ``out`` (without one they hold whatever the memory held)."""
     lib = load()
+    if out is None and stream is None:
+        got = _tensors.layer_grouped(x, weight, bias, offsets, relu, _stream(None), _here())
+        if got is not None:
+            return got
     dt, n, groups, i, o = _grouped_shapes(x, weight, offsets)
     _shape(_dev(bias, "bias", torch.float32), "bias", (groups, o))
     if out is None:
         out, = _empties(stream, x, ((n, o), 2))
     else:
         _shape(_dev(out, "out", weight.dtype), "out", (n, o))
+    _current(x=x, weight=weight, bias=bias, offsets=offsets, out=out)
     st = lib.maestro_layer_grouped(n, groups, i, o, dt, _ptr(x), _ptr(weight), _ptr(bias), _ptr(offsets), int(bool(relu)),
                                    _ptr(out), _stream(stream))
     _check("maestro_layer_grouped", st)
@@ -142,9 +172,14 @@ def layer_grouped_grad(x: torch.Tensor, weight: torch.Tensor, g_z: torch.Tensor,
     weights [groups][d_out][d_in] and biases [groups][d_out] in float32 (zeros for empty groups), and with ``want_x`` the
     input's. Rows of no group take no part, and theirs of ``out.x`` are left as they are."""
     lib = load()
+    if out is None and workspace is None and stream is None:
+        got = _tensors.layer_grouped_grad(x, weight, g_z, offsets, relu_input, want_x, _stream(None), _here())
+        if got is not None:
+            return LayerGrad._make(got)
     dt, n, groups, i, o = _grouped_shapes(x, weight, offsets)
     _shape(_dev(g_z, "g_z", weight.dtype), "g_z", (n, o))
     out = _grad_outputs(out, want_x, stream, x, weight.dtype, n, i, (groups, o, i), (groups, o))
+    _current(x=x, weight=weight, g_z=g_z, offsets=offsets, workspace=workspace, **_named(out))
     need = lib.maestro_layer_grouped_grad_workspace(n, groups, i, o, dt)
     _workspace(workspace)
     if workspace is None and need:
@@ -160,12 +195,17 @@ def quantize_rows(x: torch.Tensor, out: Optional[Quantized] = None, stream=None)
     """maestro_quantize_rows: rows of ``x`` [n][d] (float32 or bfloat16) as signed bytes with a scale each, the largest
     magnitude over 127. Weights [d_out][d_in] so quantised have a scale for each output channel."""
     lib = load()
+    if out is None and stream is None:
+        got = _tensors.quantize_rows(x, _stream(None), _here())
+        if got is not None:
+            return Quantized._make(got)
     n, d = _matrix(x, "x", torch.float32, torch.bfloat16)
     if out is None:
         out = Quantized._make(_new(stream, x.device, ((n, d), torch.int8), ((n,), torch.float32)))
     else:
         _shape(_dev(out.codes, "out.codes", torch.int8), "out.codes", (n, d))
         _shape(_dev(out.scale, "out.scale", torch.float32), "out.scale", (n,))
+    _current(x=x, codes=out.codes, scale=out.scale)
     st = lib.maestro_quantize_rows(n, d, _DTYPE[x.dtype], _ptr(x), _ptr(out.codes), _ptr(out.scale), _stream(stream))
     _check("maestro_quantize_rows", st)
     return out
@@ -177,6 +217,10 @@ def layer_int8(x: Quantized, weight: Quantized, bias: torch.Tensor, relu: bool =
     with ``relu``, in ``dtype`` (float32 or bfloat16; bias float32). Products are summed in whole numbers."""
     lib = load()
     dt = _code(dtype, "dtype")
+    if out is None and stream is None:
+        got = _tensors.layer_int8(x.codes, x.scale, weight.codes, weight.scale, bias, relu, dt, _stream(None), _here())
+        if got is not None:
+            return got
     n, i = _matrix(x.codes, "x.codes", torch.int8)
     o, columns = _matrix(weight.codes, "weight.codes", torch.int8)
     if columns != i:
@@ -190,6 +234,7 @@ def layer_int8(x: Quantized, weight: Quantized, bias: torch.Tensor, relu: bool =
         out, = _new(stream, x.codes.device, ((n, o), dtype))
     else:
         _shape(_dev(out, "out", dtype), "out", (n, o))
+    _current(x=x.codes, x_scale=x.scale, weight=weight.codes, weight_scale=weight.scale, bias=bias, out=out)
     st = lib.maestro_layer_int8(n, i, o, _ptr(x.codes), _ptr(x.scale), _ptr(weight.codes), _ptr(weight.scale), _ptr(bias),
                                 int(bool(relu)), dt, _ptr(out), _stream(stream))
     _check("maestro_layer_int8", st)
@@ -207,12 +252,17 @@ def pack_activations(x: torch.Tensor, rectified: bool = False, out: Optional[Pac
     """maestro_pack_activations: ``x`` [n][d] (float32 or bfloat16) in 8 bits, 32 values of a row to a power of two;
     ``rectified``: unsigned codes, 0 where x is not positive and at least 1 where it is."""
     lib = load()
+    if out is None and stream is None:
+        got = _tensors.pack(x, rectified, _stream(None), _here())
+        if got is not None:
+            return Packed._make(got)
     n, d = _matrix(x, "x", torch.float32, torch.bfloat16)
     if out is None:
         out = Packed._make(_new(stream, x.device, ((n, d), torch.uint8 if rectified else torch.int8),
                                 ((n, -(-d // BLOCK)), torch.uint8)))
     elif _packed_shapes(out) != (n, d, int(bool(rectified))):
         raise ValueError("out must have x's shape, and uint8 codes with rectified, int8 ones without")
+    _current(x=x, codes=out.codes, exponents=out.exponents)
     st = lib.maestro_pack_activations(n, d, _DTYPE[x.dtype], _ptr(x), int(bool(rectified)), _ptr(out.codes), _ptr(out.exponents),
                                       _stream(stream))
     _check("maestro_pack_activations", st)
@@ -224,11 +274,16 @@ def unpack_activations(packed: Packed, dtype: torch.dtype = torch.bfloat16, out:
     """maestro_unpack_activations: the values of a checkpoint in ``dtype`` (float32 or bfloat16), exactly."""
     lib = load()
     dt = _code(dtype, "dtype")
+    if out is None and stream is None:
+        got = _tensors.unpack(packed.codes, packed.exponents, dt, _stream(None), _here())
+        if got is not None:
+            return got
     n, d, rectified = _packed_shapes(packed)
     if out is None:
         out, = _new(stream, packed.codes.device, ((n, d), dtype))
     else:
         _shape(_dev(out, "out", dtype), "out", (n, d))
+    _current(codes=packed.codes, exponents=packed.exponents, out=out)
     st = lib.maestro_unpack_activations(n, d, dt, _ptr(packed.codes), _ptr(packed.exponents), rectified, _ptr(out), _stream(stream))
     _check("maestro_unpack_activations", st)
     return out
@@ -239,6 +294,10 @@ def layer_grad_packed(packed: Packed, weight: torch.Tensor, g_z: torch.Tensor, r
     """maestro_layer_grad_packed: ``layer_grad`` of an input kept as ``packed``: the gradients for the values that
     ``unpack_activations`` gives. ``relu_input`` needs rectified (uint8) codes."""
     lib = load()
+    if out is None and workspace is None and stream is None:
+        got = _tensors.layer_grad_packed(packed.codes, packed.exponents, weight, g_z, relu_input, want_x, _stream(None), _here())
+        if got is not None:
+            return LayerGrad._make(got)
     n, i, rectified = _packed_shapes(packed)
     if not isinstance(weight, _Tensor):
         raise TypeError("weight must be a float32 or bfloat16 tensor")
@@ -253,6 +312,7 @@ def layer_grad_packed(packed: Packed, weight: torch.Tensor, g_z: torch.Tensor, r
         raise ValueError("relu_input needs rectified codes (uint8)")
     _shape(_dev(g_z, "g_z", weight.dtype), "g_z", (n, o))
     out = _grad_outputs(out, want_x, stream, g_z, weight.dtype, n, i, (o, i), (o,))
+    _current(codes=packed.codes, exponents=packed.exponents, weight=weight, g_z=g_z, workspace=workspace, **_named(out))
     need = lib.maestro_layer_grad_packed_workspace(n, i, o, dt)
     _workspace(workspace)
     if workspace is None and need:

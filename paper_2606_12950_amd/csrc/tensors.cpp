@@ -14,7 +14,7 @@
 #include <cstring>
 #include <vector>
 
-#include "maestro_train.h"
+#include "maestro_layers.h"
 
 namespace {
 
@@ -308,11 +308,232 @@ PyObject* clip(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   END_HANDLE_TH_ERRORS
 }
 
+// --- layers by role, in 8-bit integers and from checkpoints -----------------------------------------------
+
+struct LayerEntries {
+  decltype(&maestro_layer_grouped) grouped;
+  decltype(&maestro_layer_grouped_grad_workspace) grouped_grad_workspace;
+  decltype(&maestro_layer_grouped_grad) grouped_grad;
+  decltype(&maestro_quantize_rows) quantize;
+  decltype(&maestro_layer_int8) int8;
+  decltype(&maestro_pack_activations) pack;
+  decltype(&maestro_unpack_activations) unpack;
+  decltype(&maestro_layer_grad_packed_workspace) packed_grad_workspace;
+  decltype(&maestro_layer_grad_packed) packed_grad;
+} layer_entries;
+
+// bind_layers(layer_grouped, ...): the addresses in the order of LayerEntries, after bind
+PyObject* bind_layers(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  void* at[9];
+  static_assert(sizeof(at) == sizeof(layer_entries), "one address an entry point");
+  if (n != 9) return PyErr_Format(PyExc_TypeError, "nine addresses are needed");
+  for (int i = 0; i < 9; ++i) at[i] = PyLong_AsVoidPtr(args[i]);
+  if (PyErr_Occurred()) return nullptr;
+  memcpy(&layer_entries, at, sizeof(at));
+  Py_RETURN_NONE;
+}
+
+// The last two arguments of a call: the stream's handle and the current device's number.
+struct Where {
+  void* stream;
+  long device;
+  Where(PyObject* s, PyObject* d) : stream(PyLong_AsVoidPtr(s)), device(PyLong_AsLong(d)) {}
+  template <class... T>
+  bool has(const T*... t) const {
+    return ((t->device().index() == device) && ...);
+  }
+};
+
+bool matrix(const at::Tensor* t) {
+  return strided(t) && t->dim() == 2 && t->size(1) >= 1 && t->size(1) <= INT32_MAX && t->is_contiguous();
+}
+float* floats(const at::Tensor* t) { return static_cast<float*>(at_of(t)); }
+
+// x [n][d_in], weight [groups][d_out][d_in] of one type, offsets [groups + 1]
+bool grouped_shapes(const at::Tensor* x, const at::Tensor* w, const at::Tensor* off) {
+  if (!matrix(x) || !strided(w) || w->dim() != 3 || code_of(*w) < 0 || !w->is_contiguous()) return false;
+  return x->scalar_type() == w->scalar_type() && x->size(1) == w->size(2) && w->size(0) <= INT32_MAX && w->size(1) <= INT32_MAX &&
+         is(off, at::kLong, {w->size(0) + 1});
+}
+
+// layer_grouped(x, weight, bias, offsets, relu, stream, device)
+PyObject* layer_grouped(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 7) return PyErr_Format(PyExc_TypeError, "seven arguments are needed");
+  HANDLE_TH_ERRORS
+  const at::Tensor *x = tensor(a[0]), *w = tensor(a[1]), *b = tensor(a[2]), *off = tensor(a[3]);
+  if (!grouped_shapes(x, w, off) || !is(b, at::kFloat, {w->size(0), w->size(1)})) Py_RETURN_NONE;
+  const int relu = PyObject_IsTrue(a[4]);
+  const Where where(a[5], a[6]);
+  if (PyErr_Occurred()) return nullptr;
+  if (!where.has(x, w, b, off)) Py_RETURN_NONE;
+  const int64_t n = x->size(0);
+  const int32_t groups = w->size(0), o = w->size(1), i = w->size(2), code = code_of(*w);
+  const at::Tensor y = fresh(*x, x->scalar_type(), {n, o});
+  void *xp = at_of(x), *wp = at_of(w), *yp = at_of(&y);
+  const float* bp = floats(b);
+  const int64_t* offp = static_cast<int64_t*>(at_of(off));
+  const maestro_status st = unlocked([&] { return layer_entries.grouped(n, groups, i, o, code, xp, wp, bp, offp, relu, yp, where.stream); });
+  if (st != MAESTRO_OK) return refused("maestro_layer_grouped", st);
+  return wrap(y);
+  END_HANDLE_TH_ERRORS
+}
+
+// layer_grouped_grad(x, weight, g_z, offsets, relu_input, want_x, stream, device) -> (g_x or None, g_weight, g_bias)
+PyObject* layer_grouped_grad(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 8) return PyErr_Format(PyExc_TypeError, "eight arguments are needed");
+  HANDLE_TH_ERRORS
+  const at::Tensor *x = tensor(a[0]), *w = tensor(a[1]), *gz = tensor(a[2]), *off = tensor(a[3]);
+  if (!grouped_shapes(x, w, off) || !is(gz, w->scalar_type(), {x->size(0), w->size(1)})) Py_RETURN_NONE;
+  const int relu = PyObject_IsTrue(a[4]), want_x = PyObject_IsTrue(a[5]);
+  const Where where(a[6], a[7]);
+  if (PyErr_Occurred()) return nullptr;
+  if (!where.has(x, w, gz, off)) Py_RETURN_NONE;
+  const int64_t n = x->size(0);
+  const int32_t groups = w->size(0), o = w->size(1), i = w->size(2), code = code_of(*w);
+  const at::Tensor gx = want_x ? fresh(*x, x->scalar_type(), {n, i}) : at::Tensor(), gw = fresh(*x, at::kFloat, {groups, o, i}),
+                   gb = fresh(*x, at::kFloat, {groups, o});
+  const size_t need = layer_entries.grouped_grad_workspace(n, groups, i, o, code);
+  const at::Tensor work = scratch(*x, need);
+  void *xp = at_of(x), *wp = at_of(w), *gp = at_of(gz), *gxp = at_of(&gx), *workp = at_of(&work);
+  float *gwp = floats(&gw), *gbp = floats(&gb);
+  const int64_t* offp = static_cast<int64_t*>(at_of(off));
+  const maestro_status st = unlocked([&] {
+    return layer_entries.grouped_grad(n, groups, i, o, code, xp, wp, gp, offp, relu, gxp, gwp, gbp, workp, need, where.stream);
+  });
+  if (st != MAESTRO_OK) return refused("maestro_layer_grouped_grad", st);
+  return Py_BuildValue("NNN", wrap(gx), wrap(gw), wrap(gb));
+  END_HANDLE_TH_ERRORS
+}
+
+// quantize_rows(x, stream, device) -> (codes, scale)
+PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 3) return PyErr_Format(PyExc_TypeError, "three arguments are needed");
+  HANDLE_TH_ERRORS
+  const at::Tensor* x = tensor(a[0]);
+  if (!matrix(x) || code_of(*x) < 0) Py_RETURN_NONE;
+  const Where where(a[1], a[2]);
+  if (PyErr_Occurred()) return nullptr;
+  if (!where.has(x)) Py_RETURN_NONE;
+  const int64_t n = x->size(0);
+  const int32_t d = x->size(1);
+  const at::Tensor codes = fresh(*x, at::kChar, {n, d}), scale = fresh(*x, at::kFloat, {n});
+  void* xp = at_of(x);
+  int8_t* cp = static_cast<int8_t*>(at_of(&codes));
+  float* sp = floats(&scale);
+  const maestro_status st = unlocked([&] { return layer_entries.quantize(n, d, code_of(*x), xp, cp, sp, where.stream); });
+  if (st != MAESTRO_OK) return refused("maestro_quantize_rows", st);
+  return Py_BuildValue("NN", wrap(codes), wrap(scale));
+  END_HANDLE_TH_ERRORS
+}
+
+// layer_int8(x codes, x scale, weight codes, weight scale, bias, relu, maestro_dtype, stream, device)
+PyObject* layer_int8(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 9) return PyErr_Format(PyExc_TypeError, "nine arguments are needed");
+  HANDLE_TH_ERRORS
+  const at::Tensor *x = tensor(a[0]), *xs = tensor(a[1]), *w = tensor(a[2]), *ws = tensor(a[3]), *b = tensor(a[4]);
+  if (!matrix(x) || !matrix(w) || x->scalar_type() != at::kChar || w->scalar_type() != at::kChar || x->size(1) != w->size(1)) Py_RETURN_NONE;
+  const int64_t n = x->size(0);
+  if (w->size(0) > INT32_MAX || !is(xs, at::kFloat, {n}) || !is(ws, at::kFloat, {w->size(0)}) || !is(b, at::kFloat, {w->size(0)}))
+    Py_RETURN_NONE;
+  const int relu = PyObject_IsTrue(a[5]);
+  const long code = PyLong_AsLong(a[6]);
+  const Where where(a[7], a[8]);
+  if (PyErr_Occurred()) return nullptr;
+  if (!where.has(x, xs, w, ws, b) || (code != kF32 && code != kBf16)) Py_RETURN_NONE;
+  const int32_t o = w->size(0), i = w->size(1);
+  const at::Tensor y = fresh(*x, code == kF32 ? at::kFloat : at::kBFloat16, {n, o});
+  const int8_t *xp = static_cast<int8_t*>(at_of(x)), *wp = static_cast<int8_t*>(at_of(w));
+  const float *xsp = floats(xs), *wsp = floats(ws), *bp = floats(b);
+  void* yp = at_of(&y);
+  const maestro_status st = unlocked([&] { return layer_entries.int8(n, i, o, xp, xsp, wp, wsp, bp, relu, code, yp, where.stream); });
+  if (st != MAESTRO_OK) return refused("maestro_layer_int8", st);
+  return wrap(y);
+  END_HANDLE_TH_ERRORS
+}
+
+// pack(x, rectified, stream, device) -> (codes, exponents)
+PyObject* pack(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 4) return PyErr_Format(PyExc_TypeError, "four arguments are needed");
+  HANDLE_TH_ERRORS
+  const at::Tensor* x = tensor(a[0]);
+  if (!matrix(x) || code_of(*x) < 0) Py_RETURN_NONE;
+  const int rectified = PyObject_IsTrue(a[1]);
+  const Where where(a[2], a[3]);
+  if (PyErr_Occurred()) return nullptr;
+  if (!where.has(x)) Py_RETURN_NONE;
+  const int64_t n = x->size(0), blocks = (x->size(1) + 31) / 32;
+  const int32_t d = x->size(1);
+  const at::Tensor codes = fresh(*x, rectified ? at::kByte : at::kChar, {n, d}), exponents = fresh(*x, at::kByte, {n, blocks});
+  void *xp = at_of(x), *cp = at_of(&codes);
+  uint8_t* ep = static_cast<uint8_t*>(at_of(&exponents));
+  const maestro_status st = unlocked([&] { return layer_entries.pack(n, d, code_of(*x), xp, rectified, cp, ep, where.stream); });
+  if (st != MAESTRO_OK) return refused("maestro_pack_activations", st);
+  return Py_BuildValue("NN", wrap(codes), wrap(exponents));
+  END_HANDLE_TH_ERRORS
+}
+
+// codes [n][d], bytes, signed or not, and exponents [n][ceil(d / 32)]
+bool packed_shapes(const at::Tensor* c, const at::Tensor* e) {
+  if (!matrix(c) || (c->scalar_type() != at::kChar && c->scalar_type() != at::kByte)) return false;
+  return is(e, at::kByte, {c->size(0), (c->size(1) + 31) / 32});
+}
+
+// unpack(codes, exponents, maestro_dtype, stream, device)
+PyObject* unpack(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 5) return PyErr_Format(PyExc_TypeError, "five arguments are needed");
+  HANDLE_TH_ERRORS
+  const at::Tensor *c = tensor(a[0]), *e = tensor(a[1]);
+  if (!packed_shapes(c, e)) Py_RETURN_NONE;
+  const long code = PyLong_AsLong(a[2]);
+  const Where where(a[3], a[4]);
+  if (PyErr_Occurred()) return nullptr;
+  if (!where.has(c, e) || (code != kF32 && code != kBf16)) Py_RETURN_NONE;
+  const int64_t n = c->size(0);
+  const int32_t d = c->size(1), rectified = c->scalar_type() == at::kByte;
+  const at::Tensor x = fresh(*c, code == kF32 ? at::kFloat : at::kBFloat16, {n, d});
+  void *cp = at_of(c), *xp = at_of(&x);
+  const uint8_t* ep = static_cast<uint8_t*>(at_of(e));
+  const maestro_status st = unlocked([&] { return layer_entries.unpack(n, d, code, cp, ep, rectified, xp, where.stream); });
+  if (st != MAESTRO_OK) return refused("maestro_unpack_activations", st);
+  return wrap(x);
+  END_HANDLE_TH_ERRORS
+}
+
+// layer_grad_packed(codes, exponents, weight, g_z, relu_input, want_x, stream, device) -> (g_x or None, g_weight, g_bias)
+PyObject* layer_grad_packed(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 8) return PyErr_Format(PyExc_TypeError, "eight arguments are needed");
+  HANDLE_TH_ERRORS
+  const at::Tensor *c = tensor(a[0]), *e = tensor(a[1]), *w = tensor(a[2]), *gz = tensor(a[3]);
+  if (!packed_shapes(c, e) || !matrix(w) || code_of(*w) < 0 || w->size(1) != c->size(1) || w->size(0) > INT32_MAX) Py_RETURN_NONE;
+  const int64_t n = c->size(0);
+  const int32_t o = w->size(0), i = w->size(1), code = code_of(*w), rectified = c->scalar_type() == at::kByte;
+  if (!is(gz, w->scalar_type(), {n, o})) Py_RETURN_NONE;
+  const int relu = PyObject_IsTrue(a[4]), want_x = PyObject_IsTrue(a[5]);
+  const Where where(a[6], a[7]);
+  if (PyErr_Occurred()) return nullptr;
+  if (!where.has(c, e, w, gz)) Py_RETURN_NONE;
+  const at::Tensor gx = want_x ? fresh(*gz, w->scalar_type(), {n, i}) : at::Tensor(), gw = fresh(*gz, at::kFloat, {o, i}),
+                   gb = fresh(*gz, at::kFloat, {o});
+  const size_t need = layer_entries.packed_grad_workspace(n, i, o, code);
+  const at::Tensor work = scratch(*gz, need);
+  void *cp = at_of(c), *wp = at_of(w), *gp = at_of(gz), *gxp = at_of(&gx), *workp = at_of(&work);
+  const uint8_t* ep = static_cast<uint8_t*>(at_of(e));
+  float *gwp = floats(&gw), *gbp = floats(&gb);
+  const maestro_status st = unlocked([&] {
+    return layer_entries.packed_grad(n, i, o, code, cp, ep, rectified, wp, gp, relu, gxp, gwp, gbp, workp, need, where.stream);
+  });
+  if (st != MAESTRO_OK) return refused("maestro_layer_grad_packed", st);
+  return Py_BuildValue("NNN", wrap(gx), wrap(gw), wrap(gb));
+  END_HANDLE_TH_ERRORS
+}
+
 #define FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 
 PyMethodDef methods[] = {
     {"table", table, METH_VARARGS, "addresses, sizes and dtype codes of contiguous float32 or bfloat16 tensors on a GPU"},
     FAST(empties), FAST(bind), FAST(layer), FAST(layer_grad), FAST(logprobs), FAST(logprobs_grad), FAST(clip),
+    FAST(bind_layers), FAST(layer_grouped), FAST(layer_grouped_grad), FAST(quantize_rows), FAST(layer_int8), FAST(pack), FAST(unpack),
+    FAST(layer_grad_packed),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
