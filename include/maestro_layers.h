@@ -35,7 +35,8 @@ extern "C" {
  * x [n][d_in], weight [n_groups][d_out][d_in] and y [n][d_out] in `dtype`, bias [n_groups][d_out] float32, offsets
  * [n_groups + 1] int64 (DEVICE, aligned to 8). Sums and rounding as maestro_layer. Groups may be empty. Rows of no group
  * (before offsets[0], from offsets[n_groups] on) are not read, and theirs of y are left as they are. An offset below an
- * earlier one counts as that one, one outside 0 .. n as the nearer bound. */
+ * earlier one counts as that one, one outside 0 .. n as the nearer bound. n is below 2^31 - 2^16, and n * d_in and n * d_out
+ * below about 2^43 (MAESTRO_ERR_UNSUPPORTED otherwise). */
 MAESTRO_API maestro_status maestro_layer_grouped(int64_t n, int32_t n_groups, int32_t d_in, int32_t d_out, int32_t dtype,
                              const void* x, const void* weight, const float* bias, const int64_t* offsets, int32_t relu,
                              void* y, void* stream);
@@ -58,8 +59,8 @@ MAESTRO_API maestro_status maestro_quantize_rows(int64_t n, int32_t d, int32_t d
 
 /* y [n][d_out] = x * weight^T + bias for x [n][d_in] and weight [d_out][d_in] in codes, x_scale [n] (aligned to 4) and
  * weight_scale [d_out] float32, then max(., 0) where relu is not 0; y in `dtype`, bias [d_out] float32. The products
- * are summed in 32-bit integers, exactly (codes -128 are valid); then in float32, in this order,
- * (sum * x_scale) * weight_scale + bias, rounded once to `dtype`. */
+ * are summed in 32-bit integers, exactly (codes -128 are valid); then in float32 fma(sum * x_scale, weight_scale, bias), the
+ * sum and its product with x_scale rounded to float32, rounded once to `dtype`. */
 MAESTRO_API maestro_status maestro_layer_int8(int64_t n, int32_t d_in, int32_t d_out, const int8_t* x, const float* x_scale,
                              const int8_t* weight, const float* weight_scale, const float* bias, int32_t relu, int32_t dtype,
                              void* y, void* stream);

@@ -10,54 +10,46 @@
 namespace maestro {
 namespace {
 
-// Tiles of TQ rows of a group (q), all p tiles of one after the other.
 template <int TP, int TQ, int kDepth>
-struct GroupedRows {
+struct GroupedRows : GroupedRowsWay<8> {
   const Product& g;
-  const GroupTable& table;
-  int32_t n_groups;
-  __device__ __forceinline__ int64_t items() const { return table.first_unit(n_groups) * g.p_tiles; }
-  __device__ __forceinline__ Item item(int64_t i) const {
+  __device__ __forceinline__ Item item(const Way& c) const {
+    const Place at = place(c, TQ);
     Item t;
-    const int64_t unit = i / g.p_tiles;
-    t.group = table.group_of(unit, n_groups);
-    t.p = g.p + t.group * (g.np * g.nk);
+    t.group = at.group;
+    t.p = g.p + at.group * (g.np * g.nk);
     t.q = g.q;
-    t.q0 = table.first_row(t.group) + (unit - table.first_unit(t.group)) * TQ;
-    t.q_end = table.first_row(t.group + 1);
-    t.p0 = i % g.p_tiles * TP;
+    t.q0 = at.q0;
+    t.q_end = at.q_end;
+    t.p0 = at.p_tile * TP;
     t.k0 = 0;
     t.kn = g.nk;
     t.stages = (g.nk + kDepth - 1) / kDepth;
     t.slot = 0;
-    t.whole = true;
+    t.whole = t.direct = true;
     return t;
   }
 };
 
-// Tiles of a group's weights' gradient over one of its shares of rows (k).
 template <int TP, int TQ, int kDepth>
-struct GroupedSums {
+struct GroupedSums : GroupedSumsWay<8> {
   const Product& g;
-  const GroupTable& table;
-  int32_t n_groups;
-  __device__ __forceinline__ int64_t tiles() const { return (g.nq + TQ - 1) / TQ * g.p_tiles; }
-  __device__ __forceinline__ int64_t items() const { return table.first_unit(n_groups) * tiles(); }
-  __device__ __forceinline__ Item item(int64_t i) const {
+  __device__ __forceinline__ Item item(const Way& c) const {
+    const Place at = place(c);
+    const int q_tile = quotient(at.tile, g.p_tiles);
     Item t;
-    t.slot = i / tiles();
-    const int64_t tile = i % tiles();
-    t.group = table.group_of(t.slot, n_groups);
+    t.group = at.group;
     t.p = g.p;
     t.q = g.q;
-    t.q0 = tile / g.p_tiles * TQ;
+    t.q0 = q_tile * TQ;
     t.q_end = g.nq;
-    t.p0 = tile % g.p_tiles * TP;
-    t.k0 = table.first_row(t.group) + (t.slot - table.first_unit(t.group)) * g.k_split;
-    const int64_t left = table.first_row(t.group + 1) - t.k0;
-    t.kn = left < g.k_split ? left : g.k_split;
-    t.stages = (t.kn + kDepth - 1) / kDepth;
+    t.p0 = (at.tile - q_tile * g.p_tiles) * TP;
+    t.k0 = at.k0;
+    t.kn = at.k_end - at.k0;
+    t.stages = (at.k_end - at.k0 + kDepth - 1) / kDepth;
+    t.slot = at.slot;
     t.whole = true;
+    t.direct = at.direct;
     return t;
   }
 };
@@ -66,37 +58,33 @@ struct GroupedWeightGrad {
   static constexpr bool kBias = false, kInt8 = false;
   float *gw, *gb, *gw_parts, *gb_parts;
   int32_t parts;                     // 1
-  const GroupTable* table;
-  __device__ __forceinline__ bool direct(const Item& t) const {
-    return table->first_unit(t.group + 1) - table->first_unit(t.group) == 1;
-  }
   __device__ __forceinline__ float* weights(const Product& g, const Item& t) const {
-    return direct(t) ? gw + t.group * (g.nq * g.np) : gw_parts + t.slot * g.nq * g.np;
+    return t.direct ? gw + t.group * (g.nq * g.np) : gw_parts + t.slot * (g.nq * g.np);
   }
   __device__ __forceinline__ float* biases(const Product& g, const Item& t, int64_t, int) const {
-    return direct(t) ? gb + t.group * g.nq : gb_parts + t.slot * g.nq;
+    return t.direct ? gb + t.group * g.nq : gb_parts + t.slot * g.nq;
   }
 };
 
 template <int WP, int WQ, int kDepth, int kBufs, bool kPT, class Out>
 __global__ __launch_bounds__(kThreads, (Tile<WP, WQ, kDepth, kBufs, Out>::kResident)) void rows_kernel(
-    Product g, Out out, const int64_t* offsets, int32_t n_groups, int64_t n) {
+    Product g, Out out, const int64_t* offsets, int32_t n_groups, int32_t n) {
   using L = Tile<WP, WQ, kDepth, kBufs, Out>;
   __shared__ __attribute__((aligned(16))) unsigned char lds[L::kBytes];
   __shared__ GroupTable table;
-  table.build(offsets, n_groups, n, L::TQ);
-  product<WP, WQ, kDepth, kBufs, kPT, false>(g, out, GroupedRows<L::TP, L::TQ, kDepth>{g, table, n_groups}, lds, blockIdx.x, gridDim.x);
+  table.build<kTiles>(offsets, n_groups, n, L::TQ);
+  product<WP, WQ, kDepth, kBufs, kPT, false>(g, out, GroupedRows<L::TP, L::TQ, kDepth>{{table, n_groups, g.p_tiles}, g}, lds, blockIdx.x, gridDim.x);
 }
 
 template <int WP, int WQ, int kDepth, int kBufs>
 __global__ __launch_bounds__(kThreads, (Tile<WP, WQ, kDepth, kBufs, GroupedWeightGrad>::kResident)) void sums_kernel(
-    Product g, GroupedWeightGrad out, const int64_t* offsets, int32_t n_groups, int64_t n) {
+    Product g, GroupedWeightGrad out, const int64_t* offsets, int32_t n_groups, int32_t n) {
   using L = Tile<WP, WQ, kDepth, kBufs, GroupedWeightGrad>;
   __shared__ __attribute__((aligned(16))) unsigned char lds[L::kBytes];
   __shared__ GroupTable table;
-  table.build(offsets, n_groups, n, g.k_split);
-  out.table = &table;
-  product<WP, WQ, kDepth, kBufs, true, true>(g, out, GroupedSums<L::TP, L::TQ, kDepth>{g, table, n_groups}, lds, blockIdx.x, gridDim.x);
+  table.build<kShares>(offsets, n_groups, n, (int)g.k_split);
+  const int tiles = (int)((g.nq + L::TQ - 1) / L::TQ) * g.p_tiles;
+  product<WP, WQ, kDepth, kBufs, true, true>(g, out, GroupedSums<L::TP, L::TQ, kDepth>{{table, n_groups, tiles, (int)g.k_split}, g}, lds, blockIdx.x, gridDim.x);
 }
 
 uint32_t blocks_of(int64_t items, int64_t resident) {
@@ -109,7 +97,7 @@ void launch_tiles(Product g, const Out& out, const int64_t* offsets, int32_t n_g
   using L = Tile<W, W, 64, 2, Out>;
   g.p_tiles = (int32_t)cdiv(g.np, L::TP);
   const uint32_t blocks = blocks_of((n / L::TQ + n_groups) * g.p_tiles, L::kResident);
-  rows_kernel<W, W, 64, 2, kPT><<<blocks, kThreads, 0, stream>>>(g, out, offsets, n_groups, n);
+  rows_kernel<W, W, 64, 2, kPT><<<blocks, kThreads, 0, stream>>>(g, out, offsets, n_groups, (int32_t)n);
 }
 
 template <bool kPT, class Out>
@@ -123,8 +111,8 @@ template <int WP, int WQ, int kDepth, int kBufs>
 void launch_sums(Product g, const GroupedWeightGrad& out, const int64_t* offsets, int32_t n_groups, int64_t n, hipStream_t stream) {
   using L = Tile<WP, WQ, kDepth, kBufs, GroupedWeightGrad>;
   g.p_tiles = (int32_t)cdiv(g.np, L::TP);
-  const uint32_t blocks = blocks_of((n / g.k_split + n_groups) * g.p_tiles * cdiv(g.nq, L::TQ), L::kResident);
-  sums_kernel<WP, WQ, kDepth, kBufs><<<blocks, kThreads, 0, stream>>>(g, out, offsets, n_groups, n);
+  const uint32_t blocks = blocks_of(cdiv(n, g.k_split) * g.p_tiles * cdiv(g.nq, L::TQ), L::kResident);
+  sums_kernel<WP, WQ, kDepth, kBufs><<<blocks, kThreads, 0, stream>>>(g, out, offsets, n_groups, (int32_t)n);
 }
 
 // Tile of the weights' gradient and rows of a share, as for a layer of one group.
@@ -173,7 +161,7 @@ maestro_status launch_grouped_grad_bf16(int64_t n, int32_t n_groups, int32_t d_i
     launch_rows<true>(gx, InputGrad{xb, static_cast<__bf16*>(g_x), relu_input}, offsets, n_groups, n, stream);
   }
   const Product gw{xb, gz, d_in, d_out, d_in, d_out, n, c.k_split, 1, 0, 0};
-  const GroupedWeightGrad out{g_weight, g_bias, gw_parts, gb_parts, 1, nullptr};
+  const GroupedWeightGrad out{g_weight, g_bias, gw_parts, gb_parts, 1};
   if (c.tq == 256) launch_sums<4, 4, 32, 4>(gw, out, offsets, n_groups, n, stream);
   else if (c.tp == 256) launch_sums<4, 1, 64, 2>(gw, out, offsets, n_groups, n, stream);
   else launch_sums<2, 2, 64, 2>(gw, out, offsets, n_groups, n, stream);

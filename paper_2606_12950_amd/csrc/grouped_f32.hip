@@ -9,51 +9,41 @@
 namespace maestro {
 namespace {
 
-// Tiles of T rows of a group (q), all p tiles of one after the other.
 template <int T>
-struct GroupedRows {
+struct GroupedRows : GroupedRowsWay<1> {
   const Product& g;
-  const GroupTable& table;
-  int32_t n_groups;
-  __device__ __forceinline__ int64_t items() const { return table.first_unit(n_groups) * g.p_tiles; }
-  __device__ __forceinline__ Item item(int64_t i) const {
+  __device__ __forceinline__ Item item(const Way& c) const {
+    const Place at = place(c, T);
     Item t;
-    const int64_t unit = i / g.p_tiles;
-    t.group = table.group_of(unit, n_groups);
-    t.q0 = table.first_row(t.group) + (unit - table.first_unit(t.group)) * T;
-    t.q_end = table.first_row(t.group + 1);
-    t.p0 = i % g.p_tiles * T;
+    t.group = at.group;
+    t.p_shift = at.group * (g.np * g.nk);
+    t.q0 = at.q0;
+    t.q_end = at.q_end;
+    t.p0 = at.p_tile * T;
     t.k0 = 0;
     t.k_end = g.nk;
     t.slot = 0;
-    t.p_shift = t.group * (g.np * g.nk);
     t.direct = true;
     return t;
   }
 };
 
-// Tiles of a group's weights' gradient over one of its shares of rows (k).
 template <int T>
-struct GroupedSums {
+struct GroupedSums : GroupedSumsWay<1> {
   const Product& g;
-  const GroupTable& table;
-  int32_t n_groups;
-  __device__ __forceinline__ int64_t tiles() const { return (g.nq + T - 1) / T * g.p_tiles; }
-  __device__ __forceinline__ int64_t items() const { return table.first_unit(n_groups) * tiles(); }
-  __device__ __forceinline__ Item item(int64_t i) const {
+  __device__ __forceinline__ Item item(const Way& c) const {
+    const Place at = place(c);
+    const int p_tiles = (int)g.p_tiles, q_tile = quotient(at.tile, p_tiles);
     Item t;
-    t.slot = i / tiles();
-    const int64_t tile = i % tiles();
-    t.group = table.group_of(t.slot, n_groups);
-    const int64_t first = table.first_unit(t.group);
-    t.q0 = tile / g.p_tiles * T;
-    t.q_end = g.nq;
-    t.p0 = tile % g.p_tiles * T;
-    t.k0 = table.first_row(t.group) + (t.slot - first) * g.k_split;
-    const int64_t end = table.first_row(t.group + 1);
-    t.k_end = t.k0 + g.k_split < end ? t.k0 + g.k_split : end;
+    t.group = at.group;
     t.p_shift = 0;
-    t.direct = table.first_unit(t.group + 1) - first == 1;
+    t.q0 = q_tile * T;
+    t.q_end = g.nq;
+    t.p0 = (at.tile - q_tile * p_tiles) * T;
+    t.k0 = at.k0;
+    t.k_end = at.k_end;
+    t.slot = at.slot;
+    t.direct = at.direct;
     return t;
   }
 };
@@ -70,30 +60,31 @@ struct GroupedWeightGrad {
 };
 
 template <int W, bool kPT, class Out>
-__global__ __launch_bounds__(kThreads, 2) void rows_kernel(Product g, Out out, const int64_t* offsets, int32_t n_groups, int64_t n) {
+__global__ __launch_bounds__(kThreads, 2) void rows_kernel(Product g, Out out, const int64_t* offsets, int32_t n_groups, int32_t n) {
   __shared__ __attribute__((aligned(16))) Lds<W> lds;
   __shared__ GroupTable table;
-  table.build(offsets, n_groups, n, 64 * W);
-  product<W, kPT, false>(g, out, GroupedRows<64 * W>{g, table, n_groups}, lds, blockIdx.x, gridDim.x);
+  table.build<kTiles>(offsets, n_groups, n, 64 * W);
+  product<W, kPT, false>(g, out, GroupedRows<64 * W>{{table, n_groups, (int)g.p_tiles}, g}, lds, blockIdx.x, gridDim.x);
 }
 
 template <int W>
 __global__ __launch_bounds__(kThreads, 2) void sums_kernel(Product g, GroupedWeightGrad out, const int64_t* offsets, int32_t n_groups,
-                                                           int64_t n) {
+                                                           int32_t n) {
   __shared__ __attribute__((aligned(16))) Lds<W> lds;
   __shared__ GroupTable table;
-  table.build(offsets, n_groups, n, g.k_split);
-  product<W, true, true>(g, out, GroupedSums<64 * W>{g, table, n_groups}, lds, blockIdx.x, gridDim.x);
+  table.build<kShares>(offsets, n_groups, n, (int)g.k_split);
+  const int tiles = (int)((g.nq + 64 * W - 1) / (64 * W) * g.p_tiles);
+  product<W, true, true>(g, out, GroupedSums<64 * W>{{table, n_groups, tiles, (int)g.k_split}, g}, lds, blockIdx.x, gridDim.x);
 }
 
 // Group blockIdx.y's shares added in order, a quad of values a thread; zeros where it has none.
-__global__ __launch_bounds__(kThreads) void join_groups_kernel(int64_t n, int32_t n_groups, const int64_t* offsets, int64_t k_split,
+__global__ __launch_bounds__(kThreads) void join_groups_kernel(int32_t n, int32_t n_groups, const int64_t* offsets, int32_t k_split,
                                                                const float* gw_parts, float* gw, int64_t size,
                                                                const float* gb_parts, float* gb, int32_t d_out) {
   __shared__ GroupTable table;
-  table.build(offsets, n_groups, n, k_split);
+  table.build<kShares>(offsets, n_groups, n, k_split);
   const int group = blockIdx.y;
-  const int64_t first = table.unit[group], last = table.unit[group + 1];
+  const int first = table.unit[group], last = table.unit[group + 1];
   if (last - first == 1) return;
   const int64_t quads = size / 4, all = quads + d_out / 4;
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < all; i += (int64_t)gridDim.x * kThreads) {
@@ -101,7 +92,7 @@ __global__ __launch_bounds__(kThreads) void join_groups_kernel(int64_t n, int32_
     const float4* at = w ? reinterpret_cast<const float4*>(gw_parts) + i : reinterpret_cast<const float4*>(gb_parts) + (i - quads);
     const int64_t step = w ? quads : d_out / 4;
     float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    int64_t j = first;
+    int j = first;
     for (; j + 7 < last; j += 8) {
       float4 a[8];
 #pragma unroll
@@ -125,14 +116,14 @@ template <int W, bool kPT, class Out>
 void launch_rows(Product g, const Out& out, const int64_t* offsets, int32_t n_groups, int64_t n, hipStream_t stream) {
   g.p_tiles = cdiv(g.np, 64 * W);
   const int64_t most = (n / (64 * W) + n_groups) * g.p_tiles;
-  rows_kernel<W, kPT><<<(unsigned)(most < 65536 ? most : 65536), kThreads, 0, stream>>>(g, out, offsets, n_groups, n);
+  rows_kernel<W, kPT><<<(unsigned)(most < 65536 ? most : 65536), kThreads, 0, stream>>>(g, out, offsets, n_groups, (int32_t)n);
 }
 
 template <int W>
 void launch_sums(Product g, const GroupedWeightGrad& out, const int64_t* offsets, int32_t n_groups, int64_t n, hipStream_t stream) {
   g.p_tiles = cdiv(g.np, 64 * W);
-  const int64_t most = (n / g.k_split + n_groups) * g.p_tiles * cdiv(g.nq, 64 * W);
-  sums_kernel<W><<<(unsigned)(most < 65536 ? most : 65536), kThreads, 0, stream>>>(g, out, offsets, n_groups, n);
+  const int64_t most = cdiv(n, g.k_split) * g.p_tiles * cdiv(g.nq, 64 * W);
+  sums_kernel<W><<<(unsigned)(most < 65536 ? most : 65536), kThreads, 0, stream>>>(g, out, offsets, n_groups, (int32_t)n);
 }
 
 struct Cut {
@@ -195,7 +186,7 @@ maestro_status launch_join_groups(int64_t n, int32_t n_groups, const int64_t* of
                                   float* gw, int64_t size, const float* gb_parts, float* gb, int32_t d_out, hipStream_t stream) {
   const int64_t blocks = cdiv(size / 4 + d_out / 4, kThreads);
   join_groups_kernel<<<dim3((unsigned)(blocks < 4096 ? blocks : 4096), (unsigned)n_groups), kThreads, 0, stream>>>(
-      n, n_groups, offsets, k_split, gw_parts, gw, size, gb_parts, gb, d_out);
+      (int32_t)n, n_groups, offsets, (int32_t)k_split, gw_parts, gw, size, gb_parts, gb, d_out);
   return launch_status();
 }
 

@@ -1,5 +1,6 @@
 // C-ABI entry points of include/maestro_layers.h: host-side argument checks, then the launchers.
 // Nothing here touches device memory; every check happens before the first launch.
+#include "groups.h"
 #include "layers.h"
 
 namespace {
@@ -27,7 +28,12 @@ maestro_status check_layer(int64_t n, int32_t d_in, int32_t d_out, int32_t dtype
 maestro_status check_grouped(int64_t n, int32_t n_groups, int32_t d_in, int32_t d_out, int32_t dtype) {
   if (n_groups < 1) return MAESTRO_ERR_INVALID_ARG;
   const maestro_status st = check_layer(n, d_in, d_out, dtype);
-  return st == MAESTRO_OK && n_groups > MAESTRO_MAX_LAYER_GROUPS ? MAESTRO_ERR_UNSUPPORTED : st;
+  if (st != MAESTRO_OK) return st;
+  // rows and tiles (64 x 64 at the least) are counted in 32 bits; 2^31 tiles are past any memory
+  if (n_groups > MAESTRO_MAX_LAYER_GROUPS || n > maestro::kMaxGroupedRows ||
+      (n / 64 + n_groups) * (((d_in > d_out ? d_in : d_out) + 63) / 64) >= (int64_t)1 << 31)
+    return MAESTRO_ERR_UNSUPPORTED;
+  return MAESTRO_OK;
 }
 
 }  // namespace

@@ -43,23 +43,39 @@ struct Item {
   int64_t slot;                      // which share of C, where k is split
   int32_t group;
   bool whole;                        // the sum over Q is not shared between workgroups
+  bool direct;                       // the whole of a group's C
+};
+
+// A workgroup's way through `items` units of work, workgroup `block` of `blocks` (a multiple of 8). XCD x (of 8; workgroups go
+// round them) takes a contiguous share, so that the tiles that read the same rows of Q run side by side on one L2.
+struct Cursor {
+  int64_t i, last, step;
+  __device__ __forceinline__ Cursor(int64_t items, uint32_t block, uint32_t blocks) {
+    const int64_t share = (items + 7) / 8, xcd = block & 7;
+    step = blocks >> 3;
+    last = (xcd + 1) * share < items ? (xcd + 1) * share : items;
+    i = xcd * share + (block >> 3);
+  }
+  __device__ __forceinline__ bool done() const { return i >= last; }
 };
 
 // The tiles of one product, all splits' one after the other.
 template <int TP, int TQ, int kDepth>
 struct Dense {
+  using Way = Cursor;
   const Product& g;
   int64_t per_split;
   __device__ __forceinline__ explicit Dense(const Product& product) : g(product), per_split(product.items / product.splits) {}
-  __device__ __forceinline__ int64_t items() const { return g.items; }
-  __device__ __forceinline__ Item item(int64_t i) const {
+  __device__ __forceinline__ Way begin(uint32_t block, uint32_t blocks) const { return Way(g.items, block, blocks); }
+  __device__ __forceinline__ void next(Way& c) const { c.i += c.step; }
+  __device__ __forceinline__ Item item(const Way& c) const {
     Item t;
     t.p = g.p;
     t.q = g.q;
     t.group = 0;
-    t.whole = g.splits == 1;
-    t.slot = i / per_split;
-    const int64_t tile = i % per_split;
+    t.whole = t.direct = g.splits == 1;
+    t.slot = c.i / per_split;
+    const int64_t tile = c.i % per_split;
     t.q0 = tile / g.p_tiles * TQ;
     t.q_end = g.nq;
     t.p0 = tile % g.p_tiles * TP;
@@ -329,30 +345,16 @@ struct Staging {
   static __device__ __forceinline__ int place(int q) { return (q / (16 / kUnits)) & (kUnits - 1); }
 };
 
-// Eight consecutive values of C as they are before the rounding: sums, or those of 8-bit products times their scales, with the
-// biases. `at`: where the eight p are, of the wavefront's. In float32: ((sum * scale_q) * scale_p) + bias.
-template <class Out, class Acc>
-__device__ __forceinline__ void values8(float (&v)[8], const Acc& acc, int half, const float* bias, const float* scale_p, int at,
-                                        float scale_q) {
-  if constexpr (Out::kInt8) {
-#pragma unroll
-    for (int e = 0; e < 8; e += 4) {
-      const float4 s = *reinterpret_cast<const float4*>(scale_p + at + e), b = *reinterpret_cast<const float4*>(bias + at + e);
-      v[e] = (float)acc[8 * half + e] * scale_q * s.x + b.x;
-      v[e + 1] = (float)acc[8 * half + e + 1] * scale_q * s.y + b.y;
-      v[e + 2] = (float)acc[8 * half + e + 2] * scale_q * s.z + b.z;
-      v[e + 3] = (float)acc[8 * half + e + 3] * scale_q * s.w + b.w;
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = acc[8 * half + e];
-  }
+// Keeps the sums of one block where the products left them, up to here: of 256 x 256 tiles they fill the accumulation registers,
+// and copies of other blocks made ahead would take the vector registers of the main loop's addresses.
+template <int WP, int WQ, class Acc>
+__device__ __forceinline__ void in_place(Acc& acc) {
+  if constexpr (WP * WQ == 16) asm volatile("" : "+a"(acc));
 }
 
 template <int WP, int WQ, class Out, class Acc>
 __device__ __forceinline__ void store_rows(const Out& out, const Product& g, const Item& t, unsigned char* staging, int64_t q0,
-                                           int64_t p0, int lane, const Acc (&acc)[WP][WQ], const float* bias,
-                                           const float* scale_p, const float (&scale_q)[WQ]) {
+                                           int64_t p0, int lane, Acc (&acc)[WP][WQ]) {
   using S = Staging<WP>;
   constexpr int kStores = 32 / S::kRows;                    // of one q block and WS p blocks
   const int r = lane & 31, h = lane >> 5;
@@ -385,11 +387,14 @@ __device__ __forceinline__ void store_rows(const Out& out, const Product& g, con
 #pragma unroll
     for (int w = 0; w < WP / S::WS; ++w) {
 #pragma unroll
+      for (int a = 0; a < S::WS; ++a) in_place<WP, WQ>(acc[w * S::WS + a][b]);
+#pragma unroll
       for (int a = 0; a < S::WS; ++a)
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           float v[8];
-          values8<Out>(v, acc[w * S::WS + a][b], half, bias, scale_p, 32 * (w * S::WS + a) + 16 * half + 8 * h, scale_q[b]);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = acc[w * S::WS + a][b][8 * half + e];
           *reinterpret_cast<u32x4*>(staging + r * S::kRowBytes + (((4 * a + 2 * half + h) ^ S::place(r)) << 4)) = pack8(v);
         }
       u32x4 v[kStores];
@@ -423,32 +428,81 @@ __device__ __forceinline__ void store_rows(const Out& out, const Product& g, con
   }
 }
 
-// The same in float32, straight from the lanes: eight values (32 bytes) of a row each.
-template <int WP, int WQ, class Out, class Acc>
-__device__ __forceinline__ void store_floats(const Out& out, const Product& g, const Item& t, int64_t q0, int64_t p0, int lane,
-                                             const Acc (&acc)[WP][WQ], const float* bias, const float* scale_p,
-                                             const float (&scale_q)[WQ]) {
+// A wavefront's part of C from sums of 8-bit products: fma(sum * scale_q, scale_p, bias), not below `least` (a NaN stays one).
+// `place`: the biases and, kPlace / 2 further, the scales of the wavefront's 32 WP p. bfloat16 by way of LDS as above; float32
+// straight from the lanes, eight values (32 bytes) of a row each, in stores that the main loop's waits do not count.
+template <int WP, int WQ, class Out>
+__device__ __forceinline__ void store_scaled(const Out& out, const Product& g, const Item& t, unsigned char* staging, int64_t q0,
+                                             int64_t p0, int lane, i32x16 (&acc)[WP][WQ], const float* place, int scales) {
+  typedef typename Out::type T;
+  constexpr bool kStaged = std::is_same<T, __bf16>::value;
+  using S = Staging<WP>;
+  constexpr int kStores = 32 / S::kRows;
   const int r = lane & 31, h = lane >> 5;
-  const bool relu = out.relu;
+  const int row0 = lane / S::kUnits, unit0 = lane % S::kUnits;
+  const uint32_t ld = (uint32_t)g.np * 2, step = S::kRows * ld;
+  const float least = out.relu ? 0.0f : -INFINITY;
+  Rows c;
+  c.init(out.c, q0, t.q_end, 32 * WQ, ld);
+  float scale_q[WQ];
 #pragma unroll
   for (int b = 0; b < WQ; ++b) {
     const int64_t q = q0 + 32 * b + r;
+    scale_q[b] = q < t.q_end ? out.scale_q[q] : 0.0f;
+  }
 #pragma unroll
-    for (int a = 0; a < WP; ++a)
+  for (int w = 0; w < WP / S::WS; ++w) {
+    float4 bias[S::WS][4], scale[S::WS][4];                 // of the lane's p
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int in = 32 * a + 16 * half + 8 * h;
-        float v[8];
-        values8<Out>(v, acc[a][b], half, bias, scale_p, in, scale_q[b]);
-        if (relu)
+    for (int a = 0; a < S::WS; ++a)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = v[e] < 0.0f ? 0.0f : v[e];      // a NaN stays one
-        if (q < t.q_end && p0 + in < g.np) {
-          float4* at = reinterpret_cast<float4*>(out.c + q * g.np + p0 + in);
-          at[0] = make_float4(v[0], v[1], v[2], v[3]);
-          at[1] = make_float4(v[4], v[5], v[6], v[7]);
-        }
+      for (int i = 0; i < 4; ++i) {
+        const float* from = place + 32 * (w * S::WS + a) + 16 * (i / 2) + 8 * h + 4 * (i % 2);
+        bias[a][i] = *reinterpret_cast<const float4*>(from);
+        scale[a][i] = *reinterpret_cast<const float4*>(from + scales);
       }
+    const int64_t p_unit = p0 + 32 * S::WS * w + 8 * unit0;
+    const uint32_t at = p_unit < g.np ? (uint32_t)(row0 * ld + p_unit * 2) : 0x80000000u;
+#pragma unroll
+    for (int b = 0; b < WQ; ++b) {
+#pragma unroll
+      for (int a = 0; a < S::WS; ++a) in_place<WP, WQ>(acc[w * S::WS + a][b]);
+#pragma unroll
+      for (int a = 0; a < S::WS; ++a)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float4 &s = scale[a][2 * half + e / 4], &z = bias[a][2 * half + e / 4];
+            const float sum = (float)acc[w * S::WS + a][b][8 * half + e] * scale_q[b];
+            v[e] = __builtin_elementwise_maximum(
+                fmaf(sum, e % 4 == 0 ? s.x : e % 4 == 1 ? s.y : e % 4 == 2 ? s.z : s.w,
+                     e % 4 == 0 ? z.x : e % 4 == 1 ? z.y : e % 4 == 2 ? z.z : z.w), least);
+          }
+          if constexpr (kStaged) {
+            *reinterpret_cast<u32x4*>(staging + r * S::kRowBytes + (((4 * a + 2 * half + h) ^ S::place(r)) << 4)) = pack8(v);
+          } else {
+            const int64_t q = q0 + 32 * b + r, p = p0 + 32 * (w * S::WS + a) + 16 * half + 8 * h;
+            if (q < t.q_end && p < g.np) {
+              float4* to = reinterpret_cast<float4*>(out.c + q * g.np + p);
+              to[0] = make_float4(v[0], v[1], v[2], v[3]);
+              to[1] = make_float4(v[4], v[5], v[6], v[7]);
+            }
+          }
+        }
+      if constexpr (kStaged) {
+        u32x4 v[kStores];
+#pragma unroll
+        for (int j = 0; j < kStores; ++j) {
+          const int row = j * S::kRows + row0;
+          v[j] = *reinterpret_cast<const u32x4*>(staging + row * S::kRowBytes + ((unit0 ^ S::place(row)) << 4));
+        }
+#pragma unroll
+        for (int j = 0; j < kStores; ++j) c.store(v[j], at + (b * kStores + j) * step);
+      }
+      asm volatile("" ::: "memory");                        // one block's values at a time: registers
+    }
   }
 }
 
@@ -489,25 +543,21 @@ __device__ __forceinline__ void product(const Product& g, const Out& out, const 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wp = wave % NP, wq = wave / NP;
 
-  // XCD x (of 8; workgroups go round them) takes a contiguous share of the items, so that the tiles that read
-  // the same rows of Q run side by side on one L2
-  const int64_t items = work.items();
-  const int64_t share = (items + 7) / 8, xcd = block & 7, step = blocks >> 3;
-  const int64_t last = (xcd + 1) * share < items ? (xcd + 1) * share : items;
-  const int64_t first = xcd * share + (block >> 3);
-  if (first >= last) return;
+  typename Work::Way at = work.begin(block, blocks);
+  if (at.done()) return;
 
   Operand<TP, kDepth, kPT> op;
   Operand<TQ, kDepth, kQT> oq;
-  int64_t fetch_item = first, fetch_left = 0;               // the tile being loaded, and its stages still to load
+  auto fetch_at = at;                                       // the tile being loaded, and its stages still to load
+  int64_t fetch_left = 0;
   auto open = [&]() {
-    if (fetch_item >= last) {
+    if (fetch_at.done()) {
       op.none();
       oq.none();
       fetch_left = INT64_MAX;
       return;
     }
-    const Item t = work.item(fetch_item);
+    const Item t = work.item(fetch_at);
     op.tile(t.p, g.ldp, t.p0, g.np, t.k0, t.kn, wave, lane);
     oq.tile(t.q, g.ldq, t.q0, t.q_end, t.k0, t.kn, wave, lane);
     fetch_left = t.stages;
@@ -515,7 +565,7 @@ __device__ __forceinline__ void product(const Product& g, const Out& out, const 
   const uint32_t lds0 = lds_addr(lds);
   auto fetched = [&]() {
     if (--fetch_left == 0) {
-      fetch_item += step;
+      work.next(fetch_at);
       open();
     }
   };
@@ -525,28 +575,29 @@ __device__ __forceinline__ void product(const Product& g, const Out& out, const 
   fp.init(wp * WP, lane);
   fq.init(wq * WQ, lane);
 
-  // this wavefront's biases (and scales) of item j, into LDS a tile ahead of their use; two places in turn
+  // this wavefront's biases (and scales) of a tile, into LDS a tile ahead of their use; two places in turn
   constexpr int kPlace = 64 * kEpilogueLoads;
   float* biases = reinterpret_cast<float*>(lds + kBufs * kStage + (L::kStores ? 4 * Staging<WP>::kBytes : 0)) + wave * 2 * kPlace;
   int parity = 0;
-  auto fetch_biases = [&](int64_t j) {
+  auto fetch_biases = [&](const typename Work::Way& j) {
     if constexpr (Out::kBias) {
-      const Item t = work.item(j);
+      const bool there = !j.done();
+      const Item t = work.item(there ? j : at);
       const int64_t pw = t.p0 + 32 * WP * wp;
-      const i32x4 r = buffer_rsrc(out.bias + (int64_t)t.group * g.np, j < last ? (uint32_t)(g.np * 4) : 0);
+      const i32x4 r = buffer_rsrc(out.bias + (int64_t)t.group * g.np, there ? (uint32_t)(g.np * 4) : 0);
       const uint32_t to = lds_addr(biases + (parity ? kPlace : 0));
 #pragma unroll
       for (int l = 0; l < kBiasLoads; ++l)
         dma4(r, (uint32_t)(pw + 64 * l + lane) * 4, __builtin_amdgcn_readfirstlane(to + 256 * l));
       if constexpr (Out::kInt8) {
-        const i32x4 s = buffer_rsrc(out.scale_p, j < last ? (uint32_t)(g.np * 4) : 0);
+        const i32x4 s = buffer_rsrc(out.scale_p, there ? (uint32_t)(g.np * 4) : 0);
 #pragma unroll
         for (int l = 0; l < kBiasLoads; ++l)
           dma4(s, (uint32_t)(pw + 64 * l + lane) * 4, __builtin_amdgcn_readfirstlane(to + 256 * (kBiasLoads + l)));
       }
     }
   };
-  fetch_biases(first);
+  fetch_biases(at);
 
   open();
 #pragma unroll
@@ -564,8 +615,9 @@ __device__ __forceinline__ void product(const Product& g, const Out& out, const 
   for (int b = 0; b < WQ; ++b) qf[0][b] = fq.read(lds + kQ, 0, b);
   int buf = 0;
 #pragma clang loop unroll(disable)
-  for (int64_t i = first; i < last; i += step) {
-    const Item t = work.item(i);
+  for (bool first = true; !at.done(); first = false) {
+    const Item t = work.item(at);
+    work.next(at);
     using Acc = std::conditional_t<Out::kInt8, i32x16, f32x16>;
     Acc acc[WP][WQ];
     const float* place = biases + (parity ? kPlace : 0);
@@ -581,7 +633,7 @@ __device__ __forceinline__ void product(const Product& g, const Out& out, const 
             const float4 f = *reinterpret_cast<const float4*>(bias + 32 * a + 2 * (v & 8) + (v & 4));
             acc[a][b][v] = f.x, acc[a][b][v + 1] = f.y, acc[a][b][v + 2] = f.z, acc[a][b][v + 3] = f.w;
           }
-      fetch_biases(i + step);
+      fetch_biases(at);
     } else {
 #pragma unroll
       for (int a = 0; a < WP; ++a)
@@ -589,7 +641,7 @@ __device__ __forceinline__ void product(const Product& g, const Out& out, const 
         for (int b = 0; b < WQ; ++b)
 #pragma unroll
           for (int v = 0; v < 16; ++v) acc[a][b][v] = 0;
-      fetch_biases(i + step);
+      fetch_biases(at);
     }
     float sums[kSums ? WQ : 1] = {};
     // the sum over Q's k (the biases' gradient): a stage's by one of the workgroups with these rows of Q,
@@ -622,7 +674,7 @@ __device__ __forceinline__ void product(const Product& g, const Out& out, const 
         if (end) {
           // The next stage is there, and this one read by all. Vector memory operations complete in order:
           // for the first stages after a tile's stores, those are newer than the loads waited for.
-          if (kStores && s < kBufs - 1 && i != first) wait_loads<kLoads * (kBufs - 2) + kStores>();
+          if (kStores && s < kBufs - 1 && !first) wait_loads<kLoads * (kBufs - 2) + kStores>();
           else wait_loads<kLoads * (kBufs - 2)>();
           into = lds0 + buf * kStage;
           buf = buf == kBufs - 1 ? 0 : buf + 1;
@@ -666,17 +718,9 @@ __device__ __forceinline__ void product(const Product& g, const Out& out, const 
     if (Out::kBias && t.stages < kBufs) wait_own<0>();      // else a stage's wait has covered the next biases
     const int64_t qw = t.q0 + 32 * WQ * wq, pw = t.p0 + 32 * WP * wp;        // this wavefront's part
     if constexpr (!kSums) {
-      float scale_q[WQ] = {};
-      if constexpr (Out::kInt8)
-#pragma unroll
-        for (int b = 0; b < WQ; ++b) {
-          const int64_t q = qw + 32 * b + (lane & 31);
-          scale_q[b] = q < t.q_end ? out.scale_q[q] : 0.0f;
-        }
-      if constexpr (L::kStores)
-        store_rows<WP, WQ>(out, g, t, lds + kBufs * kStage + wave * Staging<WP>::kBytes, qw, pw, lane, acc, place,
-                           place + 64 * kBiasLoads, scale_q);
-      else store_floats<WP, WQ>(out, g, t, qw, pw, lane, acc, place, place + 64 * kBiasLoads, scale_q);
+      unsigned char* staging = lds + kBufs * kStage + wave * Staging<WP>::kBytes;
+      if constexpr (Out::kInt8) store_scaled<WP, WQ>(out, g, t, staging, qw, pw, lane, acc, place, 64 * kBiasLoads);
+      else store_rows<WP, WQ>(out, g, t, staging, qw, pw, lane, acc);
     } else {
       const int r = lane & 31, h = lane >> 5;
       float* gw = out.weights(g, t);

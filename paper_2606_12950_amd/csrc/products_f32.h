@@ -58,17 +58,26 @@ struct Item {
   bool direct;                       // the whole of a group's C
 };
 
+// A workgroup's way through `items` units of work, workgroup `block` of `blocks`.
+struct Cursor {
+  int64_t i, last, step;
+  __device__ __forceinline__ Cursor(int64_t items, uint32_t block, uint32_t blocks) : i(block), last(items), step(blocks) {}
+  __device__ __forceinline__ bool done() const { return i >= last; }
+};
+
 // The tiles of one product, all splits' one after the other.
 template <int T, class P>
 struct Dense {
+  using Way = Cursor;
   const ProductOf<P>& g;
   int64_t per_split;
   __device__ __forceinline__ explicit Dense(const ProductOf<P>& product) : g(product), per_split(product.items / product.splits) {}
-  __device__ __forceinline__ int64_t items() const { return g.items; }
-  __device__ __forceinline__ Item item(int64_t i) const {
+  __device__ __forceinline__ Way begin(uint32_t block, uint32_t blocks) const { return Way(g.items, block, blocks); }
+  __device__ __forceinline__ void next(Way& c) const { c.i += c.step; }
+  __device__ __forceinline__ Item item(const Way& c) const {
     Item t;
-    t.slot = i / per_split;
-    const int64_t tile = i % per_split;
+    t.slot = c.i / per_split;
+    const int64_t tile = c.i % per_split;
     t.q0 = tile / g.p_tiles * T;
     t.q_end = g.nq;
     t.p0 = tile % g.p_tiles * T;
@@ -177,9 +186,8 @@ __device__ __forceinline__ void product(const ProductOf<P>& g, const Out& out, c
   auto& lds = shared.at;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 31, h = lane >> 5;
   const int wp = wave & 1, wq = wave >> 1;
-  const int64_t items = work.items();
-  for (int64_t i = block; i < items; i += blocks) {
-    const Item t = work.item(i);
+  for (auto at = work.begin(block, blocks); !at.done(); work.next(at)) {
+    const Item t = work.item(at);
     const int64_t q0 = t.q0, p0 = t.p0, k0 = t.k0, k_end = t.k_end;
     const P p_rows = g.p.from(t.p_shift);
     Operand<T, kPT> op;

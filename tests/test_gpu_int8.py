@@ -1,8 +1,9 @@
 """maestro_quantize_rows and maestro_layer_int8 against their definitions, bit for bit: codes from the real quotient (float64
 decides it: two float32 a 2^-24 of their size apart have quotients further from a tie than 2^-30), whole-number sums in
-int64, and the float32 steps in the documented order."""
+int64, and the float32 steps in the documented order; the fused multiply-add in 64 bits of mantissa, where its product is exact."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
@@ -77,9 +78,11 @@ def test_quantize_near_ties():
 
 
 def definition(x, w, bias, relu, dtype):
-    """(sum * x_scale) * weight_scale + bias in float32, rounded to dtype."""
+    """fma(sum * x_scale, weight_scale, bias) in float32, rounded to dtype."""
+    assert np.finfo(np.longdouble).nmant >= 63
     total = (x.codes.double() @ w.codes.double().t()).float()        # whole numbers below 2^53, rounded once
-    y = (total * x.scale[:, None]) * w.scale + bias
+    part = (total * x.scale[:, None]).numpy().astype(np.longdouble)
+    y = torch.from_numpy((part * w.scale.numpy().astype(np.longdouble) + bias.numpy().astype(np.longdouble)).astype(np.float32))
     if relu:
         y = torch.where(y < 0, 0.0, y)
     return y.to(dtype)

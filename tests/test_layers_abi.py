@@ -69,11 +69,14 @@ def test_grouped_grad_refuses(lib, bad, status):
 def test_grouped_grad_workspace(lib):
     ws = lib.maestro_layer_grouped_grad_workspace
     for dtype in (F32, BF16):
-        for n in (1, 300, 262139, 1 << 33):
+        for n in (1, 300, 262139, 1 << 30):
             need = ws(n, 3, 32, 16, dtype)
             assert need >= 4 * 33 * 16 and need % 4 == 0
             assert _grouped_grad(lib, n=n, dtype=dtype, size=need - 1) == WORKSPACE
         assert ws(0, 3, 32, 16, dtype) == 0
+    assert ws((1 << 31) - (1 << 16) + 1, 3, 32, 16, BF16) == 0
+    assert _grouped(lib, n=(1 << 31) - (1 << 16) + 1) == _grouped_grad(lib, n=(1 << 31) - (1 << 16) + 1) == UNSUPPORTED
+    assert _grouped(lib, n=1 << 30, i=16384) == UNSUPPORTED
     assert ws(4, 0, 32, 16, BF16) == ws(4, 257, 32, 16, BF16) == ws(4, 3, 24, 16, BF16) == ws(-1, 3, 32, 16, BF16) == 0
 
 
