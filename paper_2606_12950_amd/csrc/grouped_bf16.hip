@@ -1,7 +1,7 @@
 // The bfloat16 products (products_bf16.h) of a grouped layer and its gradients.
 //
 // Rows of a group make tiles of their own, each against the group's weights; workgroups are persistent and find a tile's group
-// in a table of the groups' rows that each builds in LDS. The weights' gradients cut every group's rows into shares of
+// in a table of the groups' rows that each wavefront builds. The weights' gradients cut every group's rows into shares of
 // k_split; a group of one share writes its gradient, of more its shares, which a second launch adds in order.
 #include "groups.h"
 #include "layers.h"
@@ -31,11 +31,12 @@ struct GroupedRows : GroupedRowsWay<8> {
   }
 };
 
-template <int TP, int TQ, int kDepth>
-struct GroupedSums : GroupedSumsWay<8> {
+template <int TP, int TQ, int kDepth, GroupUnits kUnits>
+struct GroupedSums : GroupedSumsWay<8, kUnits> {
+  using Way = typename GroupedSumsWay<8, kUnits>::Way;
   const Product& g;
   __device__ __forceinline__ Item item(const Way& c) const {
-    const Place at = place(c);
+    const auto at = this->place(c);
     const int q_tile = quotient(at.tile, g.p_tiles);
     Item t;
     t.group = at.group;
@@ -71,20 +72,23 @@ __global__ __launch_bounds__(kThreads, (Tile<WP, WQ, kDepth, kBufs, Out>::kResid
     Product g, Out out, const int64_t* offsets, int32_t n_groups, int32_t n) {
   using L = Tile<WP, WQ, kDepth, kBufs, Out>;
   __shared__ __attribute__((aligned(16))) unsigned char lds[L::kBytes];
-  __shared__ GroupTable table;
+  GroupTable table;
   table.build<kTiles>(offsets, n_groups, n, L::TQ);
-  product<WP, WQ, kDepth, kBufs, kPT, false>(g, out, GroupedRows<L::TP, L::TQ, kDepth>{{table, n_groups, g.p_tiles}, g}, lds, blockIdx.x, gridDim.x);
+  product<WP, WQ, kDepth, kBufs, kPT, false>(g, out, GroupedRows<L::TP, L::TQ, kDepth>{{table, g.p_tiles}, g}, lds, blockIdx.x, gridDim.x);
 }
 
-template <int WP, int WQ, int kDepth, int kBufs>
+// alone: no group has more than one unit, and no second launch follows.
+template <int WP, int WQ, int kDepth, int kBufs, GroupUnits kUnits>
 __global__ __launch_bounds__(kThreads, (Tile<WP, WQ, kDepth, kBufs, GroupedWeightGrad>::kResident)) void sums_kernel(
-    Product g, GroupedWeightGrad out, const int64_t* offsets, int32_t n_groups, int32_t n) {
+    Product g, GroupedWeightGrad out, const int64_t* offsets, int32_t n_groups, int32_t n, bool alone) {
   using L = Tile<WP, WQ, kDepth, kBufs, GroupedWeightGrad>;
   __shared__ __attribute__((aligned(16))) unsigned char lds[L::kBytes];
-  __shared__ GroupTable table;
-  table.build<kShares>(offsets, n_groups, n, (int)g.k_split);
+  GroupTable table;
+  table.build<kUnits>(offsets, n_groups, n, (int)g.k_split);
   const int tiles = (int)((g.nq + L::TQ - 1) / L::TQ) * g.p_tiles;
-  product<WP, WQ, kDepth, kBufs, true, true>(g, out, GroupedSums<L::TP, L::TQ, kDepth>{{table, n_groups, tiles, (int)g.k_split}, g}, lds, blockIdx.x, gridDim.x);
+  product<WP, WQ, kDepth, kBufs, true, true>(g, out, GroupedSums<L::TP, L::TQ, kDepth, kUnits>{{table, tiles, (int)g.k_split}, g}, lds, blockIdx.x,
+                                                gridDim.x);
+  if (alone) clear_empty_groups(table, out.gw, g.np * g.nq, out.gb, (int)g.nq);
 }
 
 uint32_t blocks_of(int64_t items, int64_t resident) {
@@ -107,18 +111,12 @@ void launch_rows(const Product& g, const Out& out, const int64_t* offsets, int32
   else launch_tiles<1, kPT>(g, out, offsets, n_groups, n, stream);
 }
 
-template <int WP, int WQ, int kDepth, int kBufs>
-void launch_sums(Product g, const GroupedWeightGrad& out, const int64_t* offsets, int32_t n_groups, int64_t n, hipStream_t stream) {
-  using L = Tile<WP, WQ, kDepth, kBufs, GroupedWeightGrad>;
-  g.p_tiles = (int32_t)cdiv(g.np, L::TP);
-  const uint32_t blocks = blocks_of(cdiv(n, g.k_split) * g.p_tiles * cdiv(g.nq, L::TQ), L::kResident);
-  sums_kernel<WP, WQ, kDepth, kBufs><<<blocks, kThreads, 0, stream>>>(g, out, offsets, n_groups, (int32_t)n);
-}
-
-// Tile of the weights' gradient and rows of a share, as for a layer of one group.
+// Tile of the weights' gradient and rows of a unit, as for a layer of one group. by_group: too few rows for a unit of them
+// in every workgroup.
 struct Cut {
   int32_t tp, tq;
   int64_t k_split, most;
+  bool by_group;
 };
 Cut cut_of(int64_t n, int64_t n_groups, int64_t d_in, int64_t d_out) {
   Cut c;
@@ -126,11 +124,23 @@ Cut cut_of(int64_t n, int64_t n_groups, int64_t d_in, int64_t d_out) {
   c.tq = c.tp == 128 ? 128 : d_out > 128 && n >= 131072 ? 256 : 64;
   const int64_t tiles = cdiv(d_in, c.tp) * cdiv(d_out, c.tq), resident = c.tq == 256 ? 1 : 2;
   int64_t splits = kCus * resident / tiles;
-  if (splits > cdiv(n, 512)) splits = cdiv(n, 512);
+  c.by_group = splits > cdiv(n, 512);
+  if (c.by_group) splits = cdiv(n, 512);
   if (splits < 1) splits = 1;
   c.k_split = cdiv(cdiv(n, splits), 64) * 64;
   c.most = n / c.k_split + n_groups;
   return c;
+}
+
+template <int WP, int WQ, int kDepth, int kBufs>
+void launch_sums(Product g, const GroupedWeightGrad& out, const int64_t* offsets, int32_t n_groups, int32_t n, bool by_group,
+                 bool alone, hipStream_t stream) {
+  using L = Tile<WP, WQ, kDepth, kBufs, GroupedWeightGrad>;
+  g.p_tiles = (int32_t)cdiv(g.np, L::TP);
+  const int64_t pieces = by_group ? n / g.k_split + n_groups : cdiv(n, g.k_split);
+  const uint32_t blocks = blocks_of(pieces * g.p_tiles * cdiv(g.nq, L::TQ), L::kResident);
+  auto kernel = by_group ? sums_kernel<WP, WQ, kDepth, kBufs, kTiles> : sums_kernel<WP, WQ, kDepth, kBufs, kShares>;
+  kernel<<<blocks, kThreads, 0, stream>>>(g, out, offsets, n_groups, n, alone);
 }
 
 }  // namespace
@@ -152,7 +162,7 @@ maestro_status launch_grouped_grad_bf16(int64_t n, int32_t n_groups, int32_t d_i
                                         const void* weight, const void* g_z, const int64_t* offsets, bool relu_input,
                                         void* g_x, float* g_weight, float* g_bias, void* workspace, hipStream_t stream) {
   const int64_t size = (int64_t)d_in * d_out;
-  if (n == 0) return launch_join_groups(0, n_groups, offsets, 1, nullptr, g_weight, size, nullptr, g_bias, d_out, stream);
+  if (n == 0) return launch_join_groups(0, n_groups, offsets, 1, true, nullptr, g_weight, size, nullptr, g_bias, d_out, stream);
   const __bf16 *xb = static_cast<const __bf16*>(x), *gz = static_cast<const __bf16*>(g_z);
   const Cut c = cut_of(n, n_groups, d_in, d_out);
   float *gw_parts = static_cast<float*>(workspace), *gb_parts = gw_parts + c.most * size;
@@ -162,12 +172,12 @@ maestro_status launch_grouped_grad_bf16(int64_t n, int32_t n_groups, int32_t d_i
   }
   const Product gw{xb, gz, d_in, d_out, d_in, d_out, n, c.k_split, 1, 0, 0};
   const GroupedWeightGrad out{g_weight, g_bias, gw_parts, gb_parts, 1};
-  if (c.tq == 256) launch_sums<4, 4, 32, 4>(gw, out, offsets, n_groups, n, stream);
-  else if (c.tp == 256) launch_sums<4, 1, 64, 2>(gw, out, offsets, n_groups, n, stream);
-  else launch_sums<2, 2, 64, 2>(gw, out, offsets, n_groups, n, stream);
+  const bool alone = n <= c.k_split;
+  auto sums = c.tq == 256 ? launch_sums<4, 4, 32, 4> : c.tp == 256 ? launch_sums<4, 1, 64, 2> : launch_sums<2, 2, 64, 2>;
+  sums(gw, out, offsets, n_groups, (int32_t)n, c.by_group, alone, stream);
   const maestro_status st = launch_status();
-  if (st != MAESTRO_OK) return st;
-  return launch_join_groups(n, n_groups, offsets, c.k_split, gw_parts, g_weight, size, gb_parts, g_bias, d_out, stream);
+  if (st != MAESTRO_OK || alone) return st;
+  return launch_join_groups(n, n_groups, offsets, c.k_split, c.by_group, gw_parts, g_weight, size, gb_parts, g_bias, d_out, stream);
 }
 
 }  // namespace maestro

@@ -28,11 +28,12 @@ struct GroupedRows : GroupedRowsWay<1> {
   }
 };
 
-template <int T>
-struct GroupedSums : GroupedSumsWay<1> {
+template <int T, GroupUnits kUnits>
+struct GroupedSums : GroupedSumsWay<1, kUnits> {
+  using Way = typename GroupedSumsWay<1, kUnits>::Way;
   const Product& g;
   __device__ __forceinline__ Item item(const Way& c) const {
-    const Place at = place(c);
+    const auto at = this->place(c);
     const int p_tiles = (int)g.p_tiles, q_tile = quotient(at.tile, p_tiles);
     Item t;
     t.group = at.group;
@@ -62,29 +63,32 @@ struct GroupedWeightGrad {
 template <int W, bool kPT, class Out>
 __global__ __launch_bounds__(kThreads, 2) void rows_kernel(Product g, Out out, const int64_t* offsets, int32_t n_groups, int32_t n) {
   __shared__ __attribute__((aligned(16))) Lds<W> lds;
-  __shared__ GroupTable table;
+  GroupTable table;
   table.build<kTiles>(offsets, n_groups, n, 64 * W);
-  product<W, kPT, false>(g, out, GroupedRows<64 * W>{{table, n_groups, (int)g.p_tiles}, g}, lds, blockIdx.x, gridDim.x);
+  product<W, kPT, false>(g, out, GroupedRows<64 * W>{{table, (int)g.p_tiles}, g}, lds, blockIdx.x, gridDim.x);
 }
 
-template <int W>
+// alone: no group has more than one unit, and no second launch follows.
+template <int W, GroupUnits kUnits>
 __global__ __launch_bounds__(kThreads, 2) void sums_kernel(Product g, GroupedWeightGrad out, const int64_t* offsets, int32_t n_groups,
-                                                           int32_t n) {
+                                                           int32_t n, bool alone) {
   __shared__ __attribute__((aligned(16))) Lds<W> lds;
-  __shared__ GroupTable table;
-  table.build<kShares>(offsets, n_groups, n, (int)g.k_split);
+  GroupTable table;
+  table.build<kUnits>(offsets, n_groups, n, (int)g.k_split);
   const int tiles = (int)((g.nq + 64 * W - 1) / (64 * W) * g.p_tiles);
-  product<W, true, true>(g, out, GroupedSums<64 * W>{{table, n_groups, tiles, (int)g.k_split}, g}, lds, blockIdx.x, gridDim.x);
+  product<W, true, true>(g, out, GroupedSums<64 * W, kUnits>{{table, tiles, (int)g.k_split}, g}, lds, blockIdx.x, gridDim.x);
+  if (alone) clear_empty_groups(table, out.gw, g.np * g.nq, out.gb, (int)g.nq);
 }
 
-// Group blockIdx.y's shares added in order, a quad of values a thread; zeros where it has none.
+// Group blockIdx.y's units added in order, a quad of values a thread; zeros where it has none.
+template <GroupUnits kUnits>
 __global__ __launch_bounds__(kThreads) void join_groups_kernel(int32_t n, int32_t n_groups, const int64_t* offsets, int32_t k_split,
                                                                const float* gw_parts, float* gw, int64_t size,
                                                                const float* gb_parts, float* gb, int32_t d_out) {
-  __shared__ GroupTable table;
-  table.build<kShares>(offsets, n_groups, n, k_split);
+  GroupTable table;
+  table.build<kUnits>(offsets, n_groups, n, k_split);
   const int group = blockIdx.y;
-  const int first = table.unit[group], last = table.unit[group + 1];
+  const int first = table.first_unit(group), last = table.first_unit(group + 1);
   if (last - first == 1) return;
   const int64_t quads = size / 4, all = quads + d_out / 4;
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < all; i += (int64_t)gridDim.x * kThreads) {
@@ -119,16 +123,10 @@ void launch_rows(Product g, const Out& out, const int64_t* offsets, int32_t n_gr
   rows_kernel<W, kPT><<<(unsigned)(most < 65536 ? most : 65536), kThreads, 0, stream>>>(g, out, offsets, n_groups, (int32_t)n);
 }
 
-template <int W>
-void launch_sums(Product g, const GroupedWeightGrad& out, const int64_t* offsets, int32_t n_groups, int64_t n, hipStream_t stream) {
-  g.p_tiles = cdiv(g.np, 64 * W);
-  const int64_t most = cdiv(n, g.k_split) * g.p_tiles * cdiv(g.nq, 64 * W);
-  sums_kernel<W><<<(unsigned)(most < 65536 ? most : 65536), kThreads, 0, stream>>>(g, out, offsets, n_groups, (int32_t)n);
-}
-
+// As for a layer of one group. by_group: too few rows for a unit of them in every workgroup.
 struct Cut {
-  bool wide;
-  int64_t k_split, most;             // rows of a share, and the most shares
+  bool wide, by_group;
+  int64_t k_split, most;             // rows of a unit, and the most units
 };
 Cut cut_of(int64_t n, int64_t n_groups, int64_t d_in, int64_t d_out) {
   Cut c;
@@ -136,11 +134,22 @@ Cut cut_of(int64_t n, int64_t n_groups, int64_t d_in, int64_t d_out) {
   c.wide = d_in > 64 && d_out > 64 && n >= 32768 && 5 * large <= 6 * small;
   const int64_t t = c.wide ? 128 : 64, tiles = cdiv(d_in, t) * cdiv(d_out, t);
   int64_t splits = 2 * kCus / tiles;
-  if (splits > cdiv(n, 256)) splits = cdiv(n, 256);
+  c.by_group = splits > cdiv(n, 256);
+  if (c.by_group) splits = cdiv(n, 256);
   if (splits < 1) splits = 1;
   c.k_split = cdiv(cdiv(n, splits), kDepth) * kDepth;
   c.most = n / c.k_split + n_groups;
   return c;
+}
+
+template <int W>
+void launch_sums(Product g, const GroupedWeightGrad& out, const int64_t* offsets, int32_t n_groups, int32_t n, bool by_group,
+                 bool alone, hipStream_t stream) {
+  g.p_tiles = cdiv(g.np, 64 * W);
+  const int64_t pieces = by_group ? n / g.k_split + n_groups : cdiv(n, g.k_split);
+  const int64_t most = pieces * g.p_tiles * cdiv(g.nq, 64 * W);
+  auto kernel = by_group ? sums_kernel<W, kTiles> : sums_kernel<W, kShares>;
+  kernel<<<(unsigned)(most < 65536 ? most : 65536), kThreads, 0, stream>>>(g, out, offsets, n_groups, n, alone);
 }
 
 }  // namespace
@@ -164,7 +173,7 @@ maestro_status launch_grouped_grad_f32(int64_t n, int32_t n_groups, int32_t d_in
                                        const float* weight, const float* g_z, const int64_t* offsets, bool relu_input,
                                        float* g_x, float* g_weight, float* g_bias, void* workspace, hipStream_t stream) {
   const int64_t size = (int64_t)d_in * d_out;
-  if (n == 0) return launch_join_groups(0, n_groups, offsets, 1, nullptr, g_weight, size, nullptr, g_bias, d_out, stream);
+  if (n == 0) return launch_join_groups(0, n_groups, offsets, 1, true, nullptr, g_weight, size, nullptr, g_bias, d_out, stream);
   const Cut c = cut_of(n, n_groups, d_in, d_out);
   float *gw_parts = static_cast<float*>(workspace), *gb_parts = gw_parts + c.most * size;
   if (g_x) {
@@ -175,17 +184,19 @@ maestro_status launch_grouped_grad_f32(int64_t n, int32_t n_groups, int32_t d_in
   }
   const Product gw{{x, d_in}, {g_z, d_out}, d_in, d_out, n, c.k_split, 1, 0, 0};
   const GroupedWeightGrad out{g_weight, g_bias, gw_parts, gb_parts};
-  if (c.wide) launch_sums<2>(gw, out, offsets, n_groups, n, stream);
-  else launch_sums<1>(gw, out, offsets, n_groups, n, stream);
+  const bool alone = n <= c.k_split;
+  (c.wide ? launch_sums<2> : launch_sums<1>)(gw, out, offsets, n_groups, (int32_t)n, c.by_group, alone, stream);
   const maestro_status st = launch_status();
-  if (st != MAESTRO_OK) return st;
-  return launch_join_groups(n, n_groups, offsets, c.k_split, gw_parts, g_weight, size, gb_parts, g_bias, d_out, stream);
+  if (st != MAESTRO_OK || alone) return st;
+  return launch_join_groups(n, n_groups, offsets, c.k_split, c.by_group, gw_parts, g_weight, size, gb_parts, g_bias, d_out, stream);
 }
 
-maestro_status launch_join_groups(int64_t n, int32_t n_groups, const int64_t* offsets, int64_t k_split, const float* gw_parts,
-                                  float* gw, int64_t size, const float* gb_parts, float* gb, int32_t d_out, hipStream_t stream) {
+maestro_status launch_join_groups(int64_t n, int32_t n_groups, const int64_t* offsets, int64_t k_split, bool by_group,
+                                  const float* gw_parts, float* gw, int64_t size, const float* gb_parts, float* gb, int32_t d_out,
+                                  hipStream_t stream) {
   const int64_t blocks = cdiv(size / 4 + d_out / 4, kThreads);
-  join_groups_kernel<<<dim3((unsigned)(blocks < 4096 ? blocks : 4096), (unsigned)n_groups), kThreads, 0, stream>>>(
+  auto kernel = by_group ? join_groups_kernel<kTiles> : join_groups_kernel<kShares>;
+  kernel<<<dim3((unsigned)(blocks < 4096 ? blocks : 4096), (unsigned)n_groups), kThreads, 0, stream>>>(
       (int32_t)n, n_groups, offsets, (int32_t)k_split, gw_parts, gw, size, gb_parts, gb, d_out);
   return launch_status();
 }

@@ -20,9 +20,10 @@ maestro_status launch_grouped_grad_f32(int64_t n, int32_t n_groups, int32_t d_in
 maestro_status launch_grouped_grad_bf16(int64_t n, int32_t n_groups, int32_t d_in, int32_t d_out, const void* x,
                                         const void* weight, const void* g_z, const int64_t* offsets, bool relu_input,
                                         void* g_x, float* g_weight, float* g_bias, void* workspace, hipStream_t stream);
-// every group's g_w and g_b from the shares of its rows, k_split rows each; a group of one share has them already
-maestro_status launch_join_groups(int64_t n, int32_t n_groups, const int64_t* offsets, int64_t k_split, const float* gw_parts,
-                                  float* gw, int64_t size, const float* gb_parts, float* gb, int32_t d_out, hipStream_t stream);
+// every group's g_w and g_b from those of its units of k_split rows (by_group: kTiles, else kShares); a group of one unit has them already
+maestro_status launch_join_groups(int64_t n, int32_t n_groups, const int64_t* offsets, int64_t k_split, bool by_group,
+                                  const float* gw_parts, float* gw, int64_t size, const float* gb_parts, float* gb, int32_t d_out,
+                                  hipStream_t stream);
 
 maestro_status launch_quantize_rows(int64_t n, int32_t d, int32_t dtype, const void* x, int8_t* codes, float* scale,
                                     hipStream_t stream);
