@@ -112,7 +112,8 @@ void launch_rows(const Product& g, const Out& out, const int64_t* offsets, int32
 }
 
 // Tile of the weights' gradient and rows of a unit, as for a layer of one group. by_group: too few rows for a unit of them
-// in every workgroup.
+// in every workgroup; then 64 x 64 tiles where four to a CU hold them all. Measured (us, 64 x 64 / 256 x 64 or 128 x 128): 300 rows in 5
+// groups 256 -> 512 5.8 / 7.9, 4,000 in 4 256 -> 256 12.1 / 15.8, 8,000 in 16 512 -> 64 10.3 / 14.0, 20,000 in 60 128 -> 128 9.8 / 12.8.
 struct Cut {
   int32_t tp, tq;
   int64_t k_split, most;
@@ -129,6 +130,7 @@ Cut cut_of(int64_t n, int64_t n_groups, int64_t d_in, int64_t d_out) {
   if (splits < 1) splits = 1;
   c.k_split = cdiv(cdiv(n, splits), 64) * 64;
   c.most = n / c.k_split + n_groups;
+  if (c.by_group && c.most * cdiv(d_in, 64) * cdiv(d_out, 64) <= 4 * kCus) c.tp = c.tq = 64;
   return c;
 }
 
@@ -173,7 +175,7 @@ maestro_status launch_grouped_grad_bf16(int64_t n, int32_t n_groups, int32_t d_i
   const Product gw{xb, gz, d_in, d_out, d_in, d_out, n, c.k_split, 1, 0, 0};
   const GroupedWeightGrad out{g_weight, g_bias, gw_parts, gb_parts, 1};
   const bool alone = n <= c.k_split;
-  auto sums = c.tq == 256 ? launch_sums<4, 4, 32, 4> : c.tp == 256 ? launch_sums<4, 1, 64, 2> : launch_sums<2, 2, 64, 2>;
+  auto sums = c.tp == 64 ? launch_sums<1, 1, 64, 2> : c.tq == 256 ? launch_sums<4, 4, 32, 4> : c.tp == 256 ? launch_sums<4, 1, 64, 2> : launch_sums<2, 2, 64, 2>;
   sums(gw, out, offsets, n_groups, (int32_t)n, c.by_group, alone, stream);
   const maestro_status st = launch_status();
   if (st != MAESTRO_OK || alone) return st;
