@@ -21,7 +21,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libmaestro.so")
 SOURCES = ("api.hip", "predict.hip", "predict_split.hip", "roles.hip", "route.hip", "fitness.hip", "fitness_pruned.hip", "prioritize.hip",
            "train_api.hip", "logprobs.hip", "layers.hip", "layers_bf16.hip", "clip.hip", "layers_api.hip", "grouped_f32.hip",
-           "grouped_bf16.hip", "int8.hip", "packed.hip")
+           "grouped_bf16.hip", "int8.hip", "packed.hip", "packed_f32.hip", "packed_bf16.hip")
 CALIBRATE_LIB = os.path.join(PKG, "libmaestro_calibrate.so")
 CALIBRATE_SOURCE = "calibrate.hip"
 # the host half of the binding, against torch's C++ interface

@@ -56,7 +56,7 @@ struct GroupedSums : GroupedSumsWay<8, kUnits> {
 };
 
 struct GroupedWeightGrad {
-  static constexpr bool kBias = false, kInt8 = false;
+  static constexpr bool kBias = false, kInt8 = false, kCodes = false;
   float *gw, *gb, *gw_parts, *gb_parts;
   int32_t parts;                     // 1
   __device__ __forceinline__ float* weights(const Product& g, const Item& t) const {

@@ -35,6 +35,14 @@ maestro_status launch_pack(int64_t n, int32_t d, int32_t dtype, const void* x, b
                            hipStream_t stream);
 maestro_status launch_unpack(int64_t n, int32_t d, int32_t dtype, const void* codes, const uint8_t* exponents, bool rectified,
                              void* x, hipStream_t stream);
+size_t grad_packed_f32_workspace_bytes(int64_t n, int32_t d_in, int32_t d_out);
+size_t grad_packed_bf16_workspace_bytes(int64_t n, int32_t d_in, int32_t d_out);
+maestro_status launch_grad_packed_f32(int64_t n, int32_t d_in, int32_t d_out, const void* codes, const uint8_t* exponents,
+                                      bool rectified, const float* weight, const float* g_z, bool relu_input, float* g_x,
+                                      float* g_weight, float* g_bias, void* workspace, hipStream_t stream);
+maestro_status launch_grad_packed_bf16(int64_t n, int32_t d_in, int32_t d_out, const void* codes, const uint8_t* exponents,
+                                       bool rectified, const void* weight, const void* g_z, bool relu_input, void* g_x,
+                                       float* g_weight, float* g_bias, void* workspace, hipStream_t stream);
 size_t grad_packed_workspace_bytes(int64_t n, int32_t d_in, int32_t d_out, int32_t dtype);
 maestro_status launch_grad_packed(int64_t n, int32_t d_in, int32_t d_out, int32_t dtype, const void* codes,
                                   const uint8_t* exponents, bool rectified, const void* weight, const void* g_z, bool relu_input,

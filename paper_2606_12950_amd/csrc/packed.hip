@@ -104,10 +104,6 @@ void unpack(int64_t n, int32_t d, const Code* codes, const uint8_t* exponents, T
   });
 }
 
-size_t values_bytes(int64_t n, int32_t d_in, int32_t dtype) {
-  return ((size_t)n * d_in * (dtype == MAESTRO_BF16 ? 2 : 4) + 255) & ~(size_t)255;
-}
-
 }  // namespace
 
 maestro_status launch_pack(int64_t n, int32_t d, int32_t dtype, const void* x, bool rectified, void* codes, uint8_t* exponents,
@@ -130,17 +126,19 @@ maestro_status launch_unpack(int64_t n, int32_t d, int32_t dtype, const void* co
 }
 
 size_t grad_packed_workspace_bytes(int64_t n, int32_t d_in, int32_t d_out, int32_t dtype) {
-  return values_bytes(n, d_in, dtype) + layer_grad_workspace_bytes(n, d_in, d_out, dtype);
+  return dtype == MAESTRO_BF16 ? grad_packed_bf16_workspace_bytes(n, d_in, d_out) : grad_packed_f32_workspace_bytes(n, d_in, d_out);
 }
 
-// The values in the workspace, then the layer's gradients as of any input.
 maestro_status launch_grad_packed(int64_t n, int32_t d_in, int32_t d_out, int32_t dtype, const void* codes,
                                   const uint8_t* exponents, bool rectified, const void* weight, const void* g_z, bool relu_input,
                                   void* g_x, float* g_weight, float* g_bias, void* workspace, hipStream_t stream) {
-  const maestro_status st = launch_unpack(n, d_in, dtype, codes, exponents, rectified, workspace, stream);
-  if (st != MAESTRO_OK) return st;
-  return launch_layer_grad(n, d_in, d_out, dtype, workspace, weight, g_z, relu_input, g_x, g_weight, g_bias,
-                           static_cast<unsigned char*>(workspace) + values_bytes(n, d_in, dtype), stream);
+  if (n == 0) return launch_join(nullptr, 0, g_weight, (int64_t)d_in * d_out, nullptr, 0, g_bias, d_out, stream);
+  if (dtype == MAESTRO_BF16)
+    return launch_grad_packed_bf16(n, d_in, d_out, codes, exponents, rectified, weight, g_z, relu_input, g_x, g_weight, g_bias,
+                                   workspace, stream);
+  return launch_grad_packed_f32(n, d_in, d_out, codes, exponents, rectified, static_cast<const float*>(weight),
+                                static_cast<const float*>(g_z), relu_input, static_cast<float*>(g_x), g_weight, g_bias, workspace,
+                                stream);
 }
 
 }  // namespace maestro

@@ -1,0 +1,118 @@
+// The bfloat16 products (products_bf16.h) of a layer's gradients from an input kept in 8 bits.
+//
+// The weights' gradient takes the codes as its operand P and makes values of them on the way into LDS; the input's needs
+// them for its mask only. Nothing is unpacked in memory.
+#include "layers.h"
+#include "products_bf16.h"
+
+namespace maestro {
+namespace {
+
+template <int WP, int WQ, int kDepth, int kBufs, bool kPT, bool kQT, class Out>
+__global__ __launch_bounds__(kThreads, (Tile<WP, WQ, kDepth, kBufs, Out>::kResident)) void product_kernel(Product g, Out out) {
+  using L = Tile<WP, WQ, kDepth, kBufs, Out>;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[L::kBytes];
+  product<WP, WQ, kDepth, kBufs, kPT, kQT>(g, out, Dense<L::TP, L::TQ, kDepth>(g), lds, blockIdx.x, gridDim.x);
+}
+
+// Both gradients in one launch: the first `blocks` workgroups make the input's, in 64 x 64 tiles, the others the weights'.
+template <int WP, int WQ>
+__global__ __launch_bounds__(kThreads, 2) void pair_kernel(Product gx, CodesInputGrad x, uint32_t blocks, Product gw, CodesWeightGrad w) {
+  using X = Tile<1, 1, 64, 2, CodesInputGrad>;
+  using W = Tile<WP, WQ, 64, 2, CodesWeightGrad>;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[X::kBytes > W::kBytes ? X::kBytes : W::kBytes];
+  if (blockIdx.x < blocks) product<1, 1, 64, 2, true, false>(gx, x, Dense<X::TP, X::TQ, 64>(gx), lds, blockIdx.x, blocks);
+  else product<WP, WQ, 64, 2, true, true>(gw, w, Dense<W::TP, W::TQ, 64>(gw), lds, blockIdx.x - blocks, gridDim.x - blocks);
+}
+
+// the rest of a product's numbers, and its workgroups
+template <class Tile>
+uint32_t plan(Product& g) {
+  g.p_tiles = (int32_t)cdiv(g.np, Tile::TP);
+  g.splits = (int32_t)cdiv(g.nk, g.k_split);
+  g.items = cdiv(g.nq, Tile::TQ) * g.p_tiles * g.splits;
+  const int64_t want = cdiv(g.items, 8) * 8, most = kCus * Tile::kResident;
+  return (uint32_t)(want < most ? want : most);
+}
+
+template <int WP, int WQ, bool kQT, class Out>
+void launch(Product g, const Out& out, hipStream_t stream) {
+  const uint32_t blocks = plan<Tile<WP, WQ, 64, 2, Out>>(g);
+  product_kernel<WP, WQ, 64, 2, true, kQT, Out><<<blocks, kThreads, 0, stream>>>(g, out);
+}
+
+template <int WP, int WQ>
+void launch_pair(Product gx, const CodesInputGrad& x, Product gw, const CodesWeightGrad& w, hipStream_t stream) {
+  const uint32_t blocks = plan<Tile<1, 1, 64, 2, CodesInputGrad>>(gx), more = plan<Tile<WP, WQ, 64, 2, CodesWeightGrad>>(gw);
+  pair_kernel<WP, WQ><<<blocks + more, kThreads, 0, stream>>>(gx, x, blocks, gw, w);
+}
+
+// As for the gradients of an input in bfloat16.
+int tile_of(int64_t np, int64_t nq) {
+  if (np > 128 && cdiv(np, 256) * cdiv(nq, 256) >= 2 * kCus) return 256;
+  return cdiv(np, 128) * cdiv(nq, 128) >= kCus ? 128 : 64;
+}
+
+struct Cut {
+  int32_t tp, tq;
+  int64_t k_split, splits;
+  int32_t parts;
+};
+Cut cut_of(int64_t n, int64_t d_in, int64_t d_out) {
+  Cut c;
+  c.tp = d_in > 128 ? 256 : 128;
+  c.tq = c.tp == 128 ? 128 : d_out > 128 && n >= 131072 ? 256 : 64;
+  const int64_t tiles = cdiv(d_in, c.tp) * cdiv(d_out, c.tq), resident = c.tq == 256 ? 1 : 2;
+  int64_t splits = kCus * resident / tiles;
+  if (splits > cdiv(n, 512)) splits = cdiv(n, 512);
+  if (splits < 1) splits = 1;
+  c.k_split = cdiv(cdiv(n, splits), 64) * 64;
+  c.splits = cdiv(n, c.k_split);
+  c.parts = c.splits > 1 ? (int32_t)cdiv(d_in, c.tp) : 1;
+  return c;
+}
+
+}  // namespace
+
+size_t grad_packed_bf16_workspace_bytes(int64_t n, int32_t d_in, int32_t d_out) {
+  if (n == 0) return 0;
+  const Cut c = cut_of(n, d_in, d_out);
+  return c.splits > 1 ? sizeof(float) * (size_t)(c.splits * ((int64_t)d_in + c.parts * 2) * d_out) : 0;
+}
+
+maestro_status launch_grad_packed_bf16(int64_t n, int32_t d_in, int32_t d_out, const void* codes, const uint8_t* exponents,
+                                       bool rectified, const void* weight, const void* g_z, bool relu_input, void* g_x,
+                                       float* g_weight, float* g_bias, void* workspace, hipStream_t stream) {
+  const __bf16* gz = static_cast<const __bf16*>(g_z);
+  const unsigned char* c8 = static_cast<const unsigned char*>(codes);
+  const Cut c = cut_of(n, d_in, d_out);
+  float* parts = static_cast<float*>(workspace);
+  float* gb_parts = parts + c.splits * d_in * d_out;
+  const Product gw{nullptr, gz, d_in, d_out, d_in, d_out, n, c.k_split, 1, 0, 0};
+  CodesWeightGrad w;
+  w.gw = c.splits > 1 ? parts : g_weight;
+  w.gb = c.splits > 1 ? gb_parts : g_bias;
+  w.parts = c.parts;
+  w.codes = c8;
+  w.exponents = exponents;
+  w.ld_exponents = (d_in + 31) / 32;
+  w.is_signed = !rectified;
+  const Product gx{static_cast<const __bf16*>(weight), gz, d_in, d_out, d_in, n, d_out, d_out, 1, 0, 0};
+  const CodesInputGrad x_out{c8, static_cast<__bf16*>(g_x), relu_input};
+  if (g_x && tile_of(d_in, n) == 64) {
+    if (c.tp == 256) launch_pair<4, 1>(gx, x_out, gw, w, stream);
+    else launch_pair<2, 2>(gx, x_out, gw, w, stream);
+  } else {
+    if (g_x && tile_of(d_in, n) == 256) launch<4, 4, false>(gx, x_out, stream);
+    else if (g_x) launch<2, 2, false>(gx, x_out, stream);
+    if (c.tq == 256) launch<4, 4, true>(gw, w, stream);
+    else if (c.tp == 256) launch<4, 1, true>(gw, w, stream);
+    else launch<2, 2, true>(gw, w, stream);
+  }
+  const maestro_status st = launch_status();
+  if (st != MAESTRO_OK || c.splits == 1) return st;
+  return launch_join(parts, (int32_t)c.splits, g_weight, (int64_t)d_in * d_out, gb_parts, (int32_t)(c.splits * c.parts * 2),
+                     g_bias, d_out, stream);
+}
+
+}  // namespace maestro

@@ -112,11 +112,12 @@ struct Rows {
 
 // What becomes of C. kMask: C is 0 wherever `x`, of C's shape, is not positive (kMaskBf16), or not zero (kMaskCodes,
 // unsigned bytes). kBias: `bias` [p], of the tile's group, is added and, with relu, negative values become 0. kInt8: the
-// operands are signed bytes, and a sum counts scale_q[q] * scale_p[p]; the products' extents of k are in pairs of them.
+// operands are signed bytes, and a sum counts scale_q[q] * scale_p[p]; the products' extents of k are in pairs of them. kCodes: P
+// is the values of kept activations (CodesOperand).
 enum { kMaskNone, kMaskBf16, kMaskCodes };
 struct Forward {
   static constexpr int kMask = kMaskNone;
-  static constexpr bool kBias = true, kInt8 = false;
+  static constexpr bool kBias = true, kInt8 = false, kCodes = false;
   typedef __bf16 type;
   const float* bias;
   __bf16* c;
@@ -124,7 +125,7 @@ struct Forward {
 };
 struct InputGrad {
   static constexpr int kMask = kMaskBf16;
-  static constexpr bool kBias = false, kInt8 = false;
+  static constexpr bool kBias = false, kInt8 = false, kCodes = false;
   typedef __bf16 type;
   const __bf16* x;
   __bf16* c;
@@ -132,7 +133,7 @@ struct InputGrad {
 };
 struct CodesInputGrad {
   static constexpr int kMask = kMaskCodes;
-  static constexpr bool kBias = false, kInt8 = false;
+  static constexpr bool kBias = false, kInt8 = false, kCodes = false;
   typedef __bf16 type;
   const unsigned char* x;
   __bf16* c;
@@ -141,14 +142,14 @@ struct CodesInputGrad {
 template <class T>
 struct Int8Forward {
   static constexpr int kMask = kMaskNone;
-  static constexpr bool kBias = true, kInt8 = true;
+  static constexpr bool kBias = true, kInt8 = true, kCodes = false;
   typedef T type;
   const float *bias, *scale_p, *scale_q;
   T* c;
   int32_t relu;
 };
 struct WeightGrad {
-  static constexpr bool kBias = false, kInt8 = false;
+  static constexpr bool kBias = false, kInt8 = false, kCodes = false;
   float* gw;                         // [splits][nq][np]
   float* gb;                         // one split: [nq], whole; else [splits][parts][two wavefronts][nq]
   int32_t parts;                     // workgroups (of one split and q) that share the sum over Q
@@ -156,6 +157,14 @@ struct WeightGrad {
   __device__ __forceinline__ float* biases(const Product& g, const Item& t, int64_t part, int wp) const {
     return t.whole ? gb : gb + ((t.slot * parts + part) * 2 + wp) * g.nq;
   }
+};
+
+struct CodesWeightGrad : WeightGrad {
+  static constexpr bool kCodes = true;
+  const unsigned char* codes;        // [nk][np]
+  const unsigned char* exponents;    // [nk][ld_exponents]
+  int64_t ld_exponents;
+  int32_t is_signed;
 };
 
 template <int N>
@@ -258,6 +267,72 @@ struct Operand {
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) fetch(j);
     advance();
+  }
+};
+
+// A turned operand that memory holds as codes, bytes, and for every 32 of a row a power of two. A stage's codes come through
+// registers, 16 to a unit, and are values before they lie in LDS: a value has at most eight significant bits, so bfloat16
+// holds it exactly. They are loaded two stages ahead of the products' and turned into values one ahead, a pair after a product.
+template <int T, int kDepth>
+struct CodesOperand {
+  static constexpr int kUnits = T * kDepth / 16 / kThreads, kRowUnits = T / 16, kRows = kThreads / kRowUnits;
+  static constexpr int kPairs = 8 * kUnits;
+  u32x4 ahead[kUnits], now[kUnits];                         // the stages being loaded and turned into values
+  uint32_t ahead_exponent[kUnits];
+  float step[kUnits];
+  u32x4 packed;
+  const unsigned char *codes, *exponents;                   // of the next stage to load
+  int64_t left;                                             // its rows and all after it
+  uint32_t ld, ld_exponents, off, off_exponents, to, flip;
+  float zero;                                               // what a code of 0 counts, in steps: -128 of flipped ones
+
+  template <class Out>
+  __device__ __forceinline__ void init(const Out& out, int64_t ldp) {
+    const int k = threadIdx.x / kRowUnits, unit = threadIdx.x % kRowUnits;
+    ld = (uint32_t)ldp;
+    ld_exponents = (uint32_t)out.ld_exponents;
+    flip = out.is_signed ? 0x80808080u : 0u;                // signed bytes as unsigned ones, 128 more
+    zero = out.is_signed ? -128.0f : 0.0f;
+    to = k * 2 * T + (((2 * unit) ^ (4 * Operand<T, kDepth, true>::turn(k))) << 4);
+  }
+  template <class Out>
+  __device__ __forceinline__ void tile(const Out& out, int64_t p0, int64_t k0, int64_t kn) {
+    const int k = threadIdx.x / kRowUnits, unit = threadIdx.x % kRowUnits;
+    codes = out.codes + k0 * ld;
+    exponents = out.exponents + k0 * ld_exponents;
+    left = kn;
+    off = (uint32_t)(k * ld + p0 + 16 * unit);
+    off_exponents = (uint32_t)(k * ld_exponents + p0 / 32 + unit / 2);
+  }
+  __device__ __forceinline__ void none() { left = 0; }
+  __device__ __forceinline__ void load() {
+    const uint32_t rows = (uint32_t)(left < kDepth ? left < 0 ? 0 : left : kDepth);
+    const auto c = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(codes), 0, rows * ld, 0x00020000);
+    const auto e = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(exponents), 0, rows * ld_exponents, 0x00020000);
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j) {
+      ahead[j] = __builtin_amdgcn_raw_buffer_load_b128(c, off + j * kRows * ld, 0, 0);
+      ahead_exponent[j] = __builtin_amdgcn_raw_buffer_load_b8(e, off_exponents + j * kRows * ld_exponents, 0, 0);
+    }
+    codes += kDepth * (int64_t)ld;
+    exponents += kDepth * (int64_t)ld_exponents;
+    left -= kDepth;
+  }
+  __device__ __forceinline__ void take() {
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j) {
+      now[j] = ahead[j] ^ flip;
+      step[j] = __uint_as_float((ahead_exponent[j] & 255u) << 23);
+    }
+  }
+  // pair i of the stage, into the stage's buffer when it completes 16 bytes
+  __device__ __forceinline__ void pair(int i, unsigned char* stage) {
+    const int j = i / 8, r = i % 8;
+    const uint32_t w = now[j][r / 2] >> (16 * (r & 1));
+    const float base = zero * step[j];
+    const float a = fmaf((float)(w & 255u), step[j], base), b = fmaf((float)((w >> 8) & 255u), step[j], base);
+    packed[r % 4] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+    if (r % 4 == 3) *reinterpret_cast<u32x4*>(stage + to + j * kRows * 2 * T + (r / 4) * 16) = packed;
   }
 };
 
@@ -534,7 +609,10 @@ __device__ __forceinline__ void product(const Product& g, const Out& out, const 
                                         uint32_t blocks) {
   using L = Tile<WP, WQ, kDepth, kBufs, Out>;
   constexpr int NP = 2, TP = L::TP, TQ = L::TQ;
-  constexpr int kStage = L::kStage, kLoads = (TP + TQ) * kDepth / 2048, kHalves = kDepth / 16;
+  constexpr bool kCodes = Out::kCodes;
+  constexpr int kStage = L::kStage, kPLoads = kCodes ? 0 : TP * kDepth / 2048, kHalves = kDepth / 16;
+  constexpr int kLoads = kPLoads + TQ * kDepth / 2048;
+  static_assert(!kCodes || (kBufs == 2 && kPT), "a stage's end waits for all loads");
   constexpr int kQ = TP * 2 * kDepth;                       // Q's place in a stage
   constexpr bool kSums = kQT;                               // the weights' gradient sums Q too (the biases')
   constexpr int kBiasLoads = L::kBiasLoads, kEpilogueLoads = L::kEpilogueLoads;
@@ -552,13 +630,13 @@ __device__ __forceinline__ void product(const Product& g, const Out& out, const 
   int64_t fetch_left = 0;
   auto open = [&]() {
     if (fetch_at.done()) {
-      op.none();
+      if constexpr (!kCodes) op.none();
       oq.none();
       fetch_left = INT64_MAX;
       return;
     }
     const Item t = work.item(fetch_at);
-    op.tile(t.p, g.ldp, t.p0, g.np, t.k0, t.kn, wave, lane);
+    if constexpr (!kCodes) op.tile(t.p, g.ldp, t.p0, g.np, t.k0, t.kn, wave, lane);
     oq.tile(t.q, g.ldq, t.q0, t.q_end, t.k0, t.kn, wave, lane);
     fetch_left = t.stages;
   };
@@ -599,14 +677,55 @@ __device__ __forceinline__ void product(const Product& g, const Out& out, const 
   };
   fetch_biases(at);
 
+  // P's codes: a stage further ahead than Q
+  CodesOperand<TP, kDepth> codes;
+  auto codes_at = at;
+  int64_t codes_left = 0;
+  auto open_codes = [&]() {
+    if constexpr (kCodes) {
+      if (codes_at.done()) {
+        codes.none();
+        codes_left = INT64_MAX;
+        return;
+      }
+      const Item t = work.item(codes_at);
+      codes.tile(out, t.p0, t.k0, t.kn);
+      codes_left = t.stages;
+    }
+  };
+  auto load_codes = [&]() {
+    if constexpr (kCodes) {
+      codes.load();
+      if (--codes_left == 0) {
+        work.next(codes_at);
+        open_codes();
+      }
+    }
+  };
+
   open();
+  if constexpr (kCodes) {
+    codes.init(out, g.ldp);
+    open_codes();
+    load_codes();
+    codes.take();
+    load_codes();
+  }
 #pragma unroll
   for (int b = 0; b < kBufs; ++b) {
-    op.fetch_all(lds0 + b * kStage, wave);
+    if constexpr (!kCodes) op.fetch_all(lds0 + b * kStage, wave);
     oq.fetch_all(lds0 + b * kStage + kQ, wave);
     fetched();
   }
-  wait_loads<kLoads * (kBufs - 1)>();
+  if constexpr (kCodes) {
+#pragma unroll
+    for (int i = 0; i < codes.kPairs; ++i) codes.pair(i, lds);
+    codes.take();
+    load_codes();
+    wait_loads<0>();
+  } else {
+    wait_loads<kLoads * (kBufs - 1)>();
+  }
 
   bf16x8 pf[2][WP], qf[2][WQ];                              // this step's fragments and the next one's
 #pragma unroll
@@ -682,7 +801,12 @@ __device__ __forceinline__ void product(const Product& g, const Out& out, const 
         }
         const int to = end ? 0 : kk + 1;
         if (end) {
-          op.aim(into, wave);
+          if constexpr (kCodes) {
+            codes.take();
+            load_codes();
+          } else {
+            op.aim(into, wave);
+          }
           oq.aim(into + kQ, wave);
         }
         // of the products, the first half is followed by a share of the reads each, all by one of the loads
@@ -702,14 +826,22 @@ __device__ __forceinline__ void product(const Product& g, const Out& out, const 
           if (end) {
 #pragma unroll
             for (int l = m * kLoads / kProducts; l < (m + 1) * kLoads / kProducts; ++l) {
-              if (l < op.kLoads) op.fetch(l);
-              else oq.fetch(l - op.kLoads);
+              if (l < kPLoads) op.fetch(l);
+              else oq.fetch(l - kPLoads);
             }
+          }
+          if constexpr (kCodes) {                           // the next stage's values, before its end
+            constexpr int kSlots = (kHalves - 1) * kProducts;
+            const int slot = kk * kProducts + m;
+            if (!end)
+#pragma unroll
+              for (int i = slot * codes.kPairs / kSlots; i < (slot + 1) * codes.kPairs / kSlots; ++i)
+                codes.pair(i, lds + (buf ^ 1) * kStage);
           }
           __builtin_amdgcn_sched_barrier(0);
         }
         if (end) {
-          op.advance();
+          if constexpr (!kCodes) op.advance();
           oq.advance();
         }
       }
