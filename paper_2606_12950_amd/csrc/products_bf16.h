@@ -278,7 +278,7 @@ struct CodesOperand {
   static constexpr int kUnits = T * kDepth / 16 / kThreads, kRowUnits = T / 16, kRows = kThreads / kRowUnits;
   static constexpr int kPairs = 8 * kUnits;
   u32x4 ahead[kUnits], now[kUnits];                         // the stages being loaded and turned into values
-  uint32_t ahead_exponent[kUnits];
+  uint8_t ahead_exponent[kUnits];
   float step[kUnits];
   u32x4 packed;
   const unsigned char *codes, *exponents;                   // of the next stage to load
@@ -322,7 +322,9 @@ struct CodesOperand {
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
       now[j] = ahead[j] ^ flip;
-      step[j] = __uint_as_float((ahead_exponent[j] & 255u) << 23);
+      step[j] = __uint_as_float((uint32_t)ahead_exponent[j] << 23);
+      // here and not after the next loads, whose registers would then be others, and waited for to be copied
+      asm volatile("" : "+v"(now[j]), "+v"(step[j]));
     }
   }
   // pair i of the stage, into the stage's buffer when it completes 16 bytes
