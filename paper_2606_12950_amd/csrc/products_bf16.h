@@ -283,7 +283,9 @@ struct CodesOperand {
   u32x4 packed;
   const unsigned char *codes, *exponents;                   // of the next stage to load
   int64_t left;                                             // its rows and all after it
-  uint32_t ld, ld_exponents, off, off_exponents, to, flip;
+  uint32_t ld, ld_exponents, off, off_exponents, flip;
+  uint32_t to;                                              // in the stage, the 16 bytes it writes first of a unit's 32
+  bool second;                                              // those are the unit's second ones
   float zero;                                               // what a code of 0 counts, in steps: -128 of flipped ones
 
   template <class Out>
@@ -293,7 +295,9 @@ struct CodesOperand {
     ld_exponents = (uint32_t)out.ld_exponents;
     flip = out.is_signed ? 0x80808080u : 0u;                // signed bytes as unsigned ones, 128 more
     zero = out.is_signed ? -128.0f : 0.0f;
-    to = k * 2 * T + (((2 * unit) ^ (4 * Operand<T, kDepth, true>::turn(k))) << 4);
+    // eight lanes write 128 bytes at a time: neighbouring fours of them begin with other halves, and meet all banks
+    second = (unit & 4) != 0;
+    to = k * 2 * T + (((2 * unit + second) ^ (4 * Operand<T, kDepth, true>::turn(k))) << 4);
   }
   template <class Out>
   __device__ __forceinline__ void tile(const Out& out, int64_t p0, int64_t k0, int64_t kn) {
@@ -321,7 +325,7 @@ struct CodesOperand {
   __device__ __forceinline__ void take() {
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
-      now[j] = ahead[j] ^ flip;
+      now[j] = (second ? __builtin_shufflevector(ahead[j], ahead[j], 2, 3, 0, 1) : ahead[j]) ^ flip;
       step[j] = __uint_as_float((uint32_t)ahead_exponent[j] << 23);
       // here and not after the next loads, whose registers would then be others, and waited for to be copied
       asm volatile("" : "+v"(now[j]), "+v"(step[j]));
@@ -334,7 +338,7 @@ struct CodesOperand {
     const float base = zero * step[j];
     const float a = fmaf((float)(w & 255u), step[j], base), b = fmaf((float)((w >> 8) & 255u), step[j], base);
     packed[r % 4] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
-    if (r % 4 == 3) *reinterpret_cast<u32x4*>(stage + to + j * kRows * 2 * T + (r / 4) * 16) = packed;
+    if (r % 4 == 3) *reinterpret_cast<u32x4*>(stage + (to ^ (16 * (r / 4))) + j * kRows * 2 * T) = packed;
   }
 };
 
@@ -832,10 +836,10 @@ __device__ __forceinline__ void product(const Product& g, const Out& out, const 
               else oq.fetch(l - kPLoads);
             }
           }
-          if constexpr (kCodes) {                           // the next stage's values, before its end
-            constexpr int kSlots = (kHalves - 1) * kProducts;
-            const int slot = kk * kProducts + m;
-            if (!end)
+          if constexpr (kCodes) {                           // the next stage's values, before its end and beside the reads
+            constexpr int kFree = kProducts - kHalf, kSlots = (kHalves - 1) * kFree;
+            const int slot = kk * kFree + m - kHalf;
+            if (!end && m >= kHalf)
 #pragma unroll
               for (int i = slot * codes.kPairs / kSlots; i < (slot + 1) * codes.kPairs / kSlots; ++i)
                 codes.pair(i, lds + (buf ^ 1) * kStage);
