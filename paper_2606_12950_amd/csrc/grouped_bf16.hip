@@ -67,26 +67,26 @@ struct GroupedWeightGrad {
   }
 };
 
-template <int WP, int WQ, int kDepth, int kBufs, bool kPT, class Out>
-__global__ __launch_bounds__(kThreads, (Tile<WP, WQ, kDepth, kBufs, Out>::kResident)) void rows_kernel(
+template <int WP, int WQ, int kDepth, int kBufs, bool kPT, int kWaves, class Out>
+__global__ __launch_bounds__(64 * kWaves, (Tile<WP, WQ, kDepth, kBufs, Out, kWaves>::kSimdWaves)) void rows_kernel(
     Product g, Out out, const int64_t* offsets, int32_t n_groups, int32_t n) {
-  using L = Tile<WP, WQ, kDepth, kBufs, Out>;
+  using L = Tile<WP, WQ, kDepth, kBufs, Out, kWaves>;
   __shared__ __attribute__((aligned(16))) unsigned char lds[L::kBytes];
   GroupTable table;
   table.build<kTiles>(offsets, n_groups, n, L::TQ);
-  product<WP, WQ, kDepth, kBufs, kPT, false>(g, out, GroupedRows<L::TP, L::TQ, kDepth>{{table, g.p_tiles}, g}, lds, blockIdx.x, gridDim.x);
+  product<WP, WQ, kDepth, kBufs, kPT, false, kWaves>(g, out, GroupedRows<L::TP, L::TQ, kDepth>{{table, g.p_tiles}, g}, lds, blockIdx.x, gridDim.x);
 }
 
 // alone: no group has more than one unit, and no second launch follows.
-template <int WP, int WQ, int kDepth, int kBufs, GroupUnits kUnits>
-__global__ __launch_bounds__(kThreads, (Tile<WP, WQ, kDepth, kBufs, GroupedWeightGrad>::kResident)) void sums_kernel(
+template <int WP, int WQ, int kDepth, int kBufs, int kWaves, GroupUnits kUnits>
+__global__ __launch_bounds__(64 * kWaves, (Tile<WP, WQ, kDepth, kBufs, GroupedWeightGrad, kWaves>::kSimdWaves)) void sums_kernel(
     Product g, GroupedWeightGrad out, const int64_t* offsets, int32_t n_groups, int32_t n, bool alone) {
-  using L = Tile<WP, WQ, kDepth, kBufs, GroupedWeightGrad>;
+  using L = Tile<WP, WQ, kDepth, kBufs, GroupedWeightGrad, kWaves>;
   __shared__ __attribute__((aligned(16))) unsigned char lds[L::kBytes];
   GroupTable table;
   table.build<kUnits>(offsets, n_groups, n, (int)g.k_split);
   const int tiles = (int)((g.nq + L::TQ - 1) / L::TQ) * g.p_tiles;
-  product<WP, WQ, kDepth, kBufs, true, true>(g, out, GroupedSums<L::TP, L::TQ, kDepth, kUnits>{{table, tiles, (int)g.k_split}, g}, lds, blockIdx.x,
+  product<WP, WQ, kDepth, kBufs, true, true, kWaves>(g, out, GroupedSums<L::TP, L::TQ, kDepth, kUnits>{{table, tiles, (int)g.k_split}, g}, lds, blockIdx.x,
                                                 gridDim.x);
   if (alone) clear_empty_groups(table, out.gw, g.np * g.nq, out.gb, (int)g.nq);
 }
@@ -96,19 +96,26 @@ uint32_t blocks_of(int64_t items, int64_t resident) {
   return (uint32_t)(want < most ? want : most);
 }
 
-template <int W, bool kPT, class Out>
+template <int WP, int WQ, bool kPT, int kWaves, class Out>
 void launch_tiles(Product g, const Out& out, const int64_t* offsets, int32_t n_groups, int64_t n, hipStream_t stream) {
-  using L = Tile<W, W, 64, 2, Out>;
+  using L = Tile<WP, WQ, 64, 2, Out, kWaves>;
   g.p_tiles = (int32_t)cdiv(g.np, L::TP);
   const uint32_t blocks = blocks_of((n / L::TQ + n_groups) * g.p_tiles, L::kResident);
-  rows_kernel<W, W, 64, 2, kPT><<<blocks, kThreads, 0, stream>>>(g, out, offsets, n_groups, (int32_t)n);
+  rows_kernel<WP, WQ, 64, 2, kPT, kWaves><<<blocks, 64 * kWaves, 0, stream>>>(g, out, offsets, n_groups, (int32_t)n);
 }
 
+// Tile by how many there are, as for a layer of one group. 256 x 256 ones by eight wavefronts, two to a SIMD, or by four: the layer
+// with eight 546 us, four 544 (262,139 x 1024 -> 1024, 16 groups); the input's gradient, whose mask wants registers, 612 and 575.
 template <bool kPT, class Out>
 void launch_rows(const Product& g, const Out& out, const int64_t* offsets, int32_t n_groups, int64_t n, hipStream_t stream) {
-  if (g.np > 128 && cdiv(g.np, 256) * (n / 256) >= 2 * kCus) launch_tiles<4, kPT>(g, out, offsets, n_groups, n, stream);
-  else if (cdiv(g.np, 128) * (n / 128) >= kCus) launch_tiles<2, kPT>(g, out, offsets, n_groups, n, stream);
-  else launch_tiles<1, kPT>(g, out, offsets, n_groups, n, stream);
+  if (g.np > 128 && cdiv(g.np, 256) * (n / 256) >= 2 * kCus) {
+    if constexpr (kPT) launch_tiles<4, 4, kPT, 4>(g, out, offsets, n_groups, n, stream);
+    else launch_tiles<4, 2, kPT, 8>(g, out, offsets, n_groups, n, stream);
+  } else if (cdiv(g.np, 128) * (n / 128) >= kCus) {
+    launch_tiles<2, 2, kPT, 4>(g, out, offsets, n_groups, n, stream);
+  } else {
+    launch_tiles<1, 1, kPT, 4>(g, out, offsets, n_groups, n, stream);
+  }
 }
 
 // Tile of the weights' gradient and rows of a unit, as for a layer of one group. by_group: too few rows for a unit of them
@@ -134,15 +141,15 @@ Cut cut_of(int64_t n, int64_t n_groups, int64_t d_in, int64_t d_out) {
   return c;
 }
 
-template <int WP, int WQ, int kDepth, int kBufs>
+template <int WP, int WQ, int kDepth, int kBufs, int kWaves>
 void launch_sums(Product g, const GroupedWeightGrad& out, const int64_t* offsets, int32_t n_groups, int32_t n, bool by_group,
                  bool alone, hipStream_t stream) {
-  using L = Tile<WP, WQ, kDepth, kBufs, GroupedWeightGrad>;
+  using L = Tile<WP, WQ, kDepth, kBufs, GroupedWeightGrad, kWaves>;
   g.p_tiles = (int32_t)cdiv(g.np, L::TP);
   const int64_t pieces = by_group ? n / g.k_split + n_groups : cdiv(n, g.k_split);
   const uint32_t blocks = blocks_of(pieces * g.p_tiles * cdiv(g.nq, L::TQ), L::kResident);
-  auto kernel = by_group ? sums_kernel<WP, WQ, kDepth, kBufs, kTiles> : sums_kernel<WP, WQ, kDepth, kBufs, kShares>;
-  kernel<<<blocks, kThreads, 0, stream>>>(g, out, offsets, n_groups, n, alone);
+  auto kernel = by_group ? sums_kernel<WP, WQ, kDepth, kBufs, kWaves, kTiles> : sums_kernel<WP, WQ, kDepth, kBufs, kWaves, kShares>;
+  kernel<<<blocks, 64 * kWaves, 0, stream>>>(g, out, offsets, n_groups, n, alone);
 }
 
 }  // namespace
@@ -175,7 +182,7 @@ maestro_status launch_grouped_grad_bf16(int64_t n, int32_t n_groups, int32_t d_i
   const Product gw{xb, gz, d_in, d_out, d_in, d_out, n, c.k_split, 1, 0, 0};
   const GroupedWeightGrad out{g_weight, g_bias, gw_parts, gb_parts, 1};
   const bool alone = n <= c.k_split;
-  auto sums = c.tp == 64 ? launch_sums<1, 1, 64, 2> : c.tq == 256 ? launch_sums<4, 4, 32, 4> : c.tp == 256 ? launch_sums<4, 1, 64, 2> : launch_sums<2, 2, 64, 2>;
+  auto sums = c.tp == 64 ? launch_sums<1, 1, 64, 2, 4> : c.tq == 256 ? launch_sums<4, 2, 32, 4, 8> : c.tp == 256 ? launch_sums<4, 1, 64, 2, 4> : launch_sums<2, 2, 64, 2, 4>;
   sums(gw, out, offsets, n_groups, (int32_t)n, c.by_group, alone, stream);
   const maestro_status st = launch_status();
   if (st != MAESTRO_OK || alone) return st;

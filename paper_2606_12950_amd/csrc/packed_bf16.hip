@@ -8,11 +8,11 @@
 namespace maestro {
 namespace {
 
-template <int WP, int WQ, int kDepth, int kBufs, bool kPT, bool kQT, class Out>
-__global__ __launch_bounds__(kThreads, (Tile<WP, WQ, kDepth, kBufs, Out>::kResident)) void product_kernel(Product g, Out out) {
-  using L = Tile<WP, WQ, kDepth, kBufs, Out>;
+template <int WP, int WQ, bool kQT, int kWaves, class Out>
+__global__ __launch_bounds__(64 * kWaves, (Tile<WP, WQ, 64, 2, Out, kWaves>::kSimdWaves)) void product_kernel(Product g, Out out) {
+  using L = Tile<WP, WQ, 64, 2, Out, kWaves>;
   __shared__ __attribute__((aligned(16))) unsigned char lds[L::kBytes];
-  product<WP, WQ, kDepth, kBufs, kPT, kQT>(g, out, Dense<L::TP, L::TQ, kDepth>(g), lds, blockIdx.x, gridDim.x);
+  product<WP, WQ, 64, 2, true, kQT, kWaves>(g, out, Dense<L::TP, L::TQ, 64>(g), lds, blockIdx.x, gridDim.x);
 }
 
 // Both gradients in one launch: the first `blocks` workgroups make the input's, in 64 x 64 tiles, the others the weights'.
@@ -35,10 +35,10 @@ uint32_t plan(Product& g) {
   return (uint32_t)(want < most ? want : most);
 }
 
-template <int WP, int WQ, bool kQT, class Out>
+template <int WP, int WQ, bool kQT, int kWaves, class Out>
 void launch(Product g, const Out& out, hipStream_t stream) {
-  const uint32_t blocks = plan<Tile<WP, WQ, 64, 2, Out>>(g);
-  product_kernel<WP, WQ, 64, 2, true, kQT, Out><<<blocks, kThreads, 0, stream>>>(g, out);
+  const uint32_t blocks = plan<Tile<WP, WQ, 64, 2, Out, kWaves>>(g);
+  product_kernel<WP, WQ, kQT, kWaves><<<blocks, 64 * kWaves, 0, stream>>>(g, out);
 }
 
 template <int WP, int WQ>
@@ -103,11 +103,11 @@ maestro_status launch_grad_packed_bf16(int64_t n, int32_t d_in, int32_t d_out, c
     if (c.tp == 256) launch_pair<4, 1>(gx, x_out, gw, w, stream);
     else launch_pair<2, 2>(gx, x_out, gw, w, stream);
   } else {
-    if (g_x && tile_of(d_in, n) == 256) launch<4, 4, false>(gx, x_out, stream);
-    else if (g_x) launch<2, 2, false>(gx, x_out, stream);
-    if (c.tq == 256) launch<4, 4, true>(gw, w, stream);
-    else if (c.tp == 256) launch<4, 1, true>(gw, w, stream);
-    else launch<2, 2, true>(gw, w, stream);
+    if (g_x && tile_of(d_in, n) == 256) launch<4, 4, false, 4>(gx, x_out, stream);
+    else if (g_x) launch<2, 2, false, 4>(gx, x_out, stream);
+    if (c.tq == 256) launch<4, 2, true, 8>(gw, w, stream);
+    else if (c.tp == 256) launch<4, 1, true, 4>(gw, w, stream);
+    else launch<2, 2, true, 4>(gw, w, stream);
   }
   const maestro_status st = launch_status();
   if (st != MAESTRO_OK || c.splits == 1) return st;

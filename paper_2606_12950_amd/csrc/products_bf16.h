@@ -24,7 +24,7 @@ namespace {
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;         // of a workgroup of four wavefronts
 
 struct Product {
   const __bf16* p;                   // P and Q and their leading dimensions (elements)
@@ -190,9 +190,9 @@ __device__ __forceinline__ void wait_own() {
 }
 
 // One operand of a tile: T rows (p or q), kTurned: rows contiguous in memory instead of k.
-template <int T, int kDepth, bool kTurned>
+template <int T, int kDepth, bool kTurned, int kWaves = 4>
 struct Operand {
-  static constexpr int kLoads = T * kDepth / 2048;          // 1 KB loads of a wavefront and stage
+  static constexpr int kLoads = T * kDepth / (512 * kWaves);      // 1 KB loads of a wavefront and stage
   static constexpr int kUnits = kDepth / 8;                 // k contiguous: 16-byte units of a row
   static constexpr int kRows = 64 / kUnits;                 // k contiguous: rows of a load
   uint32_t off[kLoads];                                     // per lane, within the resource
@@ -273,9 +273,9 @@ struct Operand {
 // A turned operand that memory holds as codes, bytes, and for every 32 of a row a power of two. A stage's codes come through
 // registers, 16 to a unit, and are values before they lie in LDS: a value has at most eight significant bits, so bfloat16
 // holds it exactly. They are loaded two stages ahead of the products' and turned into values one ahead, a pair after a product.
-template <int T, int kDepth>
+template <int T, int kDepth, int kWaves = 4>
 struct CodesOperand {
-  static constexpr int kUnits = T * kDepth / 16 / kThreads, kRowUnits = T / 16, kRows = kThreads / kRowUnits;
+  static constexpr int kUnits = T * kDepth / 16 / (64 * kWaves), kRowUnits = T / 16, kRows = 64 * kWaves / kRowUnits;
   static constexpr int kPairs = 8 * kUnits;
   u32x4 ahead[kUnits], now[kUnits];                         // the stages being loaded and turned into values
   uint8_t ahead_exponent[kUnits];
@@ -418,9 +418,9 @@ __device__ __forceinline__ uint32_t rectify(uint32_t c) {
 // runs of 8 p (16 bytes) of one q and leaves them at their place in [32 q][32 WS p]; then 4 WS lanes take a
 // row together. Units of 16 bytes are stored at unit ^ place(q): neither access meets bank conflicts. Every
 // wavefront issues 2 WP WQ stores, whatever lies outside C: the main loop's waits count them.
-template <int WP>
+template <int WP, int kWaves = 4>
 struct Staging {
-  static constexpr int WS = WP < 4 ? 1 : 2;                 // blocks of 32 p at a time
+  static constexpr int WS = WP < 4 || kWaves > 4 ? 1 : 2;   // blocks of 32 p at a time
   static constexpr int kRowBytes = 64 * WS, kUnits = 4 * WS, kRows = 64 / kUnits;
   static constexpr int kBytes = 32 * kRowBytes;             // of a wavefront
   static __device__ __forceinline__ int place(int q) { return (q / (16 / kUnits)) & (kUnits - 1); }
@@ -433,10 +433,10 @@ __device__ __forceinline__ void in_place(Acc& acc) {
   if constexpr (WP * WQ == 16) asm volatile("" : "+a"(acc));
 }
 
-template <int WP, int WQ, class Out, class Acc>
+template <int WP, int WQ, int kWaves, class Out, class Acc>
 __device__ __forceinline__ void store_rows(const Out& out, const Product& g, const Item& t, unsigned char* staging, int64_t q0,
                                            int64_t p0, int lane, Acc (&acc)[WP][WQ]) {
-  using S = Staging<WP>;
+  using S = Staging<WP, kWaves>;
   constexpr int kStores = 32 / S::kRows;                    // of one q block and WS p blocks
   const int r = lane & 31, h = lane >> 5;
   const int row0 = lane / S::kUnits, unit0 = lane % S::kUnits;
@@ -512,12 +512,12 @@ __device__ __forceinline__ void store_rows(const Out& out, const Product& g, con
 // A wavefront's part of C from sums of 8-bit products: fma(sum * scale_q, scale_p, bias), not below `least` (a NaN stays one).
 // `place`: the biases and, kPlace / 2 further, the scales of the wavefront's 32 WP p. bfloat16 by way of LDS as above; float32
 // straight from the lanes, eight values (32 bytes) of a row each, in stores that the main loop's waits do not count.
-template <int WP, int WQ, class Out>
+template <int WP, int WQ, int kWaves, class Out>
 __device__ __forceinline__ void store_scaled(const Out& out, const Product& g, const Item& t, unsigned char* staging, int64_t q0,
                                              int64_t p0, int lane, i32x16 (&acc)[WP][WQ], const float* place, int scales) {
   typedef typename Out::type T;
   constexpr bool kStaged = std::is_same<T, __bf16>::value;
-  using S = Staging<WP>;
+  using S = Staging<WP, kWaves>;
   constexpr int kStores = 32 / S::kRows;
   const int r = lane & 31, h = lane >> 5;
   const int row0 = lane / S::kUnits, unit0 = lane % S::kUnits;
@@ -595,29 +595,31 @@ constexpr bool staged() {
 }
 
 // Sizes of a product's tile, and its LDS.
-template <int WP, int WQ, int kDepth, int kBufs, class Out>
+template <int WP, int WQ, int kDepth, int kBufs, class Out, int kWaves = 4>
 struct Tile {
-  static constexpr int TP = 64 * WP, TQ = 64 * WQ;          // four wavefronts
+  static constexpr int TP = 64 * WP, TQ = 16 * kWaves * WQ;       // two wavefronts by two, or by four
   static constexpr int kStage = (TP + TQ) * 2 * kDepth;
   static constexpr bool kStores = staged<Out>();            // by way of LDS
   static constexpr int kBiasLoads = Out::kBias ? (WP + 1) / 2 : 0;            // and as many of scale_p
   static constexpr int kEpilogueLoads = kBiasLoads * (Out::kInt8 ? 2 : 1);
-  static constexpr int kBiasBytes = 2 * 4 * 256 * kEpilogueLoads;             // two places for each wavefront
-  static constexpr int kBytes = kBufs * kStage + (kStores ? 4 * Staging<WP>::kBytes : 0) + kBiasBytes;
+  static constexpr int kBiasBytes = 2 * kWaves * 256 * kEpilogueLoads;             // two places for each wavefront
+  static constexpr int kBytes = kBufs * kStage + (kStores ? kWaves * Staging<WP, kWaves>::kBytes : 0) + kBiasBytes;
   // workgroups of a CU that a launch plans for, and that registers allow. LDS lets three run of the activations' 64 x 64
   // (43,008 bytes of 160 KB) and two of pair_kernel<4, 1> (81,920, the larger tile's, in all of them).
-  static constexpr int kResident = WP * WQ > 8 ? 1 : WP * WQ > 2 ? 2 : 4;
+  static constexpr int kBlocks = WP * WQ * kWaves / 4;      // of 32 x 32, a SIMD's
+  static constexpr int kResident = kBlocks > 8 ? 1 : kBlocks > 2 ? 2 : 4;
+  static constexpr int kSimdWaves = kResident * kWaves / 4;
 };
 
 // The share of workgroup `block` of `blocks` (a multiple of 8) in the tiles of `work`, products of the sizes of `g`.
-template <int WP, int WQ, int kDepth, int kBufs, bool kPT, bool kQT, class Out, class Work>
+template <int WP, int WQ, int kDepth, int kBufs, bool kPT, bool kQT, int kWaves = 4, class Out, class Work>
 __device__ __forceinline__ void product(const Product& g, const Out& out, const Work& work, unsigned char* lds, uint32_t block,
                                         uint32_t blocks) {
-  using L = Tile<WP, WQ, kDepth, kBufs, Out>;
+  using L = Tile<WP, WQ, kDepth, kBufs, Out, kWaves>;
   constexpr int NP = 2, TP = L::TP, TQ = L::TQ;
   constexpr bool kCodes = Out::kCodes;
-  constexpr int kStage = L::kStage, kPLoads = kCodes ? 0 : TP * kDepth / 2048, kHalves = kDepth / 16;
-  constexpr int kLoads = kPLoads + TQ * kDepth / 2048;
+  constexpr int kStage = L::kStage, kPLoads = kCodes ? 0 : TP * kDepth / (512 * kWaves), kHalves = kDepth / 16;
+  constexpr int kLoads = kPLoads + TQ * kDepth / (512 * kWaves);
   static_assert(!kCodes || (kBufs == 2 && kPT), "a stage's end waits for all loads");
   constexpr int kQ = TP * 2 * kDepth;                       // Q's place in a stage
   constexpr bool kSums = kQT;                               // the weights' gradient sums Q too (the biases')
@@ -630,8 +632,8 @@ __device__ __forceinline__ void product(const Product& g, const Out& out, const 
   typename Work::Way at = work.begin(block, blocks);
   if (at.done()) return;
 
-  Operand<TP, kDepth, kPT> op;
-  Operand<TQ, kDepth, kQT> oq;
+  Operand<TP, kDepth, kPT, kWaves> op;
+  Operand<TQ, kDepth, kQT, kWaves> oq;
   auto fetch_at = at;                                       // the tile being loaded, and its stages still to load
   int64_t fetch_left = 0;
   auto open = [&]() {
@@ -661,7 +663,7 @@ __device__ __forceinline__ void product(const Product& g, const Out& out, const 
 
   // this wavefront's biases (and scales) of a tile, into LDS a tile ahead of their use; two places in turn
   constexpr int kPlace = 64 * kEpilogueLoads;
-  float* biases = reinterpret_cast<float*>(lds + kBufs * kStage + (L::kStores ? 4 * Staging<WP>::kBytes : 0)) + wave * 2 * kPlace;
+  float* biases = reinterpret_cast<float*>(lds + kBufs * kStage + (L::kStores ? kWaves * Staging<WP, kWaves>::kBytes : 0)) + wave * 2 * kPlace;
   int parity = 0;
   auto fetch_biases = [&](const typename Work::Way& j) {
     if constexpr (Out::kBias) {
@@ -684,7 +686,7 @@ __device__ __forceinline__ void product(const Product& g, const Out& out, const 
   fetch_biases(at);
 
   // P's codes: a stage further ahead than Q
-  CodesOperand<TP, kDepth> codes;
+  CodesOperand<TP, kDepth, kWaves> codes;
   auto codes_at = at;
   int64_t codes_left = 0;
   auto open_codes = [&]() {
@@ -856,9 +858,9 @@ __device__ __forceinline__ void product(const Product& g, const Out& out, const 
     if (Out::kBias && t.stages < kBufs) wait_own<0>();      // else a stage's wait has covered the next biases
     const int64_t qw = t.q0 + 32 * WQ * wq, pw = t.p0 + 32 * WP * wp;        // this wavefront's part
     if constexpr (!kSums) {
-      unsigned char* staging = lds + kBufs * kStage + wave * Staging<WP>::kBytes;
-      if constexpr (Out::kInt8) store_scaled<WP, WQ>(out, g, t, staging, qw, pw, lane, acc, place, 64 * kBiasLoads);
-      else store_rows<WP, WQ>(out, g, t, staging, qw, pw, lane, acc);
+      unsigned char* staging = lds + kBufs * kStage + wave * Staging<WP, kWaves>::kBytes;
+      if constexpr (Out::kInt8) store_scaled<WP, WQ, kWaves>(out, g, t, staging, qw, pw, lane, acc, place, 64 * kBiasLoads);
+      else store_rows<WP, WQ, kWaves>(out, g, t, staging, qw, pw, lane, acc);
     } else {
       const int r = lane & 31, h = lane >> 5;
       float* gw = out.weights(g, t);
