@@ -69,10 +69,15 @@ def load():
 # checked and made here only where that takes no part in it (None).
 
 
-def _here():
+# what torch.cuda.current_device() and current_stream().cuda_stream come to, where this torch gives it away: looked up once, since
+# a small call's time is the host's
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+def _here() -> int:
     """The current device's number."""
-    get = getattr(torch._C, "_cuda_getDevice", None)
-    return get() if get else torch.cuda.current_device()
+    return _device()
 
 
 def _current(**tensors: Optional[torch.Tensor]) -> None:
@@ -135,7 +140,8 @@ def layer_grouped(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor, off
     the device. Rows of no group are left as they are in ``out`` (without one they hold whatever the memory held)."""
     lib = load()
     if out is None and stream is None:
-        got = _tensors.layer_grouped(x, weight, bias, offsets, relu, _stream(None), _here())
+        here = _here()
+        got = _tensors.layer_grouped(x, weight, bias, offsets, relu, _raw_stream(here), here)
         if got is not None:
             return got
     dt, n, groups, i, o = _grouped_shapes(x, weight, offsets)
@@ -173,7 +179,8 @@ def layer_grouped_grad(x: torch.Tensor, weight: torch.Tensor, g_z: torch.Tensor,
     input's. Rows of no group take no part, and theirs of ``out.x`` are left as they are."""
     lib = load()
     if out is None and workspace is None and stream is None:
-        got = _tensors.layer_grouped_grad(x, weight, g_z, offsets, relu_input, want_x, _stream(None), _here())
+        here = _here()
+        got = _tensors.layer_grouped_grad(x, weight, g_z, offsets, relu_input, want_x, _raw_stream(here), here)
         if got is not None:
             return LayerGrad._make(got)
     dt, n, groups, i, o = _grouped_shapes(x, weight, offsets)
@@ -196,7 +203,8 @@ def quantize_rows(x: torch.Tensor, out: Optional[Quantized] = None, stream=None)
     magnitude over 127. Weights [d_out][d_in] so quantised have a scale for each output channel."""
     lib = load()
     if out is None and stream is None:
-        got = _tensors.quantize_rows(x, _stream(None), _here())
+        here = _here()
+        got = _tensors.quantize_rows(x, _raw_stream(here), here)
         if got is not None:
             return Quantized._make(got)
     n, d = _matrix(x, "x", torch.float32, torch.bfloat16)
@@ -218,7 +226,8 @@ def layer_int8(x: Quantized, weight: Quantized, bias: torch.Tensor, relu: bool =
     lib = load()
     dt = _code(dtype, "dtype")
     if out is None and stream is None:
-        got = _tensors.layer_int8(x.codes, x.scale, weight.codes, weight.scale, bias, relu, dt, _stream(None), _here())
+        here = _here()
+        got = _tensors.layer_int8(x.codes, x.scale, weight.codes, weight.scale, bias, relu, dt, _raw_stream(here), here)
         if got is not None:
             return got
     n, i = _matrix(x.codes, "x.codes", torch.int8)
@@ -253,7 +262,8 @@ def pack_activations(x: torch.Tensor, rectified: bool = False, out: Optional[Pac
     ``rectified``: unsigned codes, 0 where x is not positive and at least 1 where it is."""
     lib = load()
     if out is None and stream is None:
-        got = _tensors.pack(x, rectified, _stream(None), _here())
+        here = _here()
+        got = _tensors.pack(x, rectified, _raw_stream(here), here)
         if got is not None:
             return Packed._make(got)
     n, d = _matrix(x, "x", torch.float32, torch.bfloat16)
@@ -275,7 +285,8 @@ def unpack_activations(packed: Packed, dtype: torch.dtype = torch.bfloat16, out:
     lib = load()
     dt = _code(dtype, "dtype")
     if out is None and stream is None:
-        got = _tensors.unpack(packed.codes, packed.exponents, dt, _stream(None), _here())
+        here = _here()
+        got = _tensors.unpack(packed.codes, packed.exponents, dt, _raw_stream(here), here)
         if got is not None:
             return got
     n, d, rectified = _packed_shapes(packed)
@@ -295,7 +306,8 @@ def layer_grad_packed(packed: Packed, weight: torch.Tensor, g_z: torch.Tensor, r
     ``unpack_activations`` gives. ``relu_input`` needs rectified (uint8) codes."""
     lib = load()
     if out is None and workspace is None and stream is None:
-        got = _tensors.layer_grad_packed(packed.codes, packed.exponents, weight, g_z, relu_input, want_x, _stream(None), _here())
+        here = _here()
+        got = _tensors.layer_grad_packed(packed.codes, packed.exponents, weight, g_z, relu_input, want_x, _raw_stream(here), here)
         if got is not None:
             return LayerGrad._make(got)
     n, i, rectified = _packed_shapes(packed)

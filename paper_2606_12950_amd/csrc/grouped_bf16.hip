@@ -88,7 +88,26 @@ __global__ __launch_bounds__(64 * kWaves, (Tile<WP, WQ, kDepth, kBufs, GroupedWe
   const int tiles = (int)((g.nq + L::TQ - 1) / L::TQ) * g.p_tiles;
   product<WP, WQ, kDepth, kBufs, true, true, kWaves>(g, out, GroupedSums<L::TP, L::TQ, kDepth, kUnits>{{table, tiles, (int)g.k_split}, g}, lds, blockIdx.x,
                                                 gridDim.x);
-  if (alone) clear_empty_groups(table, out.gw, g.np * g.nq, out.gb, (int)g.nq);
+  if (alone) clear_empty_groups(table, out.gw, g.np * g.nq, out.gb, (int)g.nq, blockIdx.x, gridDim.x);
+}
+
+// Both gradients in one launch, in 64 x 64 tiles: the first `blocks` workgroups make the input's, the others the weights'.
+__global__ __launch_bounds__(kThreads, 4) void pair_kernel(Product gx, InputGrad x, uint32_t blocks, Product gw, GroupedWeightGrad w,
+                                                           const int64_t* offsets, int32_t n_groups, int32_t n, bool alone) {
+  using X = Tile<1, 1, 64, 2, InputGrad>;
+  using W = Tile<1, 1, 64, 2, GroupedWeightGrad>;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[X::kBytes > W::kBytes ? X::kBytes : W::kBytes];
+  GroupTable table;
+  if (blockIdx.x < blocks) {
+    table.build<kTiles>(offsets, n_groups, n, X::TQ);
+    product<1, 1, 64, 2, true, false>(gx, x, GroupedRows<X::TP, X::TQ, 64>{{table, gx.p_tiles}, gx}, lds, blockIdx.x, blocks);
+    return;
+  }
+  table.build<kTiles>(offsets, n_groups, n, (int)gw.k_split);
+  const int tiles = (int)((gw.nq + W::TQ - 1) / W::TQ) * gw.p_tiles;
+  product<1, 1, 64, 2, true, true>(gw, w, GroupedSums<W::TP, W::TQ, 64, kTiles>{{table, tiles, (int)gw.k_split}, gw}, lds,
+                                   blockIdx.x - blocks, gridDim.x - blocks);
+  if (alone) clear_empty_groups(table, w.gw, gw.np * gw.nq, w.gb, (int)gw.nq, blockIdx.x - blocks, gridDim.x - blocks);
 }
 
 uint32_t blocks_of(int64_t items, int64_t resident) {
@@ -106,12 +125,18 @@ void launch_tiles(Product g, const Out& out, const int64_t* offsets, int32_t n_g
 
 // Tile by how many there are, as for a layer of one group. 256 x 256 ones by eight wavefronts, two to a SIMD, or by four: the layer
 // with eight 546 us, four 544 (262,139 x 1024 -> 1024, 16 groups); the input's gradient, whose mask wants registers, 612 and 575.
+int tile_of(int64_t np, int64_t n) {
+  if (np > 128 && cdiv(np, 256) * (n / 256) >= 2 * kCus) return 256;
+  return cdiv(np, 128) * (n / 128) >= kCus ? 128 : 64;
+}
+
 template <bool kPT, class Out>
 void launch_rows(const Product& g, const Out& out, const int64_t* offsets, int32_t n_groups, int64_t n, hipStream_t stream) {
-  if (g.np > 128 && cdiv(g.np, 256) * (n / 256) >= 2 * kCus) {
+  const int tile = tile_of(g.np, n);
+  if (tile == 256) {
     if constexpr (kPT) launch_tiles<4, 4, kPT, 4>(g, out, offsets, n_groups, n, stream);
     else launch_tiles<4, 2, kPT, 8>(g, out, offsets, n_groups, n, stream);
-  } else if (cdiv(g.np, 128) * (n / 128) >= kCus) {
+  } else if (tile == 128) {
     launch_tiles<2, 2, kPT, 4>(g, out, offsets, n_groups, n, stream);
   } else {
     launch_tiles<1, 1, kPT, 4>(g, out, offsets, n_groups, n, stream);
@@ -152,6 +177,15 @@ void launch_sums(Product g, const GroupedWeightGrad& out, const int64_t* offsets
   kernel<<<blocks, 64 * kWaves, 0, stream>>>(g, out, offsets, n_groups, n, alone);
 }
 
+void launch_pair(Product gx, const InputGrad& x, Product gw, const GroupedWeightGrad& w, const int64_t* offsets, int32_t n_groups,
+                 int32_t n, bool alone, hipStream_t stream) {
+  gx.p_tiles = (int32_t)cdiv(gx.np, 64);
+  gw.p_tiles = (int32_t)cdiv(gw.np, 64);
+  const uint32_t blocks = blocks_of((n / 64 + n_groups) * gx.p_tiles, 4);
+  const uint32_t more = blocks_of((n / gw.k_split + n_groups) * gw.p_tiles * cdiv(gw.nq, 64), 4);
+  pair_kernel<<<blocks + more, kThreads, 0, stream>>>(gx, x, blocks, gw, w, offsets, n_groups, n, alone);
+}
+
 }  // namespace
 
 maestro_status launch_layer_grouped_bf16(int64_t n, int32_t n_groups, int32_t d_in, int32_t d_out, const void* x,
@@ -175,15 +209,19 @@ maestro_status launch_grouped_grad_bf16(int64_t n, int32_t n_groups, int32_t d_i
   const __bf16 *xb = static_cast<const __bf16*>(x), *gz = static_cast<const __bf16*>(g_z);
   const Cut c = cut_of(n, n_groups, d_in, d_out);
   float *gw_parts = static_cast<float*>(workspace), *gb_parts = gw_parts + c.most * size;
-  if (g_x) {
-    const Product gx{static_cast<const __bf16*>(weight), gz, d_in, d_out, d_in, n, d_out, d_out, 1, 0, 0};
-    launch_rows<true>(gx, InputGrad{xb, static_cast<__bf16*>(g_x), relu_input}, offsets, n_groups, n, stream);
-  }
+  const Product gx{static_cast<const __bf16*>(weight), gz, d_in, d_out, d_in, n, d_out, d_out, 1, 0, 0};
+  const InputGrad x_out{xb, static_cast<__bf16*>(g_x), relu_input};
   const Product gw{xb, gz, d_in, d_out, d_in, d_out, n, c.k_split, 1, 0, 0};
   const GroupedWeightGrad out{g_weight, g_bias, gw_parts, gb_parts, 1};
   const bool alone = n <= c.k_split;
-  auto sums = c.tp == 64 ? launch_sums<1, 1, 64, 2, 4> : c.tq == 256 ? launch_sums<4, 2, 32, 4, 8> : c.tp == 256 ? launch_sums<4, 1, 64, 2, 4> : launch_sums<2, 2, 64, 2, 4>;
-  sums(gw, out, offsets, n_groups, (int32_t)n, c.by_group, alone, stream);
+  if (g_x && c.tp == 64 && tile_of(d_in, n) == 64) {
+    launch_pair(gx, x_out, gw, out, offsets, n_groups, (int32_t)n, alone, stream);
+  } else {
+    if (g_x) launch_rows<true>(gx, x_out, offsets, n_groups, n, stream);
+    auto sums = c.tp == 64 ? launch_sums<1, 1, 64, 2, 4> : c.tq == 256 ? launch_sums<4, 2, 32, 4, 8>
+              : c.tp == 256 ? launch_sums<4, 1, 64, 2, 4> : launch_sums<2, 2, 64, 2, 4>;
+    sums(gw, out, offsets, n_groups, (int32_t)n, c.by_group, alone, stream);
+  }
   const maestro_status st = launch_status();
   if (st != MAESTRO_OK || alone) return st;
   return launch_join_groups(n, n_groups, offsets, c.k_split, c.by_group, gw_parts, g_weight, size, gb_parts, g_bias, d_out, stream);

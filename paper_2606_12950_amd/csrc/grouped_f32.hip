@@ -77,7 +77,24 @@ __global__ __launch_bounds__(kThreads, 2) void sums_kernel(Product g, GroupedWei
   table.build<kUnits>(offsets, n_groups, n, (int)g.k_split);
   const int tiles = (int)((g.nq + 64 * W - 1) / (64 * W) * g.p_tiles);
   product<W, true, true>(g, out, GroupedSums<64 * W, kUnits>{{table, tiles, (int)g.k_split}, g}, lds, blockIdx.x, gridDim.x);
-  if (alone) clear_empty_groups(table, out.gw, g.np * g.nq, out.gb, (int)g.nq);
+  if (alone) clear_empty_groups(table, out.gw, g.np * g.nq, out.gb, (int)g.nq, blockIdx.x, gridDim.x);
+}
+
+// Both gradients in one launch, in 64 x 64 tiles: the first `blocks` workgroups make the input's, the others the weights'.
+__global__ __launch_bounds__(kThreads, 2) void pair_kernel(Product gx, InputGrad x, uint32_t blocks, Product gw, GroupedWeightGrad w,
+                                                           const int64_t* offsets, int32_t n_groups, int32_t n, bool alone) {
+  __shared__ __attribute__((aligned(16))) Lds<1> lds;
+  GroupTable table;
+  if (blockIdx.x < blocks) {
+    table.build<kTiles>(offsets, n_groups, n, 64);
+    product<1, true, false>(gx, x, GroupedRows<64>{{table, (int)gx.p_tiles}, gx}, lds, blockIdx.x, blocks);
+    return;
+  }
+  table.build<kTiles>(offsets, n_groups, n, (int)gw.k_split);
+  const int tiles = (int)((gw.nq + 63) / 64 * gw.p_tiles);
+  product<1, true, true>(gw, w, GroupedSums<64, kTiles>{{table, tiles, (int)gw.k_split}, gw}, lds, blockIdx.x - blocks,
+                         gridDim.x - blocks);
+  if (alone) clear_empty_groups(table, w.gw, gw.np * gw.nq, w.gb, (int)gw.nq, blockIdx.x - blocks, gridDim.x - blocks);
 }
 
 // Group blockIdx.y's units added in order, a quad of values a thread; zeros where it has none.
@@ -176,16 +193,22 @@ maestro_status launch_grouped_grad_f32(int64_t n, int32_t n_groups, int32_t d_in
   if (n == 0) return launch_join_groups(0, n_groups, offsets, 1, true, nullptr, g_weight, size, nullptr, g_bias, d_out, stream);
   const Cut c = cut_of(n, n_groups, d_in, d_out);
   float *gw_parts = static_cast<float*>(workspace), *gb_parts = gw_parts + c.most * size;
-  if (g_x) {
-    const Product gx{{weight, d_in}, {g_z, d_out}, d_in, n, d_out, d_out, 1, 0, 0};
-    const InputGrad out{x, g_x, relu_input};
-    if (wide(d_in, n)) launch_rows<2, true>(gx, out, offsets, n_groups, n, stream);
-    else launch_rows<1, true>(gx, out, offsets, n_groups, n, stream);
-  }
-  const Product gw{{x, d_in}, {g_z, d_out}, d_in, d_out, n, c.k_split, 1, 0, 0};
+  Product gx{{weight, d_in}, {g_z, d_out}, d_in, n, d_out, d_out, 1, 0, 0};
+  const InputGrad x_out{x, g_x, relu_input};
+  Product gw{{x, d_in}, {g_z, d_out}, d_in, d_out, n, c.k_split, 1, 0, 0};
   const GroupedWeightGrad out{g_weight, g_bias, gw_parts, gb_parts};
   const bool alone = n <= c.k_split;
-  (c.wide ? launch_sums<2> : launch_sums<1>)(gw, out, offsets, n_groups, (int32_t)n, c.by_group, alone, stream);
+  if (g_x && c.by_group && !c.wide && !wide(d_in, n)) {
+    gx.p_tiles = cdiv(d_in, 64);
+    gw.p_tiles = cdiv(d_in, 64);
+    const int64_t rows = (n / 64 + n_groups) * gx.p_tiles, sums = c.most * gw.p_tiles * cdiv(d_out, 64);
+    const uint32_t blocks = (uint32_t)(rows < 65536 ? rows : 65536), more = (uint32_t)(sums < 65536 ? sums : 65536);
+    pair_kernel<<<blocks + more, kThreads, 0, stream>>>(gx, x_out, blocks, gw, out, offsets, n_groups, (int32_t)n, alone);
+  } else {
+    if (g_x && wide(d_in, n)) launch_rows<2, true>(gx, x_out, offsets, n_groups, n, stream);
+    else if (g_x) launch_rows<1, true>(gx, x_out, offsets, n_groups, n, stream);
+    (c.wide ? launch_sums<2> : launch_sums<1>)(gw, out, offsets, n_groups, (int32_t)n, c.by_group, alone, stream);
+  }
   const maestro_status st = launch_status();
   if (st != MAESTRO_OK || alone) return st;
   return launch_join_groups(n, n_groups, offsets, c.k_split, c.by_group, gw_parts, g_weight, size, gb_parts, g_bias, d_out, stream);

@@ -171,12 +171,13 @@ struct GroupedSumsWay {
   }
 };
 
-// Zeros for the groups without rows, by all workgroups.
-__device__ __forceinline__ void clear_empty_groups(const GroupTable& table, float* gw, int64_t size, float* gb, int d_out) {
+// Zeros for the groups without rows, by `blocks` workgroups.
+__device__ __forceinline__ void clear_empty_groups(const GroupTable& table, float* gw, int64_t size, float* gb, int d_out,
+                                                   uint32_t block, uint32_t blocks) {
   const int64_t quads = size / 4, all = quads + d_out / 4;
   for (int g = 0; g < table.n_groups; ++g) {
     if (table.first_unit(g + 1) != table.first_unit(g)) continue;
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < all; i += (int64_t)gridDim.x * blockDim.x)
+    for (int64_t i = (int64_t)block * blockDim.x + threadIdx.x; i < all; i += (int64_t)blocks * blockDim.x)
       (i < quads ? reinterpret_cast<float4*>(gw) + g * quads + i : reinterpret_cast<float4*>(gb) + g * (all - quads) + (i - quads))[0] =
           make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   }

@@ -54,6 +54,7 @@ def stub(monkeypatch):
     monkeypatch.setattr(_layers, "_tensors", _Tensors())
     monkeypatch.setattr(_layers, "_matrix", matrix)
     monkeypatch.setattr(_layers, "_here", lambda: -1)
+    monkeypatch.setattr(_layers, "_raw_stream", lambda device: 0)
     return lib
 
 
