@@ -44,7 +44,7 @@ MAESTRO_API maestro_status maestro_layer_grouped(int64_t n, int32_t n_groups, in
 /* Gradients of a grouped layer z given g_z [n][d_out] (of z, in `dtype`), as maestro_layer_grad's for every group:
  *   g_weight (out) [n_groups][d_out][d_in] float32, g_bias (out) [n_groups][d_out] float32: of empty groups zeros
  *   g_x      (out) [n][d_in] in `dtype`, or NULL where it is not wanted; rows of no group are left as they are
- * Workspace: maestro_layer_grouped_grad_workspace() bytes. */
+ * Workspace: maestro_layer_grouped_grad_workspace() bytes (0 for few rows: NULL is then allowed). */
 MAESTRO_API size_t maestro_layer_grouped_grad_workspace(int64_t n, int32_t n_groups, int32_t d_in, int32_t d_out, int32_t dtype);
 MAESTRO_API maestro_status maestro_layer_grouped_grad(int64_t n, int32_t n_groups, int32_t d_in, int32_t d_out, int32_t dtype,
                              const void* x, const void* weight, const void* g_z, const int64_t* offsets, int32_t relu_input,
@@ -81,7 +81,7 @@ MAESTRO_API maestro_status maestro_unpack_activations(int64_t n, int32_t d, int3
 
 /* maestro_layer_grad for an input kept as codes and exponents: its g_weight, g_bias and g_x are those of the values that
  * maestro_unpack_activations gives. relu_input needs rectified codes (0 elsewhere is MAESTRO_ERR_INVALID_ARG) and
- * makes g_x 0 where the code is 0. Workspace: maestro_layer_grad_packed_workspace() bytes. */
+ * makes g_x 0 where the code is 0. Workspace: maestro_layer_grad_packed_workspace() bytes (0 for few rows). */
 MAESTRO_API size_t maestro_layer_grad_packed_workspace(int64_t n, int32_t d_in, int32_t d_out, int32_t dtype);
 MAESTRO_API maestro_status maestro_layer_grad_packed(int64_t n, int32_t d_in, int32_t d_out, int32_t dtype, const void* codes,
                              const uint8_t* exponents, int32_t rectified, const void* weight, const void* g_z,

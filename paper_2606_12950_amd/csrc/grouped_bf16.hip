@@ -198,7 +198,8 @@ maestro_status launch_layer_grouped_bf16(int64_t n, int32_t n_groups, int32_t d_
 
 size_t grouped_grad_bf16_workspace_bytes(int64_t n, int32_t n_groups, int32_t d_in, int32_t d_out) {
   if (n == 0) return 0;
-  return sizeof(float) * (size_t)(cut_of(n, n_groups, d_in, d_out).most * ((int64_t)d_in + 1) * d_out);
+  const Cut c = cut_of(n, n_groups, d_in, d_out);
+  return n <= c.k_split ? 0 : sizeof(float) * (size_t)(c.most * ((int64_t)d_in + 1) * d_out);
 }
 
 maestro_status launch_grouped_grad_bf16(int64_t n, int32_t n_groups, int32_t d_in, int32_t d_out, const void* x,

@@ -53,7 +53,7 @@ def test_grouped_without_rows(lib):
     assert _grouped(lib, n=0, x=None, y=None, off=None) == INVALID
 
 
-def _grouped_grad(lib, n=4, g=3, i=32, o=16, dtype=BF16, x=A, w=A, gz=A, off=A, gx=A, gw=A, gb=A, ws=A, size=1 << 40):
+def _grouped_grad(lib, n=20000, g=3, i=32, o=16, dtype=BF16, x=A, w=A, gz=A, off=A, gx=A, gw=A, gb=A, ws=A, size=1 << 40):
     return lib.maestro_layer_grouped_grad(n, g, i, o, dtype, x, w, gz, off, 0, gx, gw, gb, ws, size, None)
 
 
@@ -69,11 +69,11 @@ def test_grouped_grad_refuses(lib, bad, status):
 def test_grouped_grad_workspace(lib):
     ws = lib.maestro_layer_grouped_grad_workspace
     for dtype in (F32, BF16):
-        for n in (1, 300, 262139, 1 << 30):
+        for n in (20000, 262139, 1 << 30):
             need = ws(n, 3, 32, 16, dtype)
             assert need >= 4 * 33 * 16 and need % 4 == 0
             assert _grouped_grad(lib, n=n, dtype=dtype, size=need - 1) == WORKSPACE
-        assert ws(0, 3, 32, 16, dtype) == 0
+        assert ws(0, 3, 32, 16, dtype) == ws(100, 3, 32, 16, dtype) == 0          # no group has more than one share
     assert ws((1 << 31) - (1 << 16) + 1, 3, 32, 16, BF16) == 0
     assert _grouped(lib, n=(1 << 31) - (1 << 16) + 1) == _grouped_grad(lib, n=(1 << 31) - (1 << 16) + 1) == UNSUPPORTED
     assert _grouped(lib, n=1 << 30, i=16384) == UNSUPPORTED
