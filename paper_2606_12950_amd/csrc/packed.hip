@@ -49,14 +49,13 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(uint32_t rows, uint32_t 
   if (!there) return;
   const int e = exponent_of<kRectified>(most);
   const float inverse = inverse_step(e == 255 ? 1 : e);
-  int q[8];
+  float t[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    q[j] = (int)__builtin_rintf(v[j] * inverse);
-    if constexpr (kRectified) q[j] = v[j] > 0.0f && q[j] < 1 ? 1 : q[j];
-    if (e == 255) q[j] = 0;
+    t[j] = fmaf(v[j], inverse, kRounder);                   // the product is exact
+    if constexpr (kRectified) t[j] = fmaxf(t[j], v[j] > 0.0f ? kRounder + 1.0f : kRounder);
   }
-  *reinterpret_cast<uint2*>(codes + (int64_t)row * d + unit * 8) = bytes8(q);
+  *reinterpret_cast<uint2*>(codes + (int64_t)row * d + unit * 8) = e == 255 ? make_uint2(0, 0) : low_bytes8(t);
   if (unit % 4 == 0) exponents[(int64_t)row * (padded / 4) + unit / 4] = (uint8_t)e;
 }
 

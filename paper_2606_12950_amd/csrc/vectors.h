@@ -51,6 +51,30 @@ __device__ __forceinline__ uint32_t largest8(const float (&v)[8]) {
   }
   return m;
 }
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t largest8(const Vector8<float>& w) {
+  float v[8];
+  w.get(v);
+  return largest8(v);
+}
+__device__ __forceinline__ uint32_t largest8(const Vector8<__bf16>& w) {      // pairs at a time
+  auto size = [](uint32_t u) { return __builtin_bit_cast(u16x2, u & 0x7FFF7FFFu); };
+  const u16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(size(w.w.x), size(w.w.y)),
+                                            __builtin_elementwise_max(size(w.w.z), size(w.w.w)));
+  return (uint32_t)(m.x > m.y ? m.x : m.y) << 16;
+}
+
+// x + kRounder is x rounded to a whole number, ties to the even one, in the sum's low bits (|x| < 2^22): its lowest byte is a code.
+constexpr float kRounder = 12582912.0f;      // 1.5 * 2^23
+
+// The lowest bytes of eight words.
+__device__ __forceinline__ uint2 low_bytes8(const float (&t)[8]) {
+  auto u = [&](int e) { return __float_as_uint(t[e]); };
+  uint2 b;
+  b.x = __builtin_amdgcn_perm(u(1), u(0), 0x0C0C0400u) | __builtin_amdgcn_perm(u(3), u(2), 0x04000C0Cu);
+  b.y = __builtin_amdgcn_perm(u(5), u(4), 0x0C0C0400u) | __builtin_amdgcn_perm(u(7), u(6), 0x04000C0Cu);
+  return b;
+}
 
 // Eight whole numbers as bytes.
 __device__ __forceinline__ uint2 bytes8(const int (&q)[8]) {
