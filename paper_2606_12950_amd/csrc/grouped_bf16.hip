@@ -144,7 +144,7 @@ void launch_rows(const Product& g, const Out& out, const int64_t* offsets, int32
 }
 
 // Tile of the weights' gradient and rows of a unit, as for a layer of one group. by_group: too few rows for a unit of them
-// in every workgroup; then 64 x 64 tiles where four to a CU hold them all. Measured (us, 64 x 64 / 256 x 64 or 128 x 128): 300 rows in 5
+// in every workgroup. 64 x 64 tiles and units of 512 rows of a group where four to a CU hold them all. Measured (us, 64 x 64 / 256 x 64 or 128 x 128): 300 rows in 5
 // groups 256 -> 512 5.8 / 7.9, 4,000 in 4 256 -> 256 12.1 / 15.8, 8,000 in 16 512 -> 64 10.3 / 14.0, 20,000 in 60 128 -> 128 9.8 / 12.8.
 struct Cut {
   int32_t tp, tq;
@@ -162,7 +162,12 @@ Cut cut_of(int64_t n, int64_t n_groups, int64_t d_in, int64_t d_out) {
   if (splits < 1) splits = 1;
   c.k_split = cdiv(cdiv(n, splits), 64) * 64;
   c.most = n / c.k_split + n_groups;
-  if (c.by_group && c.most * cdiv(d_in, 64) * cdiv(d_out, 64) <= 4 * kCus) c.tp = c.tq = 64;
+  if ((n / 512 + n_groups) * cdiv(d_in, 64) * cdiv(d_out, 64) <= 4 * kCus) {
+    c.tp = c.tq = 64;
+    c.by_group = true;
+    c.k_split = cdiv(cdiv(n, cdiv(n, 512)), 64) * 64;
+    c.most = n / c.k_split + n_groups;
+  }
   return c;
 }
 

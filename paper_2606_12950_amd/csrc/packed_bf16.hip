@@ -17,7 +17,7 @@ __global__ __launch_bounds__(64 * kWaves, (Tile<WP, WQ, 64, 2, Out, kWaves>::kSi
 
 // Both gradients in one launch: the first `blocks` workgroups make the input's, in 64 x 64 tiles, the others the weights'.
 template <int WP, int WQ>
-__global__ __launch_bounds__(kThreads, 2) void pair_kernel(Product gx, CodesInputGrad x, uint32_t blocks, Product gw, CodesWeightGrad w) {
+__global__ __launch_bounds__(kThreads, (WP * WQ == 1 ? 4 : 2)) void pair_kernel(Product gx, CodesInputGrad x, uint32_t blocks, Product gw, CodesWeightGrad w) {
   using X = Tile<1, 1, 64, 2, CodesInputGrad>;
   using W = Tile<WP, WQ, 64, 2, CodesWeightGrad>;
   __shared__ __attribute__((aligned(16))) unsigned char lds[X::kBytes > W::kBytes ? X::kBytes : W::kBytes];
@@ -47,7 +47,9 @@ void launch_pair(Product gx, const CodesInputGrad& x, Product gw, const CodesWei
   pair_kernel<WP, WQ><<<blocks + more, kThreads, 0, stream>>>(gx, x, blocks, gw, w);
 }
 
-// As for the gradients of an input in bfloat16.
+// As for the gradients of an input in bfloat16, and for little work 64 x 64 tiles of the weights' gradient, with splits of 256 rows
+// or more, where four to a CU hold them all. Measured (us, both gradients, 64 x 64 with 256 / 512 rows / the larger tiles): 300 x 256 -> 512
+// 9.1 / 6.8 (one split) / 11.7 (weights), 1,000 x 1024 -> 64 9.3 / 11.5, 4,000 x 256 -> 256 11.5 / 12.8, 30,000 x 64 -> 128 13.8 / 15.0 / 17.0 (weights).
 int tile_of(int64_t np, int64_t nq) {
   if (np > 128 && cdiv(np, 256) * cdiv(nq, 256) >= 2 * kCus) return 256;
   return cdiv(np, 128) * cdiv(nq, 128) >= kCus ? 128 : 64;
@@ -62,9 +64,11 @@ Cut cut_of(int64_t n, int64_t d_in, int64_t d_out) {
   Cut c;
   c.tp = d_in > 128 ? 256 : 128;
   c.tq = c.tp == 128 ? 128 : d_out > 128 && n >= 131072 ? 256 : 64;
-  const int64_t tiles = cdiv(d_in, c.tp) * cdiv(d_out, c.tq), resident = c.tq == 256 ? 1 : 2;
-  int64_t splits = kCus * resident / tiles;
-  if (splits > cdiv(n, 512)) splits = cdiv(n, 512);
+  int64_t tiles = cdiv(d_in, c.tp) * cdiv(d_out, c.tq), most = kCus * (c.tq == 256 ? 1 : 2), least = 512;
+  const int64_t small = cdiv(d_in, 64) * cdiv(d_out, 64), few = n <= 512 ? 512 : 256;
+  if (small * cdiv(n, few) <= 4 * kCus) c.tp = c.tq = 64, tiles = small, most = 4 * kCus, least = few;
+  int64_t splits = most / tiles;
+  if (splits > cdiv(n, least)) splits = cdiv(n, least);
   if (splits < 1) splits = 1;
   c.k_split = cdiv(cdiv(n, splits), 64) * 64;
   c.splits = cdiv(n, c.k_split);
@@ -100,12 +104,14 @@ maestro_status launch_grad_packed_bf16(int64_t n, int32_t d_in, int32_t d_out, c
   const Product gx{static_cast<const __bf16*>(weight), gz, d_in, d_out, d_in, n, d_out, d_out, 1, 0, 0};
   const CodesInputGrad x_out{c8, static_cast<__bf16*>(g_x), relu_input};
   if (g_x && tile_of(d_in, n) == 64) {
-    if (c.tp == 256) launch_pair<4, 1>(gx, x_out, gw, w, stream);
+    if (c.tp == 64) launch_pair<1, 1>(gx, x_out, gw, w, stream);
+    else if (c.tp == 256) launch_pair<4, 1>(gx, x_out, gw, w, stream);
     else launch_pair<2, 2>(gx, x_out, gw, w, stream);
   } else {
     if (g_x && tile_of(d_in, n) == 256) launch<4, 4, false, 4>(gx, x_out, stream);
     else if (g_x) launch<2, 2, false, 4>(gx, x_out, stream);
-    if (c.tq == 256) launch<4, 2, true, 8>(gw, w, stream);
+    if (c.tp == 64) launch<1, 1, true, 4>(gw, w, stream);
+    else if (c.tq == 256) launch<4, 2, true, 8>(gw, w, stream);
     else if (c.tp == 256) launch<4, 1, true, 4>(gw, w, stream);
     else launch<2, 2, true, 4>(gw, w, stream);
   }

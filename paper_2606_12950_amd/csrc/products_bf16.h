@@ -839,9 +839,9 @@ __device__ __forceinline__ void product(const Product& g, const Out& out, const 
             }
           }
           if constexpr (kCodes) {                           // the next stage's values, before its end and beside the reads
-            constexpr int kFree = kProducts - kHalf, kSlots = (kHalves - 1) * kFree;
-            const int slot = kk * kFree + m - kHalf;
-            if (!end && m >= kHalf)
+            constexpr int kFree = kProducts > kHalf ? kProducts - kHalf : kProducts, kSlots = (kHalves - 1) * kFree;
+            const int slot = kk * kFree + m - (kProducts - kFree);
+            if (!end && m >= kProducts - kFree)
 #pragma unroll
               for (int i = slot * codes.kPairs / kSlots; i < (slot + 1) * codes.kPairs / kSlots; ++i)
                 codes.pair(i, lds + (buf ^ 1) * kStage);
