@@ -120,11 +120,15 @@ void launch_tiles(Product g, const Int8Forward<T>& out, hipStream_t stream) {
   int8_kernel<WP, WQ, kWaves, T><<<(unsigned)(want < most ? want : most), 64 * kWaves, 0, stream>>>(g, out);
 }
 
-// 256 x 256 tiles by eight wavefronts, two to a SIMD, so that one's scaling and stores run under the other's products. Measured (us,
-// eight / four): 262,139 x 1024 -> 1024 373 / 404, 65,536 x 256 -> 512 23.5 / 27.4, x 512 -> 512 27.9 / 30.7, 200,000 x 256 -> 256 39.1 / 43.5.
+// 256 x 256 tiles by eight wavefronts, two to a SIMD, so that one's scaling and stores run under the other's products; by four, which
+// read a quarter less of LDS, where a dozen rounds of them or more let the matrix cores' power set the clock. Measured (us with the rows'
+// quantisation, eight / four): 262,139 x 1024 -> 1024 (16 rounds) 500 / 484, 120,001 x 768 -> 1008 (7) 218 / 224, 65,536 x 512 -> 512 (2)
+// 57 / 58; without it 65,536 x 256 -> 512 23.5 / 27.4, 200,000 x 256 -> 256 39.1 / 43.5.
 template <class T>
 void launch_product(const Product& g, const Int8Forward<T>& out, hipStream_t stream) {
-  if (g.np > 128 && cdiv(g.np, 256) * cdiv(g.nq, 256) >= 2 * kCus) launch_tiles<4, 2, 8>(g, out, stream);
+  const int64_t large = cdiv(g.np, 256) * cdiv(g.nq, 256);
+  if (g.np > 128 && large >= 12 * kCus) launch_tiles<4, 4, 4>(g, out, stream);
+  else if (g.np > 128 && large >= 2 * kCus) launch_tiles<4, 2, 8>(g, out, stream);
   else if (cdiv(g.np, 128) * cdiv(g.nq, 128) >= kCus) launch_tiles<2, 2, 4>(g, out, stream);
   else launch_tiles<1, 1, 4>(g, out, stream);
 }
