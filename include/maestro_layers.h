@@ -75,7 +75,8 @@ MAESTRO_API maestro_status maestro_layer_int8(int64_t n, int32_t d_in, int32_t d
 MAESTRO_API maestro_status maestro_pack_activations(int64_t n, int32_t d, int32_t dtype, const void* x, int32_t rectified,
                              void* codes, uint8_t* exponents, void* stream);
 
-/* x (out) [n][d] in `dtype`: the values code * 2^(exponent - 127), exactly (0 * 2^(255 - 127) is NaN). */
+/* x (out) [n][d] in `dtype`: the values code * 2^(exponent - 127), exactly. An exponent of 255 counts as an infinite step (0 times
+ * it is NaN), one of 0, which packing never gives, as a step of 0. */
 MAESTRO_API maestro_status maestro_unpack_activations(int64_t n, int32_t d, int32_t dtype, const void* codes,
                              const uint8_t* exponents, int32_t rectified, void* x, void* stream);
 

@@ -4,7 +4,7 @@
 //   activations      y[n][o]   P = weight (k contiguous)   Q = x   (k contiguous)   k over d_in
 //   input's gradient g_x[n][i] P = weight (p contiguous)   Q = g_z (k contiguous)   k over d_out
 //   weights'         g_w[o][i] P = x      (p contiguous)   Q = g_z (q contiguous)   k over the n rows
-// A workgroup of four wavefronts makes a tile of TP x TQ of C, each wavefront 32 WP x 32 WQ of it in
+// A workgroup of four wavefronts (or eight) makes a tile of TP x TQ of C, each wavefront 32 WP x 32 WQ of it in
 // 32x32x16 MFMAs. k advances in stages of kDepth (32 or 64) that come straight into LDS, kBufs buffers round. An
 // operand whose k is contiguous lies in LDS as [p][k]; one whose p (or q) is contiguous as [k][p], and
 // is turned by the transposing LDS read (ds_read_b64_tr_b16: sixteen lanes read a 4 x 16 block row-wise

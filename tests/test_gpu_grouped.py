@@ -85,7 +85,7 @@ def offsets_of(sizes, first=0):
 CASES = [([1], 16, 16), ([0, 1, 0], 16, 32), ([3, 0, 5, 1], 48, 80), ([15, 16, 17], 64, 128), ([63, 64, 65, 0], 32, 48),
          ([127, 128, 129], 144, 64), ([1] * 70, 80, 16), ([0] * 100 + [200] + [0] * 155, 64, 64), ([300, 0, 1, 255], 256, 512),
          ([1000, 3], 512, 64), ([2, 5, 700], 16, 1024), ([33] * 256, 16, 48), ([4096], 272, 144), ([1, 1], 1024, 1024),
-         ([5000, 1, 0, 9000], 128, 256), ([3000, 4000], 1024, 96)]
+         ([5000, 1, 0, 9000], 128, 256), ([3000, 4000], 1024, 96), ([100, 0, 200, 0], 4096, 2048)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
@@ -95,7 +95,8 @@ def test_groups(sizes, i, o, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("sizes,i,o", [([41000, 3, 30000], 192, 256), ([50001, 0, 90002], 256, 272), ([2, 140000], 64, 160)])
+@pytest.mark.parametrize("sizes,i,o", [([41000, 3, 30000], 192, 256), ([50001, 0, 90002], 256, 272), ([2, 140000], 64, 160),
+                                       ([900, 0, 901] * 75, 256, 272)])
 def test_many_rows(sizes, i, o, dtype):
     """The larger tiles, and groups of many shares next to groups of one."""
     check(offsets_of(sizes), sum(sizes), i, o, dtype)

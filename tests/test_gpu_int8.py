@@ -121,6 +121,17 @@ def test_layer_int8(n, i, o, dtype):
         equal(got, definition(x, w, b, relu, dtype), f"relu {relu}")
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_many_rounds(dtype):
+    """3,128 tiles of 256 x 256, rows of every workgroup's first, a middle and its last one."""
+    n, i, o = 200000, 48, 1024
+    x, w, b = draw(n, i, o, 5)
+    got = M.layer_int8(on_gpu(x), on_gpu(w), b.cuda(), relu=False, dtype=dtype)
+    for first in (0, 777, 99999, 131000, n - 600):
+        rows = slice(first, first + 600)
+        equal(got[rows], definition(M.Quantized(x.codes[rows], x.scale[rows]), w, b, False, dtype), f"rows from {first}")
+
+
 def test_largest_sums():
     """16,384 products of -128 and -128: 2^28."""
     x = M.Quantized(torch.full((3, 16384), -128, dtype=torch.int8), torch.ones(3))
