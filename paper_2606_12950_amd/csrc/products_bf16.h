@@ -667,8 +667,8 @@ __device__ __forceinline__ void product(const Product& g, const Out& out, const 
   int parity = 0;
   auto fetch_biases = [&](const typename Work::Way& j) {
     if constexpr (Out::kBias) {
-      const bool there = !j.done();
-      const Item t = work.item(there ? j : at);
+      const bool there = !j.done();                         // else its place is nowhere, and nothing is read
+      const Item t = work.item(j);
       const int64_t pw = t.p0 + 32 * WP * wp;
       const i32x4 r = buffer_rsrc(out.bias + (int64_t)t.group * g.np, there ? (uint32_t)(g.np * 4) : 0);
       const uint32_t to = lds_addr(biases + (parity ? kPlace : 0));

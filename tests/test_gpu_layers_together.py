@@ -279,3 +279,33 @@ def test_fit_from_checkpoints(dims, dtype, n):
 
 def test_the_command_keeps_8_bits():
     assert F.main(["--workload", "c1", "--stages", "2048", "--steps", "2", "--packed"])["stages"] == 2048
+
+
+def test_a_fit_from_checkpoints_replays_from_a_graph():
+    dims, n = (256, 512, 512, 64), 3001
+    g = torch.Generator().manual_seed(6)
+    x = torch.randn(n, 256, generator=g).bfloat16().cuda()
+    bins = torch.randint(0, 64, (n,), generator=g, dtype=torch.int32).cuda()
+    f = F.Fit(*network(dims, torch.bfloat16, 1), n, packed=True)
+
+    def run():
+        f.score(x, bins)
+        f.gradients(x, bins)
+        M.clip_gradients([*f.g_weights, *f.g_biases], 0.5, norm=f.norm, workspace=f.workspace)
+
+    run()
+    torch.cuda.synchronize()
+    outs = (*f.g_weights, *f.g_biases, f.norm, f.out.logprob)
+    want = [t.clone() for t in outs]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for rep in range(3):
+        for t in (*outs, f.workspace, *(k for p in f.kept for k in p), *f.hidden):
+            t.fill_(3)
+        if rep == 1:
+            f.score(x, bins)
+            torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
