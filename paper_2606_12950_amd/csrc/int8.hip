@@ -137,7 +137,7 @@ void launch_product(const Product& g, const Int8Forward<T>& out, hipStream_t str
 
 maestro_status launch_quantize_rows(int64_t n, int32_t d, int32_t dtype, const void* x, int8_t* codes, float* scale,
                                     hipStream_t stream) {
-  constexpr int64_t kRows = (int64_t)1 << 30;               // of a launch: its grid in 32 bits
+  constexpr int64_t kRows = (int64_t)1 << 25;               // of a launch: 64 threads a row at most, counted in 32 bits
   for (int64_t row = 0; row < n; row += kRows) {
     const int64_t rows = n - row < kRows ? n - row : kRows;
     if (dtype == MAESTRO_BF16)

@@ -42,6 +42,26 @@ def test_quantize_rows(n, d, dtype):
     same(M.quantize_rows(x.cuda()), quantized(x))
 
 
+def test_rows_of_several_launches():
+    """More rows than 32 bits count threads of, at 64 a row, and codes past 2^34 bytes: every row is written, from its own row."""
+    n, d = (1 << 26) + 5, 272
+    if torch.cuda.mem_get_info()[0] < 64 << 30:
+        pytest.skip("needs 64 GiB")
+    rows = torch.tensor([0, 1, (1 << 25) - 1, 1 << 25, (1 << 25) + 1, (1 << 26) - 1, 1 << 26, n - 1])
+    g = torch.Generator().manual_seed(9)
+    some = torch.randn(len(rows), d, generator=g).bfloat16()
+    x = torch.zeros(n, d, dtype=torch.bfloat16, device="cuda")
+    x[rows.cuda()] = some.cuda()
+    out = M.Quantized(torch.full((n, d), 77, dtype=torch.int8, device="cuda"), torch.full((n,), -1.0, device="cuda"))
+    M.quantize_rows(x, out=out)
+    same(M.Quantized(out.codes[rows.cuda()], out.scale[rows.cuda()]), quantized(some))
+    out.scale[rows.cuda()] = 2.0 ** -126
+    assert (out.scale == 2.0 ** -126).all()
+    out.codes[rows.cuda()] = 0
+    for part in out.codes.split(1 << 24):
+        assert not part.any()
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_quantize_hard_rows(dtype):
     """Ties, zeros, the smallest and largest values, NaN and infinities."""
