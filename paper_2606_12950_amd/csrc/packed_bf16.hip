@@ -16,10 +16,10 @@ __global__ __launch_bounds__(64 * kWaves, (Tile<WP, WQ, 64, 2, Out, kWaves>::kSi
 }
 
 // Both gradients in one launch: the first `blocks` workgroups make the input's, in 64 x 64 tiles, the others the weights'.
-template <int WP, int WQ>
-__global__ __launch_bounds__(kThreads, (WP * WQ == 1 ? 4 : 2)) void pair_kernel(Product gx, CodesInputGrad x, uint32_t blocks, Product gw, CodesWeightGrad w) {
+template <int WP, int WQ, class Code>
+__global__ __launch_bounds__(kThreads, (WP * WQ == 1 ? 4 : 2)) void pair_kernel(Product gx, CodesInputGrad x, uint32_t blocks, Product gw, CodesWeightGrad<Code> w) {
   using X = Tile<1, 1, 64, 2, CodesInputGrad>;
-  using W = Tile<WP, WQ, 64, 2, CodesWeightGrad>;
+  using W = Tile<WP, WQ, 64, 2, CodesWeightGrad<Code>>;
   __shared__ __attribute__((aligned(16))) unsigned char lds[X::kBytes > W::kBytes ? X::kBytes : W::kBytes];
   if (blockIdx.x < blocks) product<1, 1, 64, 2, true, false>(gx, x, Dense<X::TP, X::TQ, 64>(gx), lds, blockIdx.x, blocks);
   else product<WP, WQ, 64, 2, true, true>(gw, w, Dense<W::TP, W::TQ, 64>(gw), lds, blockIdx.x - blocks, gridDim.x - blocks);
@@ -41,9 +41,9 @@ void launch(Product g, const Out& out, hipStream_t stream) {
   product_kernel<WP, WQ, kQT, kWaves><<<blocks, 64 * kWaves, 0, stream>>>(g, out);
 }
 
-template <int WP, int WQ>
-void launch_pair(Product gx, const CodesInputGrad& x, Product gw, const CodesWeightGrad& w, hipStream_t stream) {
-  const uint32_t blocks = plan<Tile<1, 1, 64, 2, CodesInputGrad>>(gx), more = plan<Tile<WP, WQ, 64, 2, CodesWeightGrad>>(gw);
+template <int WP, int WQ, class Code>
+void launch_pair(Product gx, const CodesInputGrad& x, Product gw, const CodesWeightGrad<Code>& w, hipStream_t stream) {
+  const uint32_t blocks = plan<Tile<1, 1, 64, 2, CodesInputGrad>>(gx), more = plan<Tile<WP, WQ, 64, 2, CodesWeightGrad<Code>>>(gw);
   pair_kernel<WP, WQ><<<blocks + more, kThreads, 0, stream>>>(gx, x, blocks, gw, w);
 }
 
@@ -76,6 +76,24 @@ Cut cut_of(int64_t n, int64_t d_in, int64_t d_out) {
   return c;
 }
 
+template <class Code>
+void launch_gradients(int64_t n, const Product& gx, const CodesInputGrad& x, const Product& gw, const CodesWeightGrad<Code>& w,
+                      const Cut& c, hipStream_t stream) {
+  const int tile = tile_of(gx.np, n);
+  if (x.c && tile == 64) {
+    if (c.tp == 64) launch_pair<1, 1>(gx, x, gw, w, stream);
+    else if (c.tp == 256) launch_pair<4, 1>(gx, x, gw, w, stream);
+    else launch_pair<2, 2>(gx, x, gw, w, stream);
+    return;
+  }
+  if (x.c && tile == 256) launch<4, 4, false, 4>(gx, x, stream);
+  else if (x.c) launch<2, 2, false, 4>(gx, x, stream);
+  if (c.tp == 64) launch<1, 1, true, 4>(gw, w, stream);
+  else if (c.tq == 256) launch<4, 2, true, 8>(gw, w, stream);
+  else if (c.tp == 256) launch<4, 1, true, 4>(gw, w, stream);
+  else launch<2, 2, true, 4>(gw, w, stream);
+}
+
 }  // namespace
 
 size_t grad_packed_bf16_workspace_bytes(int64_t n, int32_t d_in, int32_t d_out) {
@@ -88,33 +106,16 @@ maestro_status launch_grad_packed_bf16(int64_t n, int32_t d_in, int32_t d_out, c
                                        bool rectified, const void* weight, const void* g_z, bool relu_input, void* g_x,
                                        float* g_weight, float* g_bias, void* workspace, hipStream_t stream) {
   const __bf16* gz = static_cast<const __bf16*>(g_z);
-  const unsigned char* c8 = static_cast<const unsigned char*>(codes);
   const Cut c = cut_of(n, d_in, d_out);
   float* parts = static_cast<float*>(workspace);
   float* gb_parts = parts + c.splits * d_in * d_out;
   const Product gw{nullptr, gz, d_in, d_out, d_in, d_out, n, c.k_split, 1, 0, 0};
-  CodesWeightGrad w;
-  w.gw = c.splits > 1 ? parts : g_weight;
-  w.gb = c.splits > 1 ? gb_parts : g_bias;
-  w.parts = c.parts;
-  w.codes = c8;
-  w.exponents = exponents;
-  w.ld_exponents = (d_in + 31) / 32;
-  w.is_signed = !rectified;
   const Product gx{static_cast<const __bf16*>(weight), gz, d_in, d_out, d_in, n, d_out, d_out, 1, 0, 0};
-  const CodesInputGrad x_out{c8, static_cast<__bf16*>(g_x), relu_input};
-  if (g_x && tile_of(d_in, n) == 64) {
-    if (c.tp == 64) launch_pair<1, 1>(gx, x_out, gw, w, stream);
-    else if (c.tp == 256) launch_pair<4, 1>(gx, x_out, gw, w, stream);
-    else launch_pair<2, 2>(gx, x_out, gw, w, stream);
-  } else {
-    if (g_x && tile_of(d_in, n) == 256) launch<4, 4, false, 4>(gx, x_out, stream);
-    else if (g_x) launch<2, 2, false, 4>(gx, x_out, stream);
-    if (c.tp == 64) launch<1, 1, true, 4>(gw, w, stream);
-    else if (c.tq == 256) launch<4, 2, true, 8>(gw, w, stream);
-    else if (c.tp == 256) launch<4, 1, true, 4>(gw, w, stream);
-    else launch<2, 2, true, 4>(gw, w, stream);
-  }
+  const CodesInputGrad x_out{static_cast<const unsigned char*>(codes), static_cast<__bf16*>(g_x), relu_input};
+  const WeightGrad w{c.splits > 1 ? parts : g_weight, c.splits > 1 ? gb_parts : g_bias, c.parts};
+  const int64_t blocks = (d_in + 31) / 32;
+  if (rectified) launch_gradients(n, gx, x_out, gw, CodesWeightGrad<uint8_t>{w, static_cast<const uint8_t*>(codes), exponents, blocks}, c, stream);
+  else launch_gradients(n, gx, x_out, gw, CodesWeightGrad<int8_t>{w, static_cast<const int8_t*>(codes), exponents, blocks}, c, stream);
   const maestro_status st = launch_status();
   if (st != MAESTRO_OK || c.splits == 1) return st;
   return launch_join(parts, (int32_t)c.splits, g_weight, (int64_t)d_in * d_out, gb_parts, (int32_t)(c.splits * c.parts * 2),

@@ -159,12 +159,21 @@ struct WeightGrad {
   }
 };
 
+template <class C>
 struct CodesWeightGrad : WeightGrad {
   static constexpr bool kCodes = true;
-  const unsigned char* codes;        // [nk][np]
+  typedef C Code;                    // int8_t or uint8_t
+  const Code* codes;                 // [nk][np]
   const unsigned char* exponents;    // [nk][ld_exponents]
   int64_t ld_exponents;
-  int32_t is_signed;
+};
+template <class Out, class = void>
+struct CodeOf {
+  typedef uint8_t type;
+};
+template <class Out>
+struct CodeOf<Out, std::void_t<typename Out::Code>> {
+  typedef typename Out::Code type;
 };
 
 template <int N>
@@ -273,7 +282,7 @@ struct Operand {
 // A turned operand that memory holds as codes, bytes, and for every 32 of a row a power of two. A stage's codes come through
 // registers, 16 to a unit, and are values before they lie in LDS: a value has at most eight significant bits, so bfloat16
 // holds it exactly. They are loaded two stages ahead of the products' and turned into values one ahead, a pair after a product.
-template <int T, int kDepth, int kWaves = 4>
+template <int T, int kDepth, class Code, int kWaves = 4>
 struct CodesOperand {
   static constexpr int kUnits = T * kDepth / 16 / (64 * kWaves), kRowUnits = T / 16, kRows = 64 * kWaves / kRowUnits;
   static constexpr int kPairs = 8 * kUnits;
@@ -283,18 +292,15 @@ struct CodesOperand {
   u32x4 packed;
   const unsigned char *codes, *exponents;                   // of the next stage to load
   int64_t left;                                             // its rows and all after it
-  uint32_t ld, ld_exponents, off, off_exponents, flip;
+  uint32_t ld, ld_exponents, off, off_exponents;
   uint32_t to;                                              // in the stage, the 16 bytes it writes first of a unit's 32
   bool second;                                              // those are the unit's second ones
-  float zero;                                               // what a code of 0 counts, in steps: -128 of flipped ones
 
   template <class Out>
   __device__ __forceinline__ void init(const Out& out, int64_t ldp) {
     const int k = threadIdx.x / kRowUnits, unit = threadIdx.x % kRowUnits;
     ld = (uint32_t)ldp;
     ld_exponents = (uint32_t)out.ld_exponents;
-    flip = out.is_signed ? 0x80808080u : 0u;                // signed bytes as unsigned ones, 128 more
-    zero = out.is_signed ? -128.0f : 0.0f;
     // eight lanes write 128 bytes at a time: neighbouring fours of them begin with other halves, and meet all banks
     second = (unit & 4) != 0;
     to = k * 2 * T + (((2 * unit + second) ^ (4 * Operand<T, kDepth, true>::turn(k))) << 4);
@@ -302,7 +308,7 @@ struct CodesOperand {
   template <class Out>
   __device__ __forceinline__ void tile(const Out& out, int64_t p0, int64_t k0, int64_t kn) {
     const int k = threadIdx.x / kRowUnits, unit = threadIdx.x % kRowUnits;
-    codes = out.codes + k0 * ld;
+    codes = reinterpret_cast<const unsigned char*>(out.codes) + k0 * ld;
     exponents = out.exponents + k0 * ld_exponents;
     left = kn;
     off = (uint32_t)(k * ld + p0 + 16 * unit);
@@ -325,7 +331,7 @@ struct CodesOperand {
   __device__ __forceinline__ void take() {
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
-      now[j] = (second ? __builtin_shufflevector(ahead[j], ahead[j], 2, 3, 0, 1) : ahead[j]) ^ flip;
+      now[j] = second ? __builtin_shufflevector(ahead[j], ahead[j], 2, 3, 0, 1) : ahead[j];
       step[j] = __uint_as_float((uint32_t)ahead_exponent[j] << 23);
       // here and not after the next loads, whose registers would then be others, and waited for to be copied
       asm volatile("" : "+v"(now[j]), "+v"(step[j]));
@@ -335,8 +341,7 @@ struct CodesOperand {
   __device__ __forceinline__ void pair(int i, unsigned char* stage) {
     const int j = i / 8, r = i % 8;
     const uint32_t w = now[j][r / 2] >> (16 * (r & 1));
-    const float base = zero * step[j];
-    const float a = fmaf((float)(w & 255u), step[j], base), b = fmaf((float)((w >> 8) & 255u), step[j], base);
+    const float a = (float)(Code)w * step[j], b = (float)(Code)(w >> 8) * step[j];
     packed[r % 4] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
     if (r % 4 == 3) *reinterpret_cast<u32x4*>(stage + (to ^ (16 * (r / 4))) + j * kRows * 2 * T) = packed;
   }
@@ -686,7 +691,7 @@ __device__ __forceinline__ void product(const Product& g, const Out& out, const 
   fetch_biases(at);
 
   // P's codes: a stage further ahead than Q
-  CodesOperand<TP, kDepth, kWaves> codes;
+  CodesOperand<TP, kDepth, typename CodeOf<Out>::type, kWaves> codes;
   auto codes_at = at;
   int64_t codes_left = 0;
   auto open_codes = [&]() {

@@ -193,3 +193,39 @@ def test_grad_of_values_not_finite(dtype):
     rest = [c for c in range(i) if not 32 <= c < 64]
     assert torch.equal(clean.weight[:, rest], dirty.weight[:, rest])
     assert not dirty.x[130, 32:64].any() and torch.equal(clean.x[:130], dirty.x[:130]) and torch.equal(clean.x[131:], dirty.x[131:])
+
+
+@pytest.mark.parametrize("rectified", [False, True])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,o", [(77, 48), (700, 96), (20011, 272)])
+def test_grad_of_largest_and_smallest_steps(n, o, dtype, rectified):
+    """A step for every 32 columns, from the smallest to the largest that packing gives; codes that fill them."""
+    steps = torch.tensor([1, 2, 60, 127, 200, 240, *(e - rectified for e in (246, 247, 248, 249))], dtype=torch.uint8)
+    i = 32 * len(steps)
+    g = torch.Generator().manual_seed(n)
+    codes = torch.randint(0, 256, (n, i), generator=g) if rectified else torch.randint(-127, 128, (n, i), generator=g)
+    codes[:, -32:] = torch.div(codes[:, -32:], 2, rounding_mode="trunc")      # below 2^128
+    codes = codes.to(torch.uint8 if rectified else torch.int8)
+    exponents = steps.expand(n, -1).contiguous()
+    v = values(codes, exponents)
+    assert torch.isfinite(v.float()).all()
+    w = (torch.randn(o, i, generator=g) * i ** -0.5).to(dtype)
+    gz = (torch.randn(n, o, generator=g) * 2.0 ** -40).to(dtype)
+    gd = gz.double()
+    got = M.layer_grad_packed(M.Packed(codes.cuda(), exponents.cuda()), w.cuda(), gz.cuda())
+    near(got.weight, gd.t() @ v, bound(gd.t(), v) + n * 2.0 ** -126, "weight")      # products below 2^-126 may count as 0
+
+
+@pytest.mark.parametrize("rectified", [False, True])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_grad_of_infinite_steps(dtype, rectified):
+    """Of codes that packing never gives, 1 and more of an infinite step: infinities, in their columns only."""
+    n, i, o = 200, 96, 48
+    codes, exponents, _, w, gz = draw(n, i, o, dtype, rectified, 7)
+    clean = M.layer_grad_packed(M.Packed(codes.cuda(), exponents.cuda()), w.cuda(), gz.cuda())
+    codes[130, 32:64], exponents[130, 1] = 5, 255
+    assert (gz[130] != 0).all()
+    dirty = M.layer_grad_packed(M.Packed(codes.cuda(), exponents.cuda()), w.cuda(), gz.cuda())
+    assert torch.equal(dirty.weight[:, 32:64].cpu(), (gz[130].float() * math.inf)[:, None].expand(-1, 32))
+    rest = [c for c in range(i) if not 32 <= c < 64]
+    assert torch.equal(clean.weight[:, rest], dirty.weight[:, rest]) and torch.equal(clean.x, dirty.x)
