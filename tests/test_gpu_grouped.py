@@ -154,6 +154,38 @@ def test_groups_do_not_see_each_other(dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("sizes,i,o", [([3, 41000, 0, 30077], 272, 272), ([130000, 5, 10001], 528, 272), ([500, 1500, 7], 272, 80),
+                                       ([20001, 33, 19000], 48, 176)])
+def test_poison_in_large_groups(sizes, i, o, dtype):
+    """As above in the larger tiles and shares; rows of no group before and behind hold NaN, as does the workspace."""
+    ends = offsets_of(sizes, 9)
+    n, groups = ends[-1] + 70, len(sizes)
+    off = torch.tensor(ends, device="cuda")
+    x, w, b, gz = (t.cuda() for t in draw(n, groups, i, o, dtype, 6))
+    clean, grads = M.layer_grouped(x, w, b, off, relu=False), M.layer_grouped_grad(x, w, gz, off)
+    for t in (x, gz):
+        t[:9], t[ends[-1]:] = math.nan, math.nan
+    taken = slice(9, ends[-1])
+    ws = torch.full((1 << 28,), 0xFF, dtype=torch.uint8, device="cuda")
+    again = M.layer_grouped_grad(x, w, gz, off, workspace=ws)
+    assert torch.equal(M.layer_grouped(x, w, b, off, relu=False)[taken], clean[taken]) and torch.equal(again.x[taken], grads.x[taken])
+    assert torch.equal(again.weight, grads.weight) and torch.equal(again.bias, grads.bias)
+    bad = [9, ends[1], (ends[1] + ends[2]) // 2, ends[2] - 1]               # the first row of the first group, and three of the second
+    x[bad, i - 1] = math.nan
+    gz[bad, o - 1] = math.inf
+    rest = torch.ones(n, dtype=torch.bool, device="cuda")
+    rest[bad], rest[:9], rest[ends[-1]:] = False, False, False
+    assert torch.equal(M.layer_grouped(x, w, b, off, relu=False)[rest], clean[rest])
+    dirty = M.layer_grouped_grad(x, w, gz, off, workspace=ws)
+    assert torch.equal(dirty.x[rest], grads.x[rest])
+    others = list(range(2, groups))
+    assert torch.equal(dirty.weight[others], grads.weight[others]) and torch.equal(dirty.bias[others], grads.bias[others])
+    for g in (0, 1):
+        assert torch.equal(dirty.weight[g, :-1, :-1], grads.weight[g, :-1, :-1]) and torch.equal(dirty.bias[g, :-1], grads.bias[g, :-1])
+        assert torch.isnan(dirty.weight[g, :, -1]).all() and torch.isinf(dirty.bias[g, -1])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_equal_calls_and_nothing_beside(dtype):
     sizes, i, o = [700, 0, 900], 256, 192
     n, off = sum(sizes), torch.tensor(offsets_of(sizes), device="cuda")

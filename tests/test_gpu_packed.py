@@ -229,3 +229,26 @@ def test_grad_of_infinite_steps(dtype, rectified):
     assert torch.equal(dirty.weight[:, 32:64].cpu(), (gz[130].float() * math.inf)[:, None].expand(-1, 32))
     rest = [c for c in range(i) if not 32 <= c < 64]
     assert torch.equal(clean.weight[:, rest], dirty.weight[:, rest]) and torch.equal(clean.x, dirty.x)
+
+
+@pytest.mark.parametrize("rectified", [False, True])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,i,o", [(300, 80, 48), (2001, 272, 80), (33001, 144, 272), (140003, 528, 272)])
+def test_poison_in_large_layers(n, i, o, dtype, rectified):
+    """32 values that are not finite and a gradient that is not spoil their columns, their row of g_w and their rows of g_x only."""
+    g = torch.Generator().manual_seed(n)
+    p = M.pack_activations(torch.randn(n, i, generator=g).to(dtype).cuda(), rectified=rectified)
+    w, gz = (torch.randn(o, i, generator=g) * i ** -0.5).to(dtype).cuda(), (torch.randn(n, o, generator=g) / n).to(dtype).cuda()
+    clean = M.layer_grad_packed(p, w, gz, relu_input=rectified)
+    last = i - i % 32 or i - 32                                # the last exponent's columns
+    p.codes[n - 1, last:], p.exponents[n - 1, -1] = 0, 255
+    p.codes[64, :32], p.exponents[64, 0] = 0, 255
+    gz[n // 2, o - 1] = math.nan
+    ws = torch.full((1 << 28,), 0xFF, dtype=torch.uint8, device="cuda")
+    dirty = M.layer_grad_packed(p, w, gz, relu_input=rectified, workspace=ws)
+    assert torch.equal(dirty.weight[:-1, 32:last], clean.weight[:-1, 32:last]) and torch.equal(dirty.bias[:-1], clean.bias[:-1])
+    assert torch.isnan(dirty.weight[:, :32]).all() and torch.isnan(dirty.weight[:, last:]).all() and torch.isnan(dirty.weight[-1]).all()
+    rest = torch.ones(n, dtype=torch.bool, device="cuda")
+    rest[[64, n // 2, n - 1]] = False
+    assert torch.isnan(dirty.bias[-1]) and torch.equal(dirty.x[rest], clean.x[rest])
+    assert torch.equal(dirty.x[64, 32:], clean.x[64, 32:]) and torch.equal(dirty.x[n - 1, :last], clean.x[n - 1, :last])
