@@ -125,14 +125,18 @@ void launch_tiles(Product g, const Out& out, const int64_t* offsets, int32_t n_g
 
 // Tile by how many there are, as for a layer of one group. 256 x 256 ones by eight wavefronts, two to a SIMD, or by four: the layer
 // with eight 546 us, four 544 (262,139 x 1024 -> 1024, 16 groups); the input's gradient, whose mask wants registers, 612 and 575.
+// The input's gradient no wider than 64 takes tiles that are not either (us, both gradients, 128 x 128 / 64 x 64: 100,000 x 64 -> 64 28.0 / 23.8, 100,000 x
+// 16 -> 256 36.7 / 30.5, 200,000 x 48 -> 1024 186 / 180); the layer does not gain (63,399 x 112 -> 48 8.4 / 9.9).
+template <bool kPT>
 int tile_of(int64_t np, int64_t n) {
-  if (np > 128 && cdiv(np, 256) * (n / 256) >= 2 * kCus) return 256;
+  if (kPT && np <= 64) return 64;
+  if (fits256(np) && cdiv(np, 256) * (n / 256) >= 2 * kCus) return 256;
   return cdiv(np, 128) * (n / 128) >= kCus ? 128 : 64;
 }
 
 template <bool kPT, class Out>
 void launch_rows(const Product& g, const Out& out, const int64_t* offsets, int32_t n_groups, int64_t n, hipStream_t stream) {
-  const int tile = tile_of(g.np, n);
+  const int tile = tile_of<kPT>(g.np, n);
   if (tile == 256) {
     if constexpr (kPT) launch_tiles<4, 4, kPT, 4>(g, out, offsets, n_groups, n, stream);
     else launch_tiles<4, 2, kPT, 8>(g, out, offsets, n_groups, n, stream);
@@ -153,8 +157,8 @@ struct Cut {
 };
 Cut cut_of(int64_t n, int64_t n_groups, int64_t d_in, int64_t d_out) {
   Cut c;
-  c.tp = d_in > 128 ? 256 : 128;
-  c.tq = c.tp == 128 ? 128 : d_out > 128 && n >= 131072 ? 256 : 64;
+  const WeightTile tile = weight_tile(n, d_in, d_out);
+  c.tp = tile.tp, c.tq = tile.tq;
   const int64_t tiles = cdiv(d_in, c.tp) * cdiv(d_out, c.tq), resident = c.tq == 256 ? 1 : 2;
   int64_t splits = kCus * resident / tiles;
   c.by_group = splits > cdiv(n, 512);
@@ -220,7 +224,7 @@ maestro_status launch_grouped_grad_bf16(int64_t n, int32_t n_groups, int32_t d_i
   const Product gw{xb, gz, d_in, d_out, d_in, d_out, n, c.k_split, 1, 0, 0};
   const GroupedWeightGrad out{g_weight, g_bias, gw_parts, gb_parts, 1};
   const bool alone = n <= c.k_split;
-  if (g_x && c.tp == 64 && tile_of(d_in, n) == 64) {
+  if (g_x && c.tp == 64 && tile_of<true>(d_in, n) == 64) {
     launch_pair(gx, x_out, gw, out, offsets, n_groups, (int32_t)n, alone, stream);
   } else {
     if (g_x) launch_rows<true>(gx, x_out, offsets, n_groups, n, stream);

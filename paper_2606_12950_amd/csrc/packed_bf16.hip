@@ -47,11 +47,13 @@ void launch_pair(Product gx, const CodesInputGrad& x, Product gw, const CodesWei
   pair_kernel<WP, WQ><<<blocks + more, kThreads, 0, stream>>>(gx, x, blocks, gw, w);
 }
 
-// As for the gradients of an input in bfloat16, and for little work 64 x 64 tiles of the weights' gradient, with splits of 256 rows
+// As for the gradients of an input in bfloat16, but the input's 64 wide where it is no wider (us, 128 x 128 / 64 x 64, both gradients: 100,000 x 64
+// -> 64 24.6 / 19.8, 100,000 x 16 -> 256 36.4 / 33.6, 200,000 x 48 -> 1024 190 / 196, 40,000 x 64 -> 512 34.5 / 29.0), and for little work 64 x 64 tiles of the weights' gradient, with splits of 256 rows
 // or more, where four to a CU hold them all. Measured (us, both gradients, 64 x 64 with 256 / 512 rows / the larger tiles): 300 x 256 -> 512
 // 9.1 / 6.8 (one split) / 11.7 (weights), 1,000 x 1024 -> 64 9.3 / 11.5, 4,000 x 256 -> 256 11.5 / 12.8, 30,000 x 64 -> 128 13.8 / 15.0 / 17.0 (weights).
 int tile_of(int64_t np, int64_t nq) {
-  if (np > 128 && cdiv(np, 256) * cdiv(nq, 256) >= 2 * kCus) return 256;
+  if (np <= 64) return 64;
+  if (fits256(np) && cdiv(np, 256) * cdiv(nq, 256) >= 2 * kCus) return 256;
   return cdiv(np, 128) * cdiv(nq, 128) >= kCus ? 128 : 64;
 }
 
@@ -62,8 +64,8 @@ struct Cut {
 };
 Cut cut_of(int64_t n, int64_t d_in, int64_t d_out) {
   Cut c;
-  c.tp = d_in > 128 ? 256 : 128;
-  c.tq = c.tp == 128 ? 128 : d_out > 128 && n >= 131072 ? 256 : 64;
+  const WeightTile tile = weight_tile(n, d_in, d_out);
+  c.tp = tile.tp, c.tq = tile.tq;
   int64_t tiles = cdiv(d_in, c.tp) * cdiv(d_out, c.tq), most = kCus * (c.tq == 256 ? 1 : 2), least = 512;
   const int64_t small = cdiv(d_in, 64) * cdiv(d_out, 64), few = n <= 512 ? 512 : 256;
   if (small * cdiv(n, few) <= 4 * kCus) c.tp = c.tq = 64, tiles = small, most = 4 * kCus, least = few;
