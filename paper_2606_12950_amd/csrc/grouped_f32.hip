@@ -97,8 +97,10 @@ __global__ __launch_bounds__(kThreads, 2) void pair_kernel(Product gx, InputGrad
   if (alone) clear_empty_groups(table, w.gw, gw.np * gw.nq, w.gb, (int)gw.nq, blockIdx.x - blocks, gridDim.x - blocks);
 }
 
-// Group blockIdx.y's units added in order, a quad of values a thread; zeros where it has none.
-template <GroupUnits kUnits>
+// Group blockIdx.y's units added in a fixed order; zeros where it has none. A quad of values to each of 256 / G neighbouring threads,
+// its units dealt out over G groups of them. G = 16 where there are few values, else 1. Measured (us, weights' gradient, G = 1 / 16): float32 100,000 x 64 ->
+// 64 in 4 groups 36.9 / 22.8, 22,266 x 64 -> 80 in 2 21.3 / 16.9, bfloat16 60,000 x 64 -> 64 in 3 16.9 / 13.6; 31,065 x 384 -> 48 in 8 15.4 / 16.5.
+template <GroupUnits kUnits, int G>
 __global__ __launch_bounds__(kThreads) void join_groups_kernel(int32_t n, int32_t n_groups, const int64_t* offsets, int32_t k_split,
                                                                const float* gw_parts, float* gw, int64_t size,
                                                                const float* gb_parts, float* gb, int32_t d_out) {
@@ -107,24 +109,41 @@ __global__ __launch_bounds__(kThreads) void join_groups_kernel(int32_t n, int32_
   const int group = blockIdx.y;
   const int first = table.first_unit(group), last = table.first_unit(group + 1);
   if (last - first == 1) return;
+  constexpr int kQuads = kThreads / G;
+  const int part = threadIdx.x / kQuads, own = threadIdx.x % kQuads;
   const int64_t quads = size / 4, all = quads + d_out / 4;
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < all; i += (int64_t)gridDim.x * kThreads) {
+  __shared__ float4 s_sum[G][kQuads];
+  for (int64_t from = (int64_t)blockIdx.x * kQuads; from < all; from += (int64_t)gridDim.x * kQuads) {
+    const int64_t i = from + own;
     const bool w = i < quads;
     const float4* at = w ? reinterpret_cast<const float4*>(gw_parts) + i : reinterpret_cast<const float4*>(gb_parts) + (i - quads);
     const int64_t step = w ? quads : d_out / 4;
     float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    int j = first;
-    for (; j + 7 < last; j += 8) {
+    const int end = i < all ? last : first;
+    int j = first + part;
+    for (; j + 7 * G < end; j += 8 * G) {
       float4 a[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) a[u] = at[(j + u) * step];
+      for (int u = 0; u < 8; ++u) a[u] = at[(j + u * G) * step];
 #pragma unroll
       for (int u = 0; u < 8; ++u) s.x += a[u].x, s.y += a[u].y, s.z += a[u].z, s.w += a[u].w;
     }
-    for (; j < last; ++j) {
+    for (; j < end; j += G) {
       const float4 a = at[j * step];
       s.x += a.x, s.y += a.y, s.z += a.z, s.w += a.w;
     }
+    if constexpr (G > 1) {
+      __syncthreads();                                      // the last round's sums are read
+      s_sum[part][own] = s;
+      __syncthreads();
+      if (part > 0) continue;
+#pragma unroll
+      for (int u = 1; u < G; ++u) {
+        const float4 a = s_sum[u][own];
+        s.x += a.x, s.y += a.y, s.z += a.z, s.w += a.w;
+      }
+    }
+    if (i >= all) continue;
     float4* to = w ? reinterpret_cast<float4*>(gw) + group * quads + i : reinterpret_cast<float4*>(gb) + group * step + (i - quads);
     *to = s;
   }
@@ -140,7 +159,8 @@ void launch_rows(Product g, const Out& out, const int64_t* offsets, int32_t n_gr
   rows_kernel<W, kPT><<<(unsigned)(most < 65536 ? most : 65536), kThreads, 0, stream>>>(g, out, offsets, n_groups, (int32_t)n);
 }
 
-// As for a layer of one group. by_group: too few rows for a unit of them in every workgroup.
+// As for a layer of one group. by_group: too few rows for a unit of 256 in every workgroup; units of 128 then (us, weights' gradient, 256 / 128 / 64 rows:
+// 4,096 x 64 -> 128 in 3 groups 14.7 / 11.4 / 10.6, with the input's 14.8 / 11.7 / 12.8, 20,000 x 128 -> 128 in 30 both 29.8 / 26.7 / 26.7).
 struct Cut {
   bool wide, by_group;
   int64_t k_split, most;             // rows of a unit, and the most units
@@ -152,7 +172,8 @@ Cut cut_of(int64_t n, int64_t n_groups, int64_t d_in, int64_t d_out) {
   const int64_t t = c.wide ? 128 : 64, tiles = cdiv(d_in, t) * cdiv(d_out, t);
   int64_t splits = 2 * kCus / tiles;
   c.by_group = splits > cdiv(n, 256);
-  if (c.by_group) splits = cdiv(n, 256);
+  const int64_t least = n <= 256 ? 256 : 128;
+  if (splits > cdiv(n, least)) splits = cdiv(n, least);
   if (splits < 1) splits = 1;
   c.k_split = cdiv(cdiv(n, splits), kDepth) * kDepth;
   c.most = n / c.k_split + n_groups;
@@ -218,8 +239,11 @@ maestro_status launch_grouped_grad_f32(int64_t n, int32_t n_groups, int32_t d_in
 maestro_status launch_join_groups(int64_t n, int32_t n_groups, const int64_t* offsets, int64_t k_split, bool by_group,
                                   const float* gw_parts, float* gw, int64_t size, const float* gb_parts, float* gb, int32_t d_out,
                                   hipStream_t stream) {
-  const int64_t blocks = cdiv(size / 4 + d_out / 4, kThreads);
-  auto kernel = by_group ? join_groups_kernel<kTiles> : join_groups_kernel<kShares>;
+  const int64_t quads = size / 4 + d_out / 4;
+  const bool dealt = cdiv(quads, kThreads) * n_groups <= kCus / 2 && n / k_split > 8;
+  const int64_t blocks = cdiv(quads, dealt ? kThreads / 16 : kThreads);
+  auto kernel = dealt ? by_group ? join_groups_kernel<kTiles, 16> : join_groups_kernel<kShares, 16>
+                      : by_group ? join_groups_kernel<kTiles, 1> : join_groups_kernel<kShares, 1>;
   kernel<<<dim3((unsigned)(blocks < 4096 ? blocks : 4096), (unsigned)n_groups), kThreads, 0, stream>>>(
       (int32_t)n, n_groups, offsets, (int32_t)k_split, gw_parts, gw, size, gb_parts, gb, d_out);
   return launch_status();
