@@ -66,7 +66,8 @@ MAESTRO_API maestro_status maestro_layer_int8(int64_t n, int32_t d_in, int32_t d
                              void* y, void* stream);
 
 /* x [n][d] (`dtype`) as codes (out) [n][d], a byte each, and exponents (out) [n][(d + 31) / 32] bytes (no alignment): every 32 values of
- * a row share the step 2^(exponent - 127), the least one (from 2^-126 on) that leaves all of them within the codes:
+ * a row share the step 2^(exponent - 127), the least one (from 2^-126 on) that leaves all of them within the codes, at most 2^121
+ * (2^120 where rectified): one more would make 2^128, an infinity, of finite values, which have the last code instead.
  *   rectified = 0: signed bytes, code = x / step to the nearest, ties to the even one: -127 .. 127
  *   rectified = 1: unsigned bytes 0 .. 255; values that are not positive have code 0, positive ones at least 1 (a
  *                  value below half a step counts as a step), so that code > 0 where x > 0

@@ -3,7 +3,8 @@
 // pack_kernel, unpack_kernel: eight values a thread; four neighbouring threads hold the 32 values of an exponent (two, at the end
 // of a row of an odd number of 16s). The step 2^e is read off the largest magnitude's bits: with most = 127 (255 for
 // rectified values, which need no sign) the least e with rint(largest / 2^e) <= most, so largest / 2^e < most + 1/2; the
-// quotient by a power of two is exact. A value has at most 8 significant bits then, so bfloat16 holds it exactly.
+// quotient by a power of two is exact. A value has at most 8 significant bits then, so bfloat16 holds it exactly. The step that would
+// make 2^128 of a finite value is not taken: the one below it is, and codes end at the last one, less than a step from the value.
 #include "layers.h"
 #include "vectors.h"
 
@@ -18,10 +19,11 @@ template <bool kRectified>
 __device__ __forceinline__ int exponent_of(uint32_t most) {
   if (most >= 0x7F800000u) return 255;
   constexpr uint32_t kLast = kRectified ? 0x7F8000u : 0x7F0000u;      // mantissa of (most + 1/2) / 2^k
-  const int e = (int)(most >> 23) - (kRectified ? 7 : 6) + ((most & 0x7FFFFFu) >= kLast ? 1 : 0);
-  return e < 1 ? 1 : e;
+  constexpr int kBelow = kRectified ? 7 : 6;                          // a largest value's exponent over its step's
+  const int e = (int)(most >> 23) - kBelow + ((most & 0x7FFFFFu) >= kLast ? 1 : 0);
+  return e < 1 ? 1 : e > 254 - kBelow ? 254 - kBelow : e;
 }
-// 2^(127 - e): the inverse step's bits, for e = 1 .. 250
+// 2^(127 - e): the inverse step's bits, for e = 1 .. 248
 __device__ __forceinline__ float inverse_step(int e) { return __uint_as_float((uint32_t)(254 - e) << 23); }
 __device__ __forceinline__ float step_of(int e) { return __uint_as_float((uint32_t)e << 23); }
 
@@ -53,7 +55,8 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(uint32_t rows, uint32_t 
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     t[j] = fmaf(v[j], inverse, kRounder);                   // the product is exact
-    if constexpr (kRectified) t[j] = fmaxf(t[j], v[j] > 0.0f ? kRounder + 1.0f : kRounder);
+    const float least = !kRectified ? kRounder - 127.0f : v[j] > 0.0f ? kRounder + 1.0f : kRounder;
+    t[j] = __builtin_amdgcn_fmed3f(t[j], least, kRounder + (kRectified ? 255.0f : 127.0f));
   }
   *reinterpret_cast<uint2*>(codes + (int64_t)row * d + unit * 8) = e == 255 ? make_uint2(0, 0) : low_bytes8(t);
   if (unit % 4 == 0) exponents[(int64_t)row * (padded / 4) + unit / 4] = (uint8_t)e;

@@ -252,3 +252,46 @@ def test_poison_in_large_layers(n, i, o, dtype, rectified):
     rest[[64, n // 2, n - 1]] = False
     assert torch.isnan(dirty.bias[-1]) and torch.equal(dirty.x[rest], clean.x[rest])
     assert torch.equal(dirty.x[64, 32:], clean.x[64, 32:]) and torch.equal(dirty.x[n - 1, :last], clean.x[n - 1, :last])
+
+
+@pytest.mark.parametrize("rectified", [False, True])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,d", [(7, 16), (40, 80), (2000, 112)])
+def test_pack_of_the_largest_finite_values(n, d, dtype, rectified):
+    """Finite values stay finite and within a step, up to the type's largest: where the least step that fits the codes would make
+    2^128 of one, it is the step below, and codes past the last one are the last one."""
+    most, top = 255 if rectified else 127, torch.finfo(dtype).max
+    g = torch.Generator().manual_seed(n)
+    x = torch.randn(n, d, generator=g) * 2.0 ** (120 + 7 * torch.rand(n, d, generator=g))
+    limit = (most + 0.5) * 2.0 ** (120 if rectified else 121)                # from here on the definition's code is 2^128
+    hard = torch.tensor([top, -top, limit, -limit, float(torch.nextafter(torch.tensor(limit), torch.tensor(0.0))), 1.0])
+    x[torch.arange(n), torch.arange(n) % d] = hard[torch.arange(n) % 6]      # alone in its block, or beside others of its size
+    x[n // 2] = top
+    x = x.to(dtype)
+    x = torch.where(torch.isinf(x), torch.tensor(top, dtype=dtype).copysign(x), x)
+    assert torch.isfinite(x).all() and (x == top).any()
+    p = M.pack_activations(x.cuda(), rectified=rectified)
+    codes, exponents = p.codes.cpu().double(), p.exponents.cpu()
+    v = x.double().clamp_min(0.0) if rectified else x.double()
+    big = torch.nn.functional.pad(v, (0, -d % 32)).view(n, -1, 32).abs().amax(2)
+    e = packed(x, rectified)[1].double()
+    e = torch.where(big >= limit, e - 1, e)
+    assert torch.equal(exponents.double(), e), (exponents.double() != e).nonzero()[:4].tolist()
+    steps = torch.exp2(e - 127).repeat_interleave(32, 1)[:, :d]
+    q = torch.round(v / steps).clamp(-most, most)
+    if rectified:
+        q = torch.where((v > 0) & (q < 1), 1.0, q)
+    assert torch.equal(codes, q), (codes != q).nonzero()[:4].tolist()
+    for to in (torch.float32, torch.bfloat16):
+        held = M.unpack_activations(p, dtype=to).cpu()
+        assert torch.isfinite(held).all() and torch.equal(held.double(), codes * steps)
+        assert ((held.double() - v).abs() <= steps).all()
+    # and the gradients of such values: w's are the sums of the values held
+    o = 48
+    gz = (torch.randn(n, o, generator=g) * 2.0 ** -30).to(dtype)
+    w = torch.randn(o, d, generator=g).to(dtype)
+    got = M.layer_grad_packed(p, w.cuda(), gz.cuda(), relu_input=rectified)
+    gd, held = gz.double(), codes * steps
+    near(got.weight, gd.t() @ held, bound(gd.t(), held) + n * 2.0 ** -126, "weight")
+    want = torch.where(held > 0, gd @ w.double(), 0.0) if rectified else gd @ w.double()
+    near(got.x, want, bound(gd, w.double()) + ROUND[dtype] * want.abs(), "x")
