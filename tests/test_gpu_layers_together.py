@@ -309,3 +309,23 @@ def test_a_fit_from_checkpoints_replays_from_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+def test_a_fit_from_checkpoints_holds_less():
+    """Bytes of a Fit's layers, plain and with the hidden ones kept in 8 bits: one buffer for the values of one hidden layer, two for
+    more, a byte a value kept and one for every 32."""
+    n = 40000
+    for dims, dtype in (((64, 128, 32), torch.float32), ((256, 512, 64), torch.bfloat16), ((256, 512, 512, 64), torch.bfloat16),
+                        ((16, 48, 80, 32, 16), torch.bfloat16), ((32, 16), torch.float32)):
+        size, hidden = torch.finfo(dtype).bits // 8, dims[1:-1]
+        held = {}
+        for kept in (False, True):
+            w, b = network(dims, dtype, 5)
+            f = F.Fit(w, b, n, packed=kept)
+            tensors = [*f.hidden, *f.g_z, *(t for p in f.kept or () for t in p)]
+            held[kept] = sum({t.untyped_storage().data_ptr(): t.untyped_storage().nbytes() for t in tensors}.values())
+        logits = 2 * n * size * dims[-1]
+        buffers = min(2, len(hidden)) * n * size * max(hidden, default=0)
+        assert held[False] == logits + 2 * n * size * sum(hidden), (dims, held)
+        assert held[True] == logits + buffers + n * sum(h + -(-h // 32) for h in hidden), (dims, held)
+        assert held[True] < held[False] or not hidden, (dims, held)
