@@ -10,6 +10,8 @@
 namespace maestro {
 namespace {
 
+using namespace grouped_bf16;
+
 template <int TP, int TQ, int kDepth>
 struct GroupedRows : GroupedRowsWay<8> {
   const Product& g;
@@ -123,20 +125,9 @@ void launch_tiles(Product g, const Out& out, const int64_t* offsets, int32_t n_g
   rows_kernel<WP, WQ, 64, 2, kPT, kWaves><<<blocks, 64 * kWaves, 0, stream>>>(g, out, offsets, n_groups, (int32_t)n);
 }
 
-// Tile by how many there are, as for a layer of one group. 256 x 256 ones by eight wavefronts, two to a SIMD, or by four: the layer
-// with eight 546 us, four 544 (262,139 x 1024 -> 1024, 16 groups); the input's gradient, whose mask wants registers, 612 and 575.
-// The input's gradient no wider than 64 takes tiles that are not either (us, both gradients, 128 x 128 / 64 x 64: 100,000 x 64 -> 64 28.0 / 23.8, 100,000 x
-// 16 -> 256 36.7 / 30.5, 200,000 x 48 -> 1024 186 / 180); the layer does not gain (63,399 x 112 -> 48 8.4 / 9.9).
-template <bool kPT>
-int tile_of(int64_t np, int64_t n) {
-  if (kPT && np <= 64) return 64;
-  if (fits256(np) && cdiv(np, 256) * (n / 256) >= 2 * kCus) return 256;
-  return cdiv(np, 128) * (n / 128) >= kCus ? 128 : 64;
-}
-
 template <bool kPT, class Out>
 void launch_rows(const Product& g, const Out& out, const int64_t* offsets, int32_t n_groups, int64_t n, hipStream_t stream) {
-  const int tile = tile_of<kPT>(g.np, n);
+  const int tile = tile_of(kPT, g.np, n);
   if (tile == 256) {
     if constexpr (kPT) launch_tiles<4, 4, kPT, 4>(g, out, offsets, n_groups, n, stream);
     else launch_tiles<4, 2, kPT, 8>(g, out, offsets, n_groups, n, stream);
@@ -145,34 +136,6 @@ void launch_rows(const Product& g, const Out& out, const int64_t* offsets, int32
   } else {
     launch_tiles<1, 1, kPT, 4>(g, out, offsets, n_groups, n, stream);
   }
-}
-
-// Tile of the weights' gradient and rows of a unit, as for a layer of one group. by_group: too few rows for a unit of them
-// in every workgroup. 64 x 64 tiles and units of 512 rows of a group where four to a CU hold them all. Measured (us, 64 x 64 / 256 x 64 or 128 x 128): 300 rows in 5
-// groups 256 -> 512 5.8 / 7.9, 4,000 in 4 256 -> 256 12.1 / 15.8, 8,000 in 16 512 -> 64 10.3 / 14.0, 20,000 in 60 128 -> 128 9.8 / 12.8.
-struct Cut {
-  int32_t tp, tq;
-  int64_t k_split, most;
-  bool by_group;
-};
-Cut cut_of(int64_t n, int64_t n_groups, int64_t d_in, int64_t d_out) {
-  Cut c;
-  const WeightTile tile = weight_tile(n, d_in, d_out);
-  c.tp = tile.tp, c.tq = tile.tq;
-  const int64_t tiles = cdiv(d_in, c.tp) * cdiv(d_out, c.tq), resident = c.tq == 256 ? 1 : 2;
-  int64_t splits = kCus * resident / tiles;
-  c.by_group = splits > cdiv(n, 512);
-  if (c.by_group) splits = cdiv(n, 512);
-  if (splits < 1) splits = 1;
-  c.k_split = cdiv(cdiv(n, splits), 64) * 64;
-  c.most = n / c.k_split + n_groups;
-  if ((n / 512 + n_groups) * cdiv(d_in, 64) * cdiv(d_out, 64) <= 4 * kCus) {
-    c.tp = c.tq = 64;
-    c.by_group = true;
-    c.k_split = cdiv(cdiv(n, cdiv(n, 512)), 64) * 64;
-    c.most = n / c.k_split + n_groups;
-  }
-  return c;
 }
 
 template <int WP, int WQ, int kDepth, int kBufs, int kWaves>
@@ -224,7 +187,7 @@ maestro_status launch_grouped_grad_bf16(int64_t n, int32_t n_groups, int32_t d_i
   const Product gw{xb, gz, d_in, d_out, d_in, d_out, n, c.k_split, 1, 0, 0};
   const GroupedWeightGrad out{g_weight, g_bias, gw_parts, gb_parts, 1};
   const bool alone = n <= c.k_split;
-  if (g_x && c.tp == 64 && tile_of<true>(d_in, n) == 64) {
+  if (g_x && paired(c, n, d_in)) {
     launch_pair(gx, x_out, gw, out, offsets, n_groups, (int32_t)n, alone, stream);
   } else {
     if (g_x) launch_rows<true>(gx, x_out, offsets, n_groups, n, stream);

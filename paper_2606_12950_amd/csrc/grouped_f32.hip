@@ -9,6 +9,8 @@
 namespace maestro {
 namespace {
 
+using namespace grouped_f32;
+
 template <int T>
 struct GroupedRows : GroupedRowsWay<1> {
   const Product& g;
@@ -149,35 +151,11 @@ __global__ __launch_bounds__(kThreads) void join_groups_kernel(int32_t n, int32_
   }
 }
 
-// 128 x 128 tiles where there are two rounds of them, else 64 x 64, as a layer of one group.
-bool wide(int64_t np, int64_t n) { return np > 64 && cdiv(np, 128) * (n / 128) >= 2 * kCus; }
-
 template <int W, bool kPT, class Out>
 void launch_rows(Product g, const Out& out, const int64_t* offsets, int32_t n_groups, int64_t n, hipStream_t stream) {
   g.p_tiles = cdiv(g.np, 64 * W);
   const int64_t most = (n / (64 * W) + n_groups) * g.p_tiles;
   rows_kernel<W, kPT><<<(unsigned)(most < 65536 ? most : 65536), kThreads, 0, stream>>>(g, out, offsets, n_groups, (int32_t)n);
-}
-
-// As for a layer of one group, and twice the workgroups where each has 256 rows then (150,000 x 80 -> 160 in 10 groups 92 / 83 us). by_group: too few rows for a unit of 256 in every workgroup; units of 128 then (us, weights' gradient, 256 / 128 / 64 rows:
-// 4,096 x 64 -> 128 in 3 groups 14.7 / 11.4 / 10.6, with the input's 14.8 / 11.7 / 12.8, 20,000 x 128 -> 128 in 30 both 29.8 / 26.7 / 26.7).
-struct Cut {
-  bool wide, by_group;
-  int64_t k_split, most;             // rows of a unit, and the most units
-};
-Cut cut_of(int64_t n, int64_t n_groups, int64_t d_in, int64_t d_out) {
-  Cut c;
-  const int64_t large = 4 * cdiv(d_in, 128) * cdiv(d_out, 128), small = cdiv(d_in, 64) * cdiv(d_out, 64);
-  c.wide = d_in > 64 && d_out > 64 && n >= 32768 && 5 * large <= 6 * small;
-  const int64_t t = c.wide ? 128 : 64, tiles = cdiv(d_in, t) * cdiv(d_out, t);
-  int64_t splits = (c.wide || 4 * kCus / tiles > n / 256 ? 2 : 4) * kCus / tiles;
-  c.by_group = splits > cdiv(n, 256);
-  const int64_t least = n <= 256 ? 256 : 128;
-  if (splits > cdiv(n, least)) splits = cdiv(n, least);
-  if (splits < 1) splits = 1;
-  c.k_split = cdiv(cdiv(n, splits), kDepth) * kDepth;
-  c.most = n / c.k_split + n_groups;
-  return c;
 }
 
 template <int W>
@@ -197,7 +175,7 @@ maestro_status launch_layer_grouped_f32(int64_t n, int32_t n_groups, int32_t d_i
                                         hipStream_t stream) {
   const Product g{{weight, d_in}, {x, d_in}, d_out, n, d_in, d_in, 1, 0, 0};
   const Forward out{bias, y, relu};
-  if (wide(d_out, n) && d_in >= 192 && cdiv(d_out, 64) % 2 == 0) launch_rows<2, false>(g, out, offsets, n_groups, n, stream);
+  if (wide_forward(d_out, n, d_in)) launch_rows<2, false>(g, out, offsets, n_groups, n, stream);
   else launch_rows<1, false>(g, out, offsets, n_groups, n, stream);
   return launch_status();
 }
@@ -220,7 +198,7 @@ maestro_status launch_grouped_grad_f32(int64_t n, int32_t n_groups, int32_t d_in
   Product gw{{x, d_in}, {g_z, d_out}, d_in, d_out, n, c.k_split, 1, 0, 0};
   const GroupedWeightGrad out{g_weight, g_bias, gw_parts, gb_parts};
   const bool alone = n <= c.k_split;
-  if (g_x && c.by_group && !c.wide && !wide(d_in, n)) {
+  if (g_x && paired(c, n, d_in)) {
     gx.p_tiles = cdiv(d_in, 64);
     gw.p_tiles = cdiv(d_in, 64);
     const int64_t rows = (n / 64 + n_groups) * gx.p_tiles, sums = c.most * gw.p_tiles * cdiv(d_out, 64);
@@ -240,7 +218,7 @@ maestro_status launch_join_groups(int64_t n, int32_t n_groups, const int64_t* of
                                   const float* gw_parts, float* gw, int64_t size, const float* gb_parts, float* gb, int32_t d_out,
                                   hipStream_t stream) {
   const int64_t quads = size / 4 + d_out / 4;
-  const bool dealt = cdiv(quads, kThreads) * n_groups <= kCus / 2 && n / k_split > 8;
+  const bool dealt = join_dealt(n, n_groups, k_split, size, d_out);
   const int64_t blocks = cdiv(quads, dealt ? kThreads / 16 : kThreads);
   auto kernel = dealt ? by_group ? join_groups_kernel<kTiles, 16> : join_groups_kernel<kShares, 16>
                       : by_group ? join_groups_kernel<kTiles, 1> : join_groups_kernel<kShares, 1>;

@@ -94,13 +94,12 @@ __global__ __launch_bounds__(256) void quantize_kernel(int64_t n, int32_t d, int
 
 template <class T>
 void launch_quantize(int64_t n, int32_t d, const T* x, int8_t* codes, float* scale, hipStream_t stream) {
-  int32_t lanes = 2;
-  while (lanes < 64 && lanes < d / 8) lanes *= 2;
-  const int64_t rows = 256 / lanes, each = (d / 8 + lanes - 1) / lanes;
+  const int8::RowLanes l = int8::row_lanes(d);
+  const int64_t rows = 256 / l.lanes;
   const unsigned blocks = (unsigned)((n + rows - 1) / rows);
-  auto kernel = each <= 1 ? quantize_kernel<T, 1> : each <= 2 ? quantize_kernel<T, 2> : each <= 4 ? quantize_kernel<T, 4>
-              : each <= 8 ? quantize_kernel<T, 8> : quantize_kernel<T, 0>;
-  kernel<<<blocks, 256, 0, stream>>>(n, d, lanes, x, codes, scale);
+  auto kernel = l.units == 1 ? quantize_kernel<T, 1> : l.units == 2 ? quantize_kernel<T, 2> : l.units == 4 ? quantize_kernel<T, 4>
+              : l.units == 8 ? quantize_kernel<T, 8> : quantize_kernel<T, 0>;
+  kernel<<<blocks, 256, 0, stream>>>(n, d, l.lanes, x, codes, scale);
 }
 
 template <int WP, int WQ, int kWaves, class T>
@@ -120,16 +119,12 @@ void launch_tiles(Product g, const Int8Forward<T>& out, hipStream_t stream) {
   int8_kernel<WP, WQ, kWaves, T><<<(unsigned)(want < most ? want : most), 64 * kWaves, 0, stream>>>(g, out);
 }
 
-// 256 x 256 tiles by eight wavefronts, two to a SIMD, so that one's scaling and stores run under the other's products; by four, which
-// read a quarter less of LDS, where a dozen rounds of them or more let the matrix cores' power set the clock. Measured (us with the rows'
-// quantisation, eight / four): 262,139 x 1024 -> 1024 (16 rounds) 500 / 484, 120,001 x 768 -> 1008 (7) 218 / 224, 65,536 x 512 -> 512 (2)
-// 57 / 58; without it 65,536 x 256 -> 512 23.5 / 27.4, 200,000 x 256 -> 256 39.1 / 43.5.
 template <class T>
 void launch_product(const Product& g, const Int8Forward<T>& out, hipStream_t stream) {
-  const int64_t large = cdiv(g.np, 256) * cdiv(g.nq, 256);
-  if (g.np > 128 && large >= 12 * kCus) launch_tiles<4, 4, 4>(g, out, stream);
-  else if (g.np > 128 && large >= 2 * kCus) launch_tiles<4, 2, 8>(g, out, stream);
-  else if (cdiv(g.np, 128) * cdiv(g.nq, 128) >= kCus) launch_tiles<2, 2, 4>(g, out, stream);
+  const int8::ProductTile t = int8::product_tile(g.np, g.nq);
+  if (t.tile == 256 && t.wavefronts == 4) launch_tiles<4, 4, 4>(g, out, stream);
+  else if (t.tile == 256) launch_tiles<4, 2, 8>(g, out, stream);
+  else if (t.tile == 128) launch_tiles<2, 2, 4>(g, out, stream);
   else launch_tiles<1, 1, 4>(g, out, stream);
 }
 

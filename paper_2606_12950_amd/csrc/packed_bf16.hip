@@ -8,6 +8,8 @@
 namespace maestro {
 namespace {
 
+using namespace packed_bf16;
+
 template <int WP, int WQ, bool kQT, int kWaves, class Out>
 __global__ __launch_bounds__(64 * kWaves, (Tile<WP, WQ, 64, 2, Out, kWaves>::kSimdWaves)) void product_kernel(Product g, Out out) {
   using L = Tile<WP, WQ, 64, 2, Out, kWaves>;
@@ -45,37 +47,6 @@ template <int WP, int WQ, class Code>
 void launch_pair(Product gx, const CodesInputGrad& x, Product gw, const CodesWeightGrad<Code>& w, hipStream_t stream) {
   const uint32_t blocks = plan<Tile<1, 1, 64, 2, CodesInputGrad>>(gx), more = plan<Tile<WP, WQ, 64, 2, CodesWeightGrad<Code>>>(gw);
   pair_kernel<WP, WQ><<<blocks + more, kThreads, 0, stream>>>(gx, x, blocks, gw, w);
-}
-
-// As for the gradients of an input in bfloat16, but the input's 64 wide where it is no wider (us, 128 x 128 / 64 x 64, both gradients: 100,000 x 64
-// -> 64 24.6 / 19.8, 100,000 x 16 -> 256 36.4 / 33.6, 200,000 x 48 -> 1024 190 / 196, 40,000 x 64 -> 512 34.5 / 29.0), and for little work 64 x 64 tiles of the weights' gradient, with splits of 256 rows
-// or more, where four to a CU hold them all. Measured (us, both gradients, 64 x 64 with 256 / 512 rows / the larger tiles): 300 x 256 -> 512
-// 9.1 / 6.8 (one split) / 11.7 (weights), 1,000 x 1024 -> 64 9.3 / 11.5, 4,000 x 256 -> 256 11.5 / 12.8, 30,000 x 64 -> 128 13.8 / 15.0 / 17.0 (weights).
-int tile_of(int64_t np, int64_t nq) {
-  if (np <= 64) return 64;
-  if (fits256(np) && cdiv(np, 256) * cdiv(nq, 256) >= 2 * kCus) return 256;
-  return cdiv(np, 128) * cdiv(nq, 128) >= kCus ? 128 : 64;
-}
-
-struct Cut {
-  int32_t tp, tq;
-  int64_t k_split, splits;
-  int32_t parts;
-};
-Cut cut_of(int64_t n, int64_t d_in, int64_t d_out) {
-  Cut c;
-  const WeightTile tile = weight_tile(n, d_in, d_out);
-  c.tp = tile.tp, c.tq = tile.tq;
-  int64_t tiles = cdiv(d_in, c.tp) * cdiv(d_out, c.tq), most = kCus * (c.tq == 256 ? 1 : 2), least = 512;
-  const int64_t small = cdiv(d_in, 64) * cdiv(d_out, 64), few = n <= 512 ? 512 : 256;
-  if (small * cdiv(n, few) <= 4 * kCus) c.tp = c.tq = 64, tiles = small, most = 4 * kCus, least = few;
-  int64_t splits = most / tiles;
-  if (splits > cdiv(n, least)) splits = cdiv(n, least);
-  if (splits < 1) splits = 1;
-  c.k_split = cdiv(cdiv(n, splits), 64) * 64;
-  c.splits = cdiv(n, c.k_split);
-  c.parts = c.splits > 1 ? (int32_t)cdiv(d_in, c.tp) : 1;
-  return c;
 }
 
 template <class Code>

@@ -6,6 +6,8 @@
 namespace maestro {
 namespace {
 
+using namespace packed_f32;
+
 template <int W, bool kQT, class P, class Out>
 __global__ __launch_bounds__(kThreads, 2) void product_kernel(ProductOf<P> g, Out out) {
   __shared__ __attribute__((aligned(16))) Lds<W> lds;
@@ -35,35 +37,13 @@ void launch(ProductOf<P> g, const Out& out, hipStream_t stream) {
   product_kernel<W, kQT><<<blocks, kThreads, 0, stream>>>(g, out);
 }
 
-bool wide(int64_t np, int64_t nq) { return np > 64 && nq > 64 && cdiv(np, 128) * cdiv(nq, 128) >= 2 * kCus; }
-
-// The weights' gradient's tiles as for an input in float32; the rows split so that there are about two workgroups a CU, four where each has 256 rows
-// then. Measured (us, two / four): 150,000 x 80 -> 160 98 / 88, 66,255 x 256 -> 16 37.8 / 34.1, 131,365 x 48 -> 240 62 / 57, 200,000 x 64 -> 64 32.5 / 32.7.
-constexpr int64_t kLeastRows = 64;
-struct Cut {
-  bool wide;
-  int64_t k_split, splits;
-};
-Cut cut_of(int64_t n, int64_t d_in, int64_t d_out) {
-  Cut c;
-  const int64_t large = 4 * cdiv(d_in, 128) * cdiv(d_out, 128), small = cdiv(d_in, 64) * cdiv(d_out, 64);
-  c.wide = d_in > 64 && d_out > 64 && n >= 32768 && 5 * large <= 6 * small;
-  const int64_t t = c.wide ? 128 : 64, tiles = cdiv(d_in, t) * cdiv(d_out, t);
-  int64_t splits = (c.wide || 4 * kCus / tiles > n / 256 ? 2 : 4) * kCus / tiles;
-  if (splits > cdiv(n, kLeastRows)) splits = cdiv(n, kLeastRows);
-  if (splits < 1) splits = 1;
-  c.k_split = cdiv(cdiv(n, splits), kDepth) * kDepth;
-  c.splits = cdiv(n, c.k_split);
-  return c;
-}
-
 template <class Code>
 void launch_gradients(int64_t n, int32_t d_in, int32_t d_out, const Codes<Code>& x, const float* weight, const float* gz,
                       bool relu_input, float* g_x, const Cut& c, const WeightGrad& w, hipStream_t stream) {
   ProductOf<Codes<Code>> gw{x, {gz, d_out}, d_in, d_out, n, c.k_split, c.splits, 0, 0};
   Product gx{{weight, d_in}, {gz, d_out}, d_in, n, d_out, d_out, 1, 0, 0};
   const CodesInputGrad x_out{reinterpret_cast<const unsigned char*>(x.m), g_x, relu_input};
-  if (g_x && !c.wide && !wide(d_in, n)) {
+  if (g_x && paired(c, n, d_in)) {
     const uint32_t blocks = plan<1>(gx), more = plan<1>(gw);
     pair_kernel<<<blocks + more, kThreads, 0, stream>>>(gx, x_out, blocks, gw, w);
     return;

@@ -16,6 +16,7 @@
 #include <type_traits>
 
 #include "mlp.h"
+#include "rules.h"
 #include "train.h"
 
 namespace maestro {
@@ -893,26 +894,6 @@ __device__ __forceinline__ void product(const Product& g, const Out& out, const 
     }
   }
   wait_loads<0>();                                          // no load into LDS outlives the workgroup
-}
-
-int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
-constexpr int64_t kCus = 256;
-
-// Widths that tiles of 256 fit as well as tiles of 128, nearly: those above 128, but for 257 .. 384. Measured (us, 256 / 128): grouped
-// layers 100,000 x 256 -> 384 43 / 37, 1024 -> 304 108 / 97, 200,000 x 512 -> 640 190 / 196; packed gradients 100,000 x 384 -> 512 172 / 156.
-bool fits256(int64_t width) { return 5 * cdiv(width, 128) > 8 * cdiv(width, 256); }
-
-// Tile of a weights' gradient, of d_in and of d_out: 256 x 256 for many rows where it fits, 256 x 64 for few outputs, else 128 x 128.
-// Measured (us, 256 x 256 / 128 x 128, kept bytes and then groups): 262,139 x 1024 -> 1024 545 / 687 and 540 / 637, 146,481 x 288 -> 896
-// 175 / 157 and 177 / 144, 140,000 x 768 -> 512 149 / 173 and 167 / 159; 256 x 64 / 128 x 128: 100,000 x 512 -> 512 98 / 88 and 82 / 81,
-// 60,000 x 256 -> 128 23.7 / 22.4 and 23.7 / 23.7, 40,000 x 512 -> 64 22.2 / 24.6.
-struct WeightTile {
-  int32_t tp, tq;
-};
-WeightTile weight_tile(int64_t n, int64_t d_in, int64_t d_out) {
-  const int64_t large = 4 * cdiv(d_in, 256) * cdiv(d_out, 256), small = cdiv(d_in, 128) * cdiv(d_out, 128);
-  if (d_in > 128 && d_out > 128 && n >= 131072 && 5 * large <= 6 * small) return {256, 256};
-  return d_in > 128 && d_out <= 64 ? WeightTile{256, 64} : WeightTile{128, 128};
 }
 
 }  // namespace

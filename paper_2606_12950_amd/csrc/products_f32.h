@@ -9,12 +9,13 @@
 #include <type_traits>
 
 #include "mlp.h"
+#include "rules.h"
 #include "train.h"
 
 namespace maestro {
 namespace {
 
-constexpr int kThreads = 256, kDepth = 16;
+constexpr int kThreads = 256, kDepth = kDepthF32;
 
 // An operand in memory, rows of ld values: four neighbouring ones of a row.
 struct Floats {
@@ -238,9 +239,6 @@ __device__ __forceinline__ void product(const ProductOf<P>& g, const Out& out, c
     }
   }
 }
-
-int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
-constexpr int64_t kCus = 256;
 
 }  // namespace
 }  // namespace maestro

@@ -1,0 +1,115 @@
+"""Every kernel that the rules by size of the layers by role, in 8-bit integers and from kept bytes choose is run by a size of the GPU
+tests: a rule that changes takes no kernel out of them unseen. The rules are host code (csrc/rules.h), compiled here."""
+import ctypes
+import os
+import random
+import shutil
+import subprocess
+
+import pytest
+
+import layer_forms
+import test_gpu_grouped
+import test_gpu_int8
+import test_gpu_packed
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2606_12950_amd", "csrc")
+
+# What a call launches, as words. A weights' gradient: its tile, s for shares across the groups, g for units by group, 1 where no second
+# launch follows. Operators are called with the input's gradient (x) and without.
+SOURCE = r"""
+#include "rules.h"
+#include <string>
+using namespace maestro;
+typedef std::string S;
+static S text(int64_t v) { return std::to_string(v); }
+static S tile(int64_t p, int64_t q) { return text(p) + "x" + text(q); }
+static S grouped(int64_t n, int64_t groups, int64_t i, int64_t o, bool bf16, bool x) {
+  const bool pair = bf16 ? grouped_bf16::paired(grouped_bf16::cut_of(n, groups, i, o), n, i) : grouped_f32::paired(grouped_f32::cut_of(n, groups, i, o), n, i);
+  S out, cut;
+  int64_t k;
+  bool by_group;
+  if (bf16) {
+    const auto c = grouped_bf16::cut_of(n, groups, i, o);
+    k = c.k_split, by_group = c.by_group, cut = tile(c.tp, c.tq);
+    out = "y" + text(grouped_bf16::tile_of(false, o, n));
+    if (x && !pair) out += " gx" + text(grouped_bf16::tile_of(true, i, n));
+  } else {
+    const auto c = grouped_f32::cut_of(n, groups, i, o);
+    k = c.k_split, by_group = c.by_group, cut = c.wide ? "128" : "64";
+    out = grouped_f32::wide_forward(o, n, i) ? "y128" : "y64";
+    if (x && !pair) out += grouped_f32::wide(i, n) ? " gx128" : " gx64";
+  }
+  out += S(x && pair ? " pair" : " gw") + cut + (by_group ? "g" : "s") + (n <= k ? "1" : "");
+  if (n > k) out += S(" join") + (by_group ? "g" : "s") + (grouped_f32::join_dealt(n, groups, k, i * o, o) ? "16" : "");
+  return out;
+}
+static S packed(int64_t n, int64_t i, int64_t o, bool bf16, bool x) {
+  if (bf16) {
+    const auto c = packed_bf16::cut_of(n, i, o);
+    const int t = packed_bf16::tile_of(i, n);
+    const S cut = tile(c.tp, c.tq) + (c.splits == 1 ? "1" : "");
+    return !x ? "gw" + cut : t == 64 ? "pair" + cut : "gx" + text(t) + " gw" + cut;
+  }
+  const auto c = packed_f32::cut_of(n, i, o);
+  const S cut = S(c.wide ? "128" : "64") + (c.splits == 1 ? "1" : "");
+  return !x ? "gw" + cut : packed_f32::paired(c, n, i) ? "pair" + cut : S(packed_f32::wide(i, n) ? "gx128" : "gx64") + " gw" + cut;
+}
+static S quantised(int64_t n, int64_t i, int64_t o) {
+  const auto l = int8::row_lanes((int32_t)i);
+  const auto t = int8::product_tile(o, n);
+  return "rows" + text(l.units) + " y" + tile(t.tile, t.wavefronts);
+}
+extern "C" void form(int op, int64_t n, int64_t groups, int64_t i, int64_t o, int bf16, int x, char* out, size_t size) {
+  const S s = op == 0 ? grouped(n, groups, i, o, bf16, x) : op == 1 ? packed(n, i, o, bf16, x) : quantised(n, i, o);
+  s.copy(out, size - 1);
+  out[s.size() < size ? s.size() : size - 1] = 0;
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def forms(tmp_path_factory):
+    d = tmp_path_factory.mktemp("rules")
+    source, lib = str(d / "forms.cpp"), str(d / "forms.so")
+    open(source, "w").write(SOURCE)
+    compiler = os.environ.get("CXX") or shutil.which("g++") or "/opt/rocm/bin/amdclang++"
+    subprocess.run([compiler, "-O1", "-std=c++17", "-shared", "-fPIC", "-Wall", "-Werror", f"-I{CSRC}", source, "-o", lib], check=True)
+    call = ctypes.CDLL(lib).form
+    call.argtypes = [ctypes.c_int, *[ctypes.c_int64] * 4, ctypes.c_int, ctypes.c_int, ctypes.c_char_p, ctypes.c_size_t]
+    call.restype = None
+    text = ctypes.create_string_buffer(256)
+
+    def of(op, n, groups, i, o, bf16, x):
+        call(op, n, groups, i, o, bf16, x, text, 256)
+        return text.value.decode().split()
+    return of
+
+
+def sizes_of(test):
+    """The sizes that a test is parametrized with."""
+    return [tuple(v) for m in test.pytestmark if m.name == "parametrize" and m.args[0].endswith("i,o") for v in m.args[1]]
+
+
+TESTED = {
+    0: [(sum(s), len(s), i, o) for t in (test_gpu_grouped.test_groups, test_gpu_grouped.test_many_rows) for s, i, o in sizes_of(t)] +
+       [(sum(s) + 8, len(s), i, o) for s, i, o in layer_forms.GROUPED],
+    1: [(n, 1, i, o) for n, i, o in sizes_of(test_gpu_packed.test_layer_grad_packed) + layer_forms.PACKED],
+    2: [(n, 1, i, o) for n, i, o in sizes_of(test_gpu_int8.test_layer_int8) + layer_forms.INT8] +
+       [(n, 1, d, 16) for t in [test_gpu_int8.test_quantize_rows] for n, d in test_gpu_int8.SHAPES],
+}
+
+
+@pytest.mark.parametrize("op", [0, 1, 2])
+@pytest.mark.parametrize("bf16", [0, 1])
+def test_every_form_is_tested(forms, op, bf16):
+    x = (0, 1) if op < 2 else (0,)
+    tested = {f for n, g, i, o in TESTED[op] for w in x for f in forms(op, n, g, i, o, bf16, w)}
+    r = random.Random(op)
+    chosen = {}
+    span = lambda most: int(round(most ** r.random()))
+    for _ in range(60000):
+        n, g, i, o = span(1 << 27), span(256) if op == 0 else 1, 16 * span(1024), 16 * span(1024)
+        for f in forms(op, n, g, i, o, bf16, r.choice(x)):
+            chosen.setdefault(f, (n, g, i, o))
+    assert not {f: chosen[f] for f in chosen if f not in tested}
