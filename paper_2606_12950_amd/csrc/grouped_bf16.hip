@@ -145,7 +145,9 @@ void launch_sums(Product g, const GroupedWeightGrad& out, const int64_t* offsets
   g.p_tiles = (int32_t)cdiv(g.np, L::TP);
   const int64_t pieces = by_group ? n / g.k_split + n_groups : cdiv(n, g.k_split);
   const uint32_t blocks = blocks_of(pieces * g.p_tiles * cdiv(g.nq, L::TQ), L::kResident);
-  auto kernel = by_group ? sums_kernel<WP, WQ, kDepth, kBufs, kWaves, kTiles> : sums_kernel<WP, WQ, kDepth, kBufs, kWaves, kShares>;
+  auto kernel = sums_kernel<WP, WQ, kDepth, kBufs, kWaves, kShares>;
+  if constexpr (WP * WQ < 8)                                // 256 x 256 tiles: from 131,072 rows on, never by group
+    if (by_group) kernel = sums_kernel<WP, WQ, kDepth, kBufs, kWaves, kTiles>;
   kernel<<<blocks, 64 * kWaves, 0, stream>>>(g, out, offsets, n_groups, n, alone);
 }
 

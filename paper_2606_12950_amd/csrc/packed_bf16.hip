@@ -53,9 +53,8 @@ template <class Code>
 void launch_gradients(int64_t n, const Product& gx, const CodesInputGrad& x, const Product& gw, const CodesWeightGrad<Code>& w,
                       const Cut& c, hipStream_t stream) {
   const int tile = tile_of(gx.np, n);
-  if (x.c && tile == 64) {
+  if (x.c && tile == 64) {                                  // few enough tiles for it: c.tp is not 256 by any size
     if (c.tp == 64) launch_pair<1, 1>(gx, x, gw, w, stream);
-    else if (c.tp == 256) launch_pair<4, 1>(gx, x, gw, w, stream);
     else launch_pair<2, 2>(gx, x, gw, w, stream);
     return;
   }

@@ -113,3 +113,20 @@ def test_every_form_is_tested(forms, op, bf16):
         for f in forms(op, n, g, i, o, bf16, r.choice(x)):
             chosen.setdefault(f, (n, g, i, o))
     assert not {f: chosen[f] for f in chosen if f not in tested}
+
+
+def test_forms_that_no_size_chooses(forms):
+    """The launchers have no kernel for these: bfloat16 gradients of kept bytes in one launch beside 256-wide tiles of the weights', and
+    256 x 256 tiles of the groups' weights' gradient by group."""
+    r = random.Random(7)
+    span = lambda low, most: int(round(low * (most / low) ** r.random()))
+    for _ in range(60000):
+        n, i, o = span(1, 1 << 28), 16 * span(1, 1024), 16 * span(1, 1024)
+        narrow = 16 * r.randint(1, 4)                         # 256 x 64 tiles' outputs
+        assert not {f for f in (*forms(1, n, 1, i, o, 1, 1), *forms(1, n, 1, i, narrow, 1, 1)) if f.startswith("pair256")}, (n, i, o, narrow)
+        assert not {f for f in forms(0, n, span(1, 256), i, o, 1, 1) if f.startswith("gw256x256g")}, (n, i, o)
+    # at the edges of both rules: the least rows that leave a 64-wide tile, and the most that stay in one
+    for i in range(144, 16385, 16):
+        for o in (16, 48, 64):
+            for n in {k + d for k in (128 * 255 // -(-i // 128), 128 * 256 // -(-i // 128), 512, 131072) for d in range(-2, 131)} - {0}:
+                assert not {f for f in forms(1, max(n, 1), 1, i, o, 1, 1) if f.startswith("pair256")}, (n, i, o)
