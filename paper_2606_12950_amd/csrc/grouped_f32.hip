@@ -109,8 +109,9 @@ __global__ __launch_bounds__(kThreads) void join_groups_kernel(int32_t n, int32_
   GroupTable table;
   table.build<kUnits>(offsets, n_groups, n, k_split);
   const int group = blockIdx.y;
-  const int first = table.first_unit(group), last = table.first_unit(group + 1);
-  if (last - first == 1) return;
+  const int units = table.first_unit(group + 1) - table.first_unit(group);
+  if (units == 1) return;
+  const int first = first_slot(group, table.first_row(group) - table.first_row(0), k_split), last = first + units;
   constexpr int kQuads = kThreads / G;
   const int part = threadIdx.x / kQuads, own = threadIdx.x % kQuads;
   const int64_t quads = size / 4, all = quads + d_out / 4;
@@ -182,8 +183,8 @@ maestro_status launch_layer_grouped_f32(int64_t n, int32_t n_groups, int32_t d_i
 
 size_t grouped_grad_f32_workspace_bytes(int64_t n, int32_t n_groups, int32_t d_in, int32_t d_out) {
   if (n == 0) return 0;
-  const Cut c = cut_of(n, n_groups, d_in, d_out);
-  return n <= c.k_split ? 0 : sizeof(float) * (size_t)(c.most * ((int64_t)d_in + 1) * d_out);
+  const Cut c = cut_of(n, d_in, d_out);
+  return n <= c.k_split ? 0 : sizeof(float) * (size_t)(slots_of(n, n_groups, c.k_split) * ((int64_t)d_in + 1) * d_out);
 }
 
 maestro_status launch_grouped_grad_f32(int64_t n, int32_t n_groups, int32_t d_in, int32_t d_out, const float* x,
@@ -191,8 +192,8 @@ maestro_status launch_grouped_grad_f32(int64_t n, int32_t n_groups, int32_t d_in
                                        float* g_x, float* g_weight, float* g_bias, void* workspace, hipStream_t stream) {
   const int64_t size = (int64_t)d_in * d_out;
   if (n == 0) return launch_join_groups(0, n_groups, offsets, 1, true, nullptr, g_weight, size, nullptr, g_bias, d_out, stream);
-  const Cut c = cut_of(n, n_groups, d_in, d_out);
-  float *gw_parts = static_cast<float*>(workspace), *gb_parts = gw_parts + c.most * size;
+  const Cut c = cut_of(n, d_in, d_out);
+  float *gw_parts = static_cast<float*>(workspace), *gb_parts = gw_parts + slots_of(n, n_groups, c.k_split) * size;
   Product gx{{weight, d_in}, {g_z, d_out}, d_in, n, d_out, d_out, 1, 0, 0};
   const InputGrad x_out{x, g_x, relu_input};
   Product gw{{x, d_in}, {g_z, d_out}, d_in, d_out, n, c.k_split, 1, 0, 0};
@@ -201,7 +202,7 @@ maestro_status launch_grouped_grad_f32(int64_t n, int32_t n_groups, int32_t d_in
   if (g_x && paired(c, n, d_in)) {
     gx.p_tiles = cdiv(d_in, 64);
     gw.p_tiles = cdiv(d_in, 64);
-    const int64_t rows = (n / 64 + n_groups) * gx.p_tiles, sums = c.most * gw.p_tiles * cdiv(d_out, 64);
+    const int64_t rows = (n / 64 + n_groups) * gx.p_tiles, sums = (n / c.k_split + n_groups) * gw.p_tiles * cdiv(d_out, 64);
     const uint32_t blocks = (uint32_t)(rows < 65536 ? rows : 65536), more = (uint32_t)(sums < 65536 ? sums : 65536);
     pair_kernel<<<blocks + more, kThreads, 0, stream>>>(gx, x_out, blocks, gw, out, offsets, n_groups, (int32_t)n, alone);
   } else {

@@ -9,6 +9,7 @@
 #include <stdint.h>
 
 #include "maestro_layers.h"
+#include "rules.h"
 
 namespace maestro {
 
@@ -163,11 +164,12 @@ struct GroupedSumsWay {
     const int g = kUnits == kTiles ? table.group_of_unit(piece) : table.group_of_row(c.row);
     const int first = table.first_unit(g), row = table.first_row(g), group_end = table.first_row(g + 1);
     const bool direct = table.first_unit(g + 1) - first == 1;
+    const int rows_before = row - table.first_row(0), slot = first_slot(g, rows_before, per);
     if constexpr (kUnits == kTiles) {
       const int k0 = row + (piece - first) * per;
-      return Place{g, tile, piece, k0, group_end - k0 < per ? group_end : k0 + per, direct};
+      return Place{g, tile, slot + piece - first, k0, group_end - k0 < per ? group_end : k0 + per, direct};
     }
-    return Place{g, tile, first + piece - quotient(row - table.first_row(0), per), c.row, group_end < c.end ? group_end : c.end, direct};
+    return Place{g, tile, slot + piece - quotient(rows_before, per), c.row, group_end < c.end ? group_end : c.end, direct};
   }
 };
 

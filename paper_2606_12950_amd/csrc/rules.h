@@ -33,6 +33,16 @@ inline bool weight_wide_f32(int64_t n, int64_t d_in, int64_t d_out) {
   return d_in > 64 && d_out > 64 && n >= 32768 && 5 * large <= 6 * small;
 }
 
+// The places in the workspace of the groups' weights' gradients. A group whose rows are one unit writes its gradient itself; one of u >= 2
+// units of up to `per` rows has u neighbouring places, from first_slot on. `row`, its first row, and `end`, the next group's, count from the
+// first group's: from row / per to end / per are u - 1 or more and at least one, whether units begin at the group's first row or at multiples of
+// `per`; and min(group, row / per) rises by one then, so that the next group's first place is u or more further.
+constexpr int first_slot(int group, int row, int per) {
+  const int passed = (int)((uint32_t)row / (uint32_t)per);
+  return passed + (group < passed ? group : passed);
+}
+inline int64_t slots_of(int64_t n, int64_t n_groups, int64_t per) { return first_slot((int)n_groups, (int)n, (int)per); }
+
 namespace grouped_bf16 {
 
 // Tile by how many there are, as for a layer of one group. 256 x 256 ones by eight wavefronts, two to a SIMD, or by four: the layer
@@ -50,7 +60,7 @@ inline int tile_of(bool input_grad, int64_t np, int64_t n) {
 // groups 256 -> 512 5.8 / 7.9, 4,000 in 4 256 -> 256 12.1 / 15.8, 8,000 in 16 512 -> 64 10.3 / 14.0, 20,000 in 60 128 -> 128 9.8 / 12.8.
 struct Cut {
   int32_t tp, tq;
-  int64_t k_split, most;
+  int64_t k_split;
   bool by_group;
 };
 inline Cut cut_of(int64_t n, int64_t n_groups, int64_t d_in, int64_t d_out) {
@@ -63,12 +73,10 @@ inline Cut cut_of(int64_t n, int64_t n_groups, int64_t d_in, int64_t d_out) {
   if (c.by_group) splits = cdiv(n, 512);
   if (splits < 1) splits = 1;
   c.k_split = cdiv(cdiv(n, splits), 64) * 64;
-  c.most = n / c.k_split + n_groups;
   if ((n / 512 + n_groups) * cdiv(d_in, 64) * cdiv(d_out, 64) <= 4 * kCus) {
     c.tp = c.tq = 64;
     c.by_group = true;
     c.k_split = cdiv(cdiv(n, cdiv(n, 512)), 64) * 64;
-    c.most = n / c.k_split + n_groups;
   }
   return c;
 }
@@ -88,9 +96,9 @@ inline bool wide_forward(int64_t np, int64_t n, int64_t nk) { return wide(np, n)
 // 4,096 x 64 -> 128 in 3 groups 14.7 / 11.4 / 10.6, with the input's 14.8 / 11.7 / 12.8, 20,000 x 128 -> 128 in 30 both 29.8 / 26.7 / 26.7).
 struct Cut {
   bool wide, by_group;
-  int64_t k_split, most;             // rows of a unit, and the most units
+  int64_t k_split;                   // rows of a unit
 };
-inline Cut cut_of(int64_t n, int64_t n_groups, int64_t d_in, int64_t d_out) {
+inline Cut cut_of(int64_t n, int64_t d_in, int64_t d_out) {
   Cut c;
   c.wide = weight_wide_f32(n, d_in, d_out);
   const int64_t t = c.wide ? 128 : 64, tiles = cdiv(d_in, t) * cdiv(d_out, t);
@@ -100,7 +108,6 @@ inline Cut cut_of(int64_t n, int64_t n_groups, int64_t d_in, int64_t d_out) {
   if (splits > cdiv(n, least)) splits = cdiv(n, least);
   if (splits < 1) splits = 1;
   c.k_split = cdiv(cdiv(n, splits), kDepthF32) * kDepthF32;
-  c.most = n / c.k_split + n_groups;
   return c;
 }
 

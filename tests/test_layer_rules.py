@@ -12,6 +12,7 @@ import layer_forms
 import test_gpu_grouped
 import test_gpu_int8
 import test_gpu_packed
+from paper_2606_12950_amd import _layers
 
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2606_12950_amd", "csrc")
 
@@ -25,7 +26,7 @@ typedef std::string S;
 static S text(int64_t v) { return std::to_string(v); }
 static S tile(int64_t p, int64_t q) { return text(p) + "x" + text(q); }
 static S grouped(int64_t n, int64_t groups, int64_t i, int64_t o, bool bf16, bool x) {
-  const bool pair = bf16 ? grouped_bf16::paired(grouped_bf16::cut_of(n, groups, i, o), n, i) : grouped_f32::paired(grouped_f32::cut_of(n, groups, i, o), n, i);
+  const bool pair = bf16 ? grouped_bf16::paired(grouped_bf16::cut_of(n, groups, i, o), n, i) : grouped_f32::paired(grouped_f32::cut_of(n, i, o), n, i);
   S out, cut;
   int64_t k;
   bool by_group;
@@ -35,7 +36,7 @@ static S grouped(int64_t n, int64_t groups, int64_t i, int64_t o, bool bf16, boo
     out = "y" + text(grouped_bf16::tile_of(false, o, n));
     if (x && !pair) out += " gx" + text(grouped_bf16::tile_of(true, i, n));
   } else {
-    const auto c = grouped_f32::cut_of(n, groups, i, o);
+    const auto c = grouped_f32::cut_of(n, i, o);
     k = c.k_split, by_group = c.by_group, cut = c.wide ? "128" : "64";
     out = grouped_f32::wide_forward(o, n, i) ? "y128" : "y64";
     if (x && !pair) out += grouped_f32::wide(i, n) ? " gx128" : " gx64";
@@ -60,6 +61,7 @@ static S quantised(int64_t n, int64_t i, int64_t o) {
   const auto t = int8::product_tile(o, n);
   return "rows" + text(l.units) + " y" + tile(t.tile, t.wavefronts);
 }
+extern "C" int64_t place(int64_t group, int64_t row, int64_t per) { return first_slot((int)group, (int)row, (int)per); }
 extern "C" void form(int op, int64_t n, int64_t groups, int64_t i, int64_t o, int bf16, int x, char* out, size_t size) {
   const S s = op == 0 ? grouped(n, groups, i, o, bf16, x) : op == 1 ? packed(n, i, o, bf16, x) : quantised(n, i, o);
   s.copy(out, size - 1);
@@ -69,13 +71,18 @@ extern "C" void form(int op, int64_t n, int64_t groups, int64_t i, int64_t o, in
 
 
 @pytest.fixture(scope="module")
-def forms(tmp_path_factory):
+def rules(tmp_path_factory):
     d = tmp_path_factory.mktemp("rules")
     source, lib = str(d / "forms.cpp"), str(d / "forms.so")
     open(source, "w").write(SOURCE)
     compiler = os.environ.get("CXX") or shutil.which("g++") or "/opt/rocm/bin/amdclang++"
     subprocess.run([compiler, "-O1", "-std=c++17", "-shared", "-fPIC", "-Wall", "-Werror", f"-I{CSRC}", source, "-o", lib], check=True)
-    call = ctypes.CDLL(lib).form
+    return ctypes.CDLL(lib)
+
+
+@pytest.fixture(scope="module")
+def forms(rules):
+    call = rules.form
     call.argtypes = [ctypes.c_int, *[ctypes.c_int64] * 4, ctypes.c_int, ctypes.c_int, ctypes.c_char_p, ctypes.c_size_t]
     call.restype = None
     text = ctypes.create_string_buffer(256)
@@ -130,3 +137,38 @@ def test_forms_that_no_size_chooses(forms):
         for o in (16, 48, 64):
             for n in {k + d for k in (128 * 255 // -(-i // 128), 128 * 256 // -(-i // 128), 512, 131072) for d in range(-2, 131)} - {0}:
                 assert not {f for f in forms(1, max(n, 1), 1, i, o, 1, 1) if f.startswith("pair256")}, (n, i, o)
+
+
+@pytest.mark.parametrize("by_group", [False, True])
+def test_places_of_shares(rules, by_group):
+    """No two units of the groups that have two or more share a place, and all lie below the count that sizes the workspace."""
+    rules.place.argtypes, rules.place.restype = [ctypes.c_int64] * 3, ctypes.c_int64
+    r = random.Random(3)
+    for _ in range(3000):
+        groups, per = r.choice([1, 2, 3, 8, 40, 256]), r.choice([1, 2, 5, 64])
+        sizes = [r.choice([0, 1, per - 1, per, per + 1, 2 * per, 2 * per + 1, r.randint(0, 7 * per)]) for _ in range(groups)]
+        n = sum(sizes) + r.choice([0, 0, 1, per])                  # rows of no group
+        taken, row = set(), 0
+        for g, size in enumerate(sizes):
+            units = -(-size // per) if by_group else ((row + size - 1) // per - row // per + 1 if size else 0)
+            if units > 1:
+                first = rules.place(g, row, per)
+                assert first >= 0 and not taken & set(range(first, first + units)), (sizes, per, g)
+                taken |= set(range(first, first + units))
+            row += size
+        assert max(taken, default=-1) < rules.place(groups, n, per), (sizes, per)
+        assert rules.place(groups, n, per) <= min(2 * (n // per), n // per + groups)
+
+
+def test_workspace_of_many_groups():
+    """Groups of few rows write their gradients themselves: the workspace is that of the groups with two units or more, at most two for
+    each unit that the rows fill, and grows with neither the rows' count below it nor the groups'."""
+    ws = _layers.load().maestro_layer_grouped_grad_workspace
+    for n, i, o in ((4096, 1024, 1024), (8000, 2048, 2048), (20000, 1024, 1024), (40000, 512, 768), (300, 2048, 2048)):
+        for bf16, least in ((0, 128), (1, 512)):              # rows of a unit: no fewer, but for the last multiple of 64
+            for groups in (1, 16, 64, 256):
+                need = ws(n, groups, i, o, bf16)
+                assert need <= 2 * (n // (least - 64)) * 4 * (i + 1) * o, (n, groups, i, o, bf16, need)
+                assert need <= (n // (least - 64) + groups) * 4 * (i + 1) * o
+    assert ws(20000, 256, 1024, 1024, 1) <= 64 << 20
+    assert ws(4096, 256, 1024, 1024, 1) <= 80 << 20
