@@ -2,7 +2,9 @@
 //
 // Rows, units and tiles are counted in 32 bits (kMaxGroupedRows), which the scalar unit compares by itself. The 64-bit
 // comparison of uniform numbers it has not: one that both chooses a value and branches came out of the compiler (22.0, gfx950)
-// with the choice made by an older condition, and a workgroup's way through its groups did not end.
+// with the choice made by an older condition (the branch came from a vector comparison, the choice from what a shift had left), and a
+// workgroup's way through its groups did not end. Where counts pass 32 bits (rows of one product), 64-bit ones stay; a test of every build
+// looks for that form in all of the library's kernels.
 #pragma once
 
 #include <hip/hip_runtime.h>

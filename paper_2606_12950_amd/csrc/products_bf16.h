@@ -49,6 +49,7 @@ struct Item {
 
 // A workgroup's way through `items` units of work, workgroup `block` of `blocks` (a multiple of 8). XCD x (of 8; workgroups go
 // round them) takes a contiguous share, so that the tiles that read the same rows of Q run side by side on one L2.
+// Counts of 64 bits: a product has up to 2^40 rows. The scalar unit does not compare them; a test looks at what becomes of it (groups.h).
 struct Cursor {
   int64_t i, last, step;
   __device__ __forceinline__ Cursor(int64_t items, uint32_t block, uint32_t blocks) {

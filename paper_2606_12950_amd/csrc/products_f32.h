@@ -60,6 +60,7 @@ struct Item {
 };
 
 // A workgroup's way through `items` units of work, workgroup `block` of `blocks`.
+// Counts of 64 bits, as in the bfloat16 kernel.
 struct Cursor {
   int64_t i, last, step;
   __device__ __forceinline__ Cursor(int64_t items, uint32_t block, uint32_t blocks) : i(block), last(items), step(blocks) {}
