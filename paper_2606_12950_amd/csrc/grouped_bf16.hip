@@ -173,7 +173,7 @@ maestro_status launch_layer_grouped_bf16(int64_t n, int32_t n_groups, int32_t d_
 size_t grouped_grad_bf16_workspace_bytes(int64_t n, int32_t n_groups, int32_t d_in, int32_t d_out) {
   if (n == 0) return 0;
   const Cut c = cut_of(n, n_groups, d_in, d_out);
-  return n <= c.k_split ? 0 : sizeof(float) * (size_t)(slots_of(n, n_groups, c.k_split) * ((int64_t)d_in + 1) * d_out);
+  return n <= c.k_split ? 0 : sizeof(float) * (size_t)(places_of(n, n_groups, c.k_split) * ((int64_t)d_in + 1) * d_out);
 }
 
 maestro_status launch_grouped_grad_bf16(int64_t n, int32_t n_groups, int32_t d_in, int32_t d_out, const void* x,
@@ -183,7 +183,7 @@ maestro_status launch_grouped_grad_bf16(int64_t n, int32_t n_groups, int32_t d_i
   if (n == 0) return launch_join_groups(0, n_groups, offsets, 1, true, nullptr, g_weight, size, nullptr, g_bias, d_out, stream);
   const __bf16 *xb = static_cast<const __bf16*>(x), *gz = static_cast<const __bf16*>(g_z);
   const Cut c = cut_of(n, n_groups, d_in, d_out);
-  float *gw_parts = static_cast<float*>(workspace), *gb_parts = gw_parts + slots_of(n, n_groups, c.k_split) * size;
+  float *gw_parts = static_cast<float*>(workspace), *gb_parts = gw_parts + places_of(n, n_groups, c.k_split) * size;
   const Product gx{static_cast<const __bf16*>(weight), gz, d_in, d_out, d_in, n, d_out, d_out, 1, 0, 0};
   const InputGrad x_out{xb, static_cast<__bf16*>(g_x), relu_input};
   const Product gw{xb, gz, d_in, d_out, d_in, d_out, n, c.k_split, 1, 0, 0};

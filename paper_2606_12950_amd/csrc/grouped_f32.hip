@@ -111,7 +111,7 @@ __global__ __launch_bounds__(kThreads) void join_groups_kernel(int32_t n, int32_
   const int group = blockIdx.y;
   const int units = table.first_unit(group + 1) - table.first_unit(group);
   if (units == 1) return;
-  const int first = first_slot(group, table.first_row(group) - table.first_row(0), k_split), last = first + units;
+  const int first = table.first_unit(group) - table.alone_before(group), last = first + units;
   constexpr int kQuads = kThreads / G;
   const int part = threadIdx.x / kQuads, own = threadIdx.x % kQuads;
   const int64_t quads = size / 4, all = quads + d_out / 4;
@@ -184,7 +184,7 @@ maestro_status launch_layer_grouped_f32(int64_t n, int32_t n_groups, int32_t d_i
 size_t grouped_grad_f32_workspace_bytes(int64_t n, int32_t n_groups, int32_t d_in, int32_t d_out) {
   if (n == 0) return 0;
   const Cut c = cut_of(n, d_in, d_out);
-  return n <= c.k_split ? 0 : sizeof(float) * (size_t)(slots_of(n, n_groups, c.k_split) * ((int64_t)d_in + 1) * d_out);
+  return n <= c.k_split ? 0 : sizeof(float) * (size_t)(places_of(n, n_groups, c.k_split) * ((int64_t)d_in + 1) * d_out);
 }
 
 maestro_status launch_grouped_grad_f32(int64_t n, int32_t n_groups, int32_t d_in, int32_t d_out, const float* x,
@@ -193,7 +193,7 @@ maestro_status launch_grouped_grad_f32(int64_t n, int32_t n_groups, int32_t d_in
   const int64_t size = (int64_t)d_in * d_out;
   if (n == 0) return launch_join_groups(0, n_groups, offsets, 1, true, nullptr, g_weight, size, nullptr, g_bias, d_out, stream);
   const Cut c = cut_of(n, d_in, d_out);
-  float *gw_parts = static_cast<float*>(workspace), *gb_parts = gw_parts + slots_of(n, n_groups, c.k_split) * size;
+  float *gw_parts = static_cast<float*>(workspace), *gb_parts = gw_parts + places_of(n, n_groups, c.k_split) * size;
   Product gx{{weight, d_in}, {g_z, d_out}, d_in, n, d_out, d_out, 1, 0, 0};
   const InputGrad x_out{x, g_x, relu_input};
   Product gw{{x, d_in}, {g_z, d_out}, d_in, d_out, n, c.k_split, 1, 0, 0};

@@ -33,15 +33,11 @@ inline bool weight_wide_f32(int64_t n, int64_t d_in, int64_t d_out) {
   return d_in > 64 && d_out > 64 && n >= 32768 && 5 * large <= 6 * small;
 }
 
-// The places in the workspace of the groups' weights' gradients. A group whose rows are one unit writes its gradient itself; one of u >= 2
-// units of up to `per` rows has u neighbouring places, from first_slot on. `row`, its first row, and `end`, the next group's, count from the
-// first group's: from row / per to end / per are u - 1 or more and at least one, whether units begin at the group's first row or at multiples of
-// `per`; and min(group, row / per) rises by one then, so that the next group's first place is u or more further.
-constexpr int first_slot(int group, int row, int per) {
-  const int passed = (int)((uint32_t)row / (uint32_t)per);
-  return passed + (group < passed ? group : passed);
-}
-inline int64_t slots_of(int64_t n, int64_t n_groups, int64_t per) { return first_slot((int)n_groups, (int)n, (int)per); }
+// The most places in the workspace of the groups' weights' gradients: one for every unit of up to `per` rows of the groups that have two units
+// or more (the others write their gradient themselves). From such a group's first row to the next group's are u - 1 multiples of `per` or more,
+// and at least one, whether units begin at the group's first row or at multiples of `per`; so the groups' u are as many as the multiples
+// up to n, and one more for each of these groups, which are no more than the groups, nor than the multiples.
+inline int64_t places_of(int64_t n, int64_t n_groups, int64_t per) { return n / per + (n_groups < n / per ? n_groups : n / per); }
 
 namespace grouped_bf16 {
 

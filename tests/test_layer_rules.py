@@ -61,7 +61,7 @@ static S quantised(int64_t n, int64_t i, int64_t o) {
   const auto t = int8::product_tile(o, n);
   return "rows" + text(l.units) + " y" + tile(t.tile, t.wavefronts);
 }
-extern "C" int64_t place(int64_t group, int64_t row, int64_t per) { return first_slot((int)group, (int)row, (int)per); }
+extern "C" int64_t places(int64_t n, int64_t groups, int64_t per) { return places_of(n, groups, per); }
 extern "C" void form(int op, int64_t n, int64_t groups, int64_t i, int64_t o, int bf16, int x, char* out, size_t size) {
   const S s = op == 0 ? grouped(n, groups, i, o, bf16, x) : op == 1 ? packed(n, i, o, bf16, x) : quantised(n, i, o);
   s.copy(out, size - 1);
@@ -141,23 +141,20 @@ def test_forms_that_no_size_chooses(forms):
 
 @pytest.mark.parametrize("by_group", [False, True])
 def test_places_of_shares(rules, by_group):
-    """No two units of the groups that have two or more share a place, and all lie below the count that sizes the workspace."""
-    rules.place.argtypes, rules.place.restype = [ctypes.c_int64] * 3, ctypes.c_int64
+    """The workspace has a place for every unit of the groups that have two or more, whatever the groups' sizes, and not twice as many."""
+    rules.places.argtypes, rules.places.restype = [ctypes.c_int64] * 3, ctypes.c_int64
     r = random.Random(3)
-    for _ in range(3000):
+    for _ in range(20000):
         groups, per = r.choice([1, 2, 3, 8, 40, 256]), r.choice([1, 2, 5, 64])
-        sizes = [r.choice([0, 1, per - 1, per, per + 1, 2 * per, 2 * per + 1, r.randint(0, 7 * per)]) for _ in range(groups)]
+        few = r.random() < 0.5
+        sizes = [r.choice([0, 1, per - 1, per, per + 1, 2 * per, 2 * per + 1, r.randint(0, 7 * per)] if few else [per + 1, 2, 2 * per]) for _ in range(groups)]
         n = sum(sizes) + r.choice([0, 0, 1, per])                  # rows of no group
-        taken, row = set(), 0
-        for g, size in enumerate(sizes):
-            units = -(-size // per) if by_group else ((row + size - 1) // per - row // per + 1 if size else 0)
-            if units > 1:
-                first = rules.place(g, row, per)
-                assert first >= 0 and not taken & set(range(first, first + units)), (sizes, per, g)
-                taken |= set(range(first, first + units))
-            row += size
-        assert max(taken, default=-1) < rules.place(groups, n, per), (sizes, per)
-        assert rules.place(groups, n, per) <= min(2 * (n // per), n // per + groups)
+        shared, at = 0, 0
+        for size in sizes:
+            units = -(-size // per) if by_group else ((at + size - 1) // per - at // per + 1 if size else 0)
+            shared += units if units > 1 else 0
+            at += size
+        assert shared <= rules.places(n, groups, per) <= min(2 * (n // per), n // per + groups), (sizes, per)
 
 
 def test_workspace_of_many_groups():
