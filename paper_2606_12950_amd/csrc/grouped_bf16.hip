@@ -33,9 +33,9 @@ struct GroupedRows : GroupedRowsWay<8> {
   }
 };
 
-template <int TP, int TQ, int kDepth, GroupUnits kUnits>
-struct GroupedSums : GroupedSumsWay<8, kUnits> {
-  using Way = typename GroupedSumsWay<8, kUnits>::Way;
+template <int TP, int TQ, int kDepth, GroupUnits kUnits, bool kShared>
+struct GroupedSums : GroupedSumsWay<8, kUnits, kShared> {
+  using Way = typename GroupedSumsWay<8, kUnits, kShared>::Way;
   const Product& g;
   __device__ __forceinline__ Item item(const Way& c) const {
     const auto at = this->place(c);
@@ -80,7 +80,7 @@ __global__ __launch_bounds__(64 * kWaves, (Tile<WP, WQ, kDepth, kBufs, Out, kWav
 }
 
 // alone: no group has more than one unit, and no second launch follows.
-template <int WP, int WQ, int kDepth, int kBufs, int kWaves, GroupUnits kUnits>
+template <int WP, int WQ, int kDepth, int kBufs, int kWaves, GroupUnits kUnits, bool kShared>
 __global__ __launch_bounds__(64 * kWaves, (Tile<WP, WQ, kDepth, kBufs, GroupedWeightGrad, kWaves>::kSimdWaves)) void sums_kernel(
     Product g, GroupedWeightGrad out, const int64_t* offsets, int32_t n_groups, int32_t n, bool alone) {
   using L = Tile<WP, WQ, kDepth, kBufs, GroupedWeightGrad, kWaves>;
@@ -88,12 +88,13 @@ __global__ __launch_bounds__(64 * kWaves, (Tile<WP, WQ, kDepth, kBufs, GroupedWe
   GroupTable table;
   table.build<kUnits>(offsets, n_groups, n, (int)g.k_split);
   const int tiles = (int)((g.nq + L::TQ - 1) / L::TQ) * g.p_tiles;
-  product<WP, WQ, kDepth, kBufs, true, true, kWaves>(g, out, GroupedSums<L::TP, L::TQ, kDepth, kUnits>{{table, tiles, (int)g.k_split}, g}, lds, blockIdx.x,
+  product<WP, WQ, kDepth, kBufs, true, true, kWaves>(g, out, GroupedSums<L::TP, L::TQ, kDepth, kUnits, kShared>{{table, tiles, (int)g.k_split}, g}, lds, blockIdx.x,
                                                 gridDim.x);
   if (alone) clear_empty_groups(table, out.gw, g.np * g.nq, out.gb, (int)g.nq, blockIdx.x, gridDim.x);
 }
 
 // Both gradients in one launch, in 64 x 64 tiles: the first `blocks` workgroups make the input's, the others the weights'.
+template <bool kShared>
 __global__ __launch_bounds__(kThreads, 4) void pair_kernel(Product gx, InputGrad x, uint32_t blocks, Product gw, GroupedWeightGrad w,
                                                            const int64_t* offsets, int32_t n_groups, int32_t n, bool alone) {
   using X = Tile<1, 1, 64, 2, InputGrad>;
@@ -107,7 +108,7 @@ __global__ __launch_bounds__(kThreads, 4) void pair_kernel(Product gx, InputGrad
   }
   table.build<kTiles>(offsets, n_groups, n, (int)gw.k_split);
   const int tiles = (int)((gw.nq + W::TQ - 1) / W::TQ) * gw.p_tiles;
-  product<1, 1, 64, 2, true, true>(gw, w, GroupedSums<W::TP, W::TQ, 64, kTiles>{{table, tiles, (int)gw.k_split}, gw}, lds,
+  product<1, 1, 64, 2, true, true>(gw, w, GroupedSums<W::TP, W::TQ, 64, kTiles, kShared>{{table, tiles, (int)gw.k_split}, gw}, lds,
                                    blockIdx.x - blocks, gridDim.x - blocks);
   if (alone) clear_empty_groups(table, w.gw, gw.np * gw.nq, w.gb, (int)gw.nq, blockIdx.x - blocks, gridDim.x - blocks);
 }
@@ -145,9 +146,13 @@ void launch_sums(Product g, const GroupedWeightGrad& out, const int64_t* offsets
   g.p_tiles = (int32_t)cdiv(g.np, L::TP);
   const int64_t pieces = by_group ? n / g.k_split + n_groups : cdiv(n, g.k_split);
   const uint32_t blocks = blocks_of(pieces * g.p_tiles * cdiv(g.nq, L::TQ), L::kResident);
-  auto kernel = sums_kernel<WP, WQ, kDepth, kBufs, kWaves, kShares>;
-  if constexpr (WP * WQ < 8)                                // 256 x 256 tiles: from 131,072 rows on, never by group
-    if (by_group) kernel = sums_kernel<WP, WQ, kDepth, kBufs, kWaves, kTiles>;
+  auto of = [&](auto shared) {
+    constexpr bool kShared = decltype(shared)::value;
+    if constexpr (WP * WQ == 1) return sums_kernel<WP, WQ, kDepth, kBufs, kWaves, kTiles, kShared>;          // always by group
+    else if constexpr (WP * WQ == 8) return sums_kernel<WP, WQ, kDepth, kBufs, kWaves, kShares, kShared>;    // 131,072 rows and more: never
+    else return by_group ? sums_kernel<WP, WQ, kDepth, kBufs, kWaves, kTiles, kShared> : sums_kernel<WP, WQ, kDepth, kBufs, kWaves, kShares, kShared>;
+  };
+  auto kernel = shared_places(n, n_groups, g.k_split) ? of(std::true_type{}) : of(std::false_type{});
   kernel<<<blocks, 64 * kWaves, 0, stream>>>(g, out, offsets, n_groups, n, alone);
 }
 
@@ -157,7 +162,8 @@ void launch_pair(Product gx, const InputGrad& x, Product gw, const GroupedWeight
   gw.p_tiles = (int32_t)cdiv(gw.np, 64);
   const uint32_t blocks = blocks_of((n / 64 + n_groups) * gx.p_tiles, 4);
   const uint32_t more = blocks_of((n / gw.k_split + n_groups) * gw.p_tiles * cdiv(gw.nq, 64), 4);
-  pair_kernel<<<blocks + more, kThreads, 0, stream>>>(gx, x, blocks, gw, w, offsets, n_groups, n, alone);
+  auto kernel = shared_places(n, n_groups, gw.k_split) ? pair_kernel<true> : pair_kernel<false>;
+  kernel<<<blocks + more, kThreads, 0, stream>>>(gx, x, blocks, gw, w, offsets, n_groups, n, alone);
 }
 
 }  // namespace

@@ -30,9 +30,9 @@ struct GroupedRows : GroupedRowsWay<1> {
   }
 };
 
-template <int T, GroupUnits kUnits>
-struct GroupedSums : GroupedSumsWay<1, kUnits> {
-  using Way = typename GroupedSumsWay<1, kUnits>::Way;
+template <int T, GroupUnits kUnits, bool kShared>
+struct GroupedSums : GroupedSumsWay<1, kUnits, kShared> {
+  using Way = typename GroupedSumsWay<1, kUnits, kShared>::Way;
   const Product& g;
   __device__ __forceinline__ Item item(const Way& c) const {
     const auto at = this->place(c);
@@ -71,18 +71,19 @@ __global__ __launch_bounds__(kThreads, 2) void rows_kernel(Product g, Out out, c
 }
 
 // alone: no group has more than one unit, and no second launch follows.
-template <int W, GroupUnits kUnits>
+template <int W, GroupUnits kUnits, bool kShared>
 __global__ __launch_bounds__(kThreads, 2) void sums_kernel(Product g, GroupedWeightGrad out, const int64_t* offsets, int32_t n_groups,
                                                            int32_t n, bool alone) {
   __shared__ __attribute__((aligned(16))) Lds<W> lds;
   GroupTable table;
   table.build<kUnits>(offsets, n_groups, n, (int)g.k_split);
   const int tiles = (int)((g.nq + 64 * W - 1) / (64 * W) * g.p_tiles);
-  product<W, true, true>(g, out, GroupedSums<64 * W, kUnits>{{table, tiles, (int)g.k_split}, g}, lds, blockIdx.x, gridDim.x);
+  product<W, true, true>(g, out, GroupedSums<64 * W, kUnits, kShared>{{table, tiles, (int)g.k_split}, g}, lds, blockIdx.x, gridDim.x);
   if (alone) clear_empty_groups(table, out.gw, g.np * g.nq, out.gb, (int)g.nq, blockIdx.x, gridDim.x);
 }
 
 // Both gradients in one launch, in 64 x 64 tiles: the first `blocks` workgroups make the input's, the others the weights'.
+template <bool kShared>
 __global__ __launch_bounds__(kThreads, 2) void pair_kernel(Product gx, InputGrad x, uint32_t blocks, Product gw, GroupedWeightGrad w,
                                                            const int64_t* offsets, int32_t n_groups, int32_t n, bool alone) {
   __shared__ __attribute__((aligned(16))) Lds<1> lds;
@@ -94,7 +95,7 @@ __global__ __launch_bounds__(kThreads, 2) void pair_kernel(Product gx, InputGrad
   }
   table.build<kTiles>(offsets, n_groups, n, (int)gw.k_split);
   const int tiles = (int)((gw.nq + 63) / 64 * gw.p_tiles);
-  product<1, true, true>(gw, w, GroupedSums<64, kTiles>{{table, tiles, (int)gw.k_split}, gw}, lds, blockIdx.x - blocks,
+  product<1, true, true>(gw, w, GroupedSums<64, kTiles, kShared>{{table, tiles, (int)gw.k_split}, gw}, lds, blockIdx.x - blocks,
                          gridDim.x - blocks);
   if (alone) clear_empty_groups(table, w.gw, gw.np * gw.nq, w.gb, (int)gw.nq, blockIdx.x - blocks, gridDim.x - blocks);
 }
@@ -102,16 +103,19 @@ __global__ __launch_bounds__(kThreads, 2) void pair_kernel(Product gx, InputGrad
 // Group blockIdx.y's units added in a fixed order; zeros where it has none. A quad of values to each of 256 / G neighbouring threads,
 // its units dealt out over G groups of them. G = 16 where there are few values, else 1. Measured (us, weights' gradient, G = 1 / 16): float32 100,000 x 64 ->
 // 64 in 4 groups 36.9 / 22.8, 22,266 x 64 -> 80 in 2 21.3 / 16.9, bfloat16 60,000 x 64 -> 64 in 3 16.9 / 13.6; 31,065 x 384 -> 48 in 8 15.4 / 16.5.
-template <GroupUnits kUnits, int G>
+template <GroupUnits kUnits, bool kShared, int G>
 __global__ __launch_bounds__(kThreads) void join_groups_kernel(int32_t n, int32_t n_groups, const int64_t* offsets, int32_t k_split,
                                                                const float* gw_parts, float* gw, int64_t size,
                                                                const float* gb_parts, float* gb, int32_t d_out) {
   GroupTable table;
   table.build<kUnits>(offsets, n_groups, n, k_split);
   const int group = blockIdx.y;
-  const int units = table.first_unit(group + 1) - table.first_unit(group);
-  if (units == 1) return;
-  const int first = table.first_unit(group) - table.alone_before(group), last = first + units;
+  int first = table.first_unit(group), last = table.first_unit(group + 1);
+  if (last - first == 1) return;
+  if (kShared && last > first) {
+    const int place = first_place(group, table.first_row(group) - table.first_row(0), k_split);
+    last += place - first, first = place;
+  }
   constexpr int kQuads = kThreads / G;
   const int part = threadIdx.x / kQuads, own = threadIdx.x % kQuads;
   const int64_t quads = size / 4, all = quads + d_out / 4;
@@ -165,7 +169,9 @@ void launch_sums(Product g, const GroupedWeightGrad& out, const int64_t* offsets
   g.p_tiles = cdiv(g.np, 64 * W);
   const int64_t pieces = by_group ? n / g.k_split + n_groups : cdiv(n, g.k_split);
   const int64_t most = pieces * g.p_tiles * cdiv(g.nq, 64 * W);
-  auto kernel = by_group ? sums_kernel<W, kTiles> : sums_kernel<W, kShares>;
+  const bool shared = shared_places(n, n_groups, g.k_split);
+  auto kernel = by_group ? shared ? sums_kernel<W, kTiles, true> : sums_kernel<W, kTiles, false>
+                         : shared ? sums_kernel<W, kShares, true> : sums_kernel<W, kShares, false>;
   kernel<<<(unsigned)(most < 65536 ? most : 65536), kThreads, 0, stream>>>(g, out, offsets, n_groups, n, alone);
 }
 
@@ -204,7 +210,8 @@ maestro_status launch_grouped_grad_f32(int64_t n, int32_t n_groups, int32_t d_in
     gw.p_tiles = cdiv(d_in, 64);
     const int64_t rows = (n / 64 + n_groups) * gx.p_tiles, sums = (n / c.k_split + n_groups) * gw.p_tiles * cdiv(d_out, 64);
     const uint32_t blocks = (uint32_t)(rows < 65536 ? rows : 65536), more = (uint32_t)(sums < 65536 ? sums : 65536);
-    pair_kernel<<<blocks + more, kThreads, 0, stream>>>(gx, x_out, blocks, gw, out, offsets, n_groups, (int32_t)n, alone);
+    auto kernel = shared_places(n, n_groups, c.k_split) ? pair_kernel<true> : pair_kernel<false>;
+    kernel<<<blocks + more, kThreads, 0, stream>>>(gx, x_out, blocks, gw, out, offsets, n_groups, (int32_t)n, alone);
   } else {
     if (g_x && wide(d_in, n)) launch_rows<2, true>(gx, x_out, offsets, n_groups, n, stream);
     else if (g_x) launch_rows<1, true>(gx, x_out, offsets, n_groups, n, stream);
@@ -221,8 +228,12 @@ maestro_status launch_join_groups(int64_t n, int32_t n_groups, const int64_t* of
   const int64_t quads = size / 4 + d_out / 4;
   const bool dealt = join_dealt(n, n_groups, k_split, size, d_out);
   const int64_t blocks = cdiv(quads, dealt ? kThreads / 16 : kThreads);
-  auto kernel = dealt ? by_group ? join_groups_kernel<kTiles, 16> : join_groups_kernel<kShares, 16>
-                      : by_group ? join_groups_kernel<kTiles, 1> : join_groups_kernel<kShares, 1>;
+  auto of = [&](auto shared) {
+    constexpr bool kShared = decltype(shared)::value;
+    return dealt ? by_group ? join_groups_kernel<kTiles, kShared, 16> : join_groups_kernel<kShares, kShared, 16>
+                 : by_group ? join_groups_kernel<kTiles, kShared, 1> : join_groups_kernel<kShares, kShared, 1>;
+  };
+  auto kernel = shared_places(n, n_groups, k_split) ? of(std::true_type{}) : of(std::false_type{});
   kernel<<<dim3((unsigned)(blocks < 4096 ? blocks : 4096), (unsigned)n_groups), kThreads, 0, stream>>>(
       (int32_t)n, n_groups, offsets, (int32_t)k_split, gw_parts, gw, size, gb_parts, gb, d_out);
   return launch_status();

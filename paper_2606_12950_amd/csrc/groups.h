@@ -30,7 +30,7 @@ enum GroupUnits { kTiles, kShares };
 // second workgroup of a CU, and a look-up is a ballot or a lane's read. All of a wavefront's lanes take part in every call.
 struct GroupTable {
   static constexpr int kSets = MAESTRO_MAX_LAYER_GROUPS / 64;
-  int row_end[kSets], unit_end[kSets], alone[kSets];        // of group 64 s + lane; alone: groups of one unit before it
+  int row_end[kSets], unit_end[kSets];                      // of group 64 s + lane
   int base, n_groups;
 
   // Whatever the offsets hold, rows are 0 <= first_row(0) <= first_row(1) <= ... <= n.
@@ -40,10 +40,10 @@ struct GroupTable {
     auto clamp = [&](int64_t v) { return v < 0 ? 0 : v > n ? n : (int)v; };
     n_groups = groups;
     base = uniform(clamp(offsets[0]));
-    int before = base, units = 0, single = 0;               // the last row and unit so far, and groups of one unit
+    int before = base, units = 0;                           // the last row and unit so far
 #pragma unroll
     for (int s = 0; s < kSets; ++s) {
-      row_end[s] = unit_end[s] = alone[s] = 0;
+      row_end[s] = unit_end[s] = 0;
       if (64 * s >= n_groups) continue;
       const int g = 64 * s + lane;
       int end = g < n_groups ? clamp(offsets[g + 1]) : 0;
@@ -57,9 +57,6 @@ struct GroupTable {
       if (lane == 0) start = before;
       int sum = end == start ? 0 : kUnits == kTiles ? quotient(end - start - 1, per) + 1
                                                     : quotient(end - 1 - base, per) - quotient(start - base, per) + 1;
-      const uint64_t ones = __ballot(sum == 1);
-      alone[s] = single + __builtin_amdgcn_mbcnt_hi((uint32_t)(ones >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)ones, 0));
-      single += __popcll(ones);
 #pragma unroll
       for (int d = 1; d < 64; d <<= 1) {
         const int other = __shfl_up(sum, d);
@@ -86,8 +83,6 @@ struct GroupTable {
   // of groups 0 .. n_groups: the last one's is where all end
   __device__ __forceinline__ int first_row(int g) const { return g == 0 ? base : of_group(row_end, g - 1); }
   __device__ __forceinline__ int first_unit(int g) const { return g == 0 ? 0 : of_group(unit_end, g - 1); }
-  // A group of one unit writes its gradient; the units of the others have places in the workspace, one after the other.
-  __device__ __forceinline__ int alone_before(int g) const { return of_group(alone, g); }
   static __device__ __forceinline__ int of_group(const int (&ends)[kSets], int g) {
     int v = __builtin_amdgcn_readlane(ends[0], g & 63);
 #pragma unroll
@@ -132,7 +127,8 @@ struct GroupedRowsWay {
 
 // Tiles of a group's weights' gradient over its units of rows. kShares: `per` rows of all groups together are one piece of work
 // for every tile, which a workgroup takes group after group. kTiles: a group's unit is one, so that small groups run side by side.
-template <int kXcds, GroupUnits kUnits>
+// kShared: only units of groups of two or more have places in the workspace (shared_places).
+template <int kXcds, GroupUnits kUnits, bool kShared>
 struct GroupedSumsWay {
   struct Way : GroupedCursor<kXcds> {
     int row, end;                    // kShares: the first row of the group's part, and the piece's last
@@ -173,32 +169,23 @@ struct GroupedSumsWay {
     const bool direct = table.first_unit(g + 1) - first == 1;
     if constexpr (kUnits == kTiles) {
       const int k0 = row + (piece - first) * per;
-      return Place{g, tile, piece - table.alone_before(g), k0, group_end - k0 < per ? group_end : k0 + per, direct};
+      const int slot = !kShared ? piece : direct ? 0 : first_place(g, row - table.first_row(0), per) + piece - first;
+      return Place{g, tile, slot, k0, group_end - k0 < per ? group_end : k0 + per, direct};
     }
-    const int unit = first + piece - quotient(row - table.first_row(0), per);
-    return Place{g, tile, unit - table.alone_before(g), c.row, group_end < c.end ? group_end : c.end, direct};
+    const int from = !kShared ? first : direct ? 0 : first_place(g, row - table.first_row(0), per);
+    return Place{g, tile, from + piece - quotient(row - table.first_row(0), per), c.row, group_end < c.end ? group_end : c.end, direct};
   }
 };
 
-// Zeros for the groups without rows, by `blocks` workgroups. The groups are found a set of lanes at a time: looked up one by one, 36 empty groups of 55
-// (27 rows, 16 -> 64 bfloat16) took 5 of 13.9 us.
+// Zeros for the groups without rows, by `blocks` workgroups.
 __device__ __forceinline__ void clear_empty_groups(const GroupTable& table, float* gw, int64_t size, float* gb, int d_out,
                                                    uint32_t block, uint32_t blocks) {
   const int64_t quads = size / 4, all = quads + d_out / 4;
-  const int lane = threadIdx.x & 63;
-  int before = 0;                                           // the units of the groups so far
-#pragma unroll
-  for (int s = 0; s < GroupTable::kSets; ++s) {
-    if (64 * s >= table.n_groups) continue;
-    int first = __shfl_up(table.unit_end[s], 1);
-    if (lane == 0) first = before;
-    before = __builtin_amdgcn_readlane(table.unit_end[s], 63);
-    for (uint64_t left = __ballot(64 * s + lane < table.n_groups && table.unit_end[s] == first); left; left &= left - 1) {
-      const int64_t g = 64 * s + __builtin_ctzll(left);
-      for (int64_t i = (int64_t)block * blockDim.x + threadIdx.x; i < all; i += (int64_t)blocks * blockDim.x)
-        (i < quads ? reinterpret_cast<float4*>(gw) + g * quads + i : reinterpret_cast<float4*>(gb) + g * (all - quads) + (i - quads))[0] =
-            make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    }
+  for (int g = 0; g < table.n_groups; ++g) {
+    if (table.first_unit(g + 1) != table.first_unit(g)) continue;
+    for (int64_t i = (int64_t)block * blockDim.x + threadIdx.x; i < all; i += (int64_t)blocks * blockDim.x)
+      (i < quads ? reinterpret_cast<float4*>(gw) + g * quads + i : reinterpret_cast<float4*>(gb) + g * (all - quads) + (i - quads))[0] =
+          make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   }
 }
 

@@ -23,6 +23,10 @@ GROUPED = [
     (spread(33_717, 46, 2_000), 80, 80),                      # large float32 tiles by group
     (spread(72_830, 83, 9_000), 208, 80), (spread(40_000, 3, 39_000), 1024, 1040),
     (spread(530_001, 5, 100_000), 32, 64),                    # many shares of few values
+    # many groups beside what the units' rows go into all of them: only groups of two units or more have places in the workspace
+    (spread(10_007, 100, 4_000), 160, 1040), (spread(2_400, 60, 1_500), 16, 32), (spread(9_300, 78, 7_000), 32, 16),
+    (spread(131_100, 16, 90_000), 2064, 2064), (spread(10_110, 203, 4_000), 352, 48), (spread(17_000, 100, 9_000), 4096, 48),
+    ([1_000, 1_500, 7] * 60, 1024, 1024), ([0, 3, 600, 1] * 64, 512, 512), ([1] * 200 + [2_600] * 2 + [0] * 54, 64, 256),
     ([2_000, 2_608], 16, 16), (spread(140_000, 30, 60_000), 16, 16),
 ]
 # n, d_in, d_out
