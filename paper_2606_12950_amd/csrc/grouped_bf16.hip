@@ -1,8 +1,9 @@
 // The bfloat16 products (products_bf16.h) of a grouped layer and its gradients.
 //
 // Rows of a group make tiles of their own, each against the group's weights; workgroups are persistent and find a tile's group
-// in a table of the groups' rows that each wavefront builds. The weights' gradients cut every group's rows into shares of
-// k_split; a group of one share writes its gradient, of more its shares, which a second launch adds in order.
+// in a table of the groups' rows that each wavefront builds. The weights' gradients cut the rows of all groups together into shares of
+// k_split, which a workgroup takes group after group, or, where rows are few, every group's by itself into units of k_split; a group of one
+// part writes its gradient, of more its parts, which a second launch adds in order.
 #include "groups.h"
 #include "layers.h"
 #include "products_bf16.h"

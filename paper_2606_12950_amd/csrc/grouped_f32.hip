@@ -1,7 +1,8 @@
 // The float32 products (products_f32.h) of a grouped layer and its gradients, and the join of a group's shares.
 //
-// Rows of a group make tiles of their own, each against the group's weights. The weights' gradients cut every group's
-// rows into shares of k_split; a group of one share writes its gradient, of more its shares, which a second launch adds in order.
+// Rows of a group make tiles of their own, each against the group's weights. The weights' gradients cut the rows of all groups together
+// into shares of k_split, or, where rows are few, every group's by itself into units of k_split; a group of one part writes its gradient, of
+// more its parts, which a second launch adds in order.
 #include "groups.h"
 #include "layers.h"
 #include "products_f32.h"

@@ -612,7 +612,8 @@ struct Tile {
   static constexpr int kBiasBytes = 2 * kWaves * 256 * kEpilogueLoads;             // two places for each wavefront
   static constexpr int kBytes = kBufs * kStage + (kStores ? kWaves * Staging<WP, kWaves>::kBytes : 0) + kBiasBytes;
   // workgroups of a CU that a launch plans for, and that registers allow. LDS lets three run of the activations' 64 x 64
-  // (43,008 bytes of 160 KB) and two of pair_kernel<4, 1> (81,920, the larger tile's, in all of them).
+  // (43,008 bytes of 160 KB, with scales for 8-bit products 45,056: the fourth's start when others end) and two of pair_kernel<4, 1>
+  // (81,920, the larger tile's, in all of them).
   static constexpr int kBlocks = WP * WQ * kWaves / 4;      // of 32 x 32, a SIMD's
   static constexpr int kResident = kBlocks > 8 ? 1 : kBlocks > 2 ? 2 : 4;
   static constexpr int kSimdWaves = kResident * kWaves / 4;
