@@ -171,8 +171,9 @@ void launch_sums(Product g, const GroupedWeightGrad& out, const int64_t* offsets
   const int64_t pieces = by_group ? n / g.k_split + n_groups : cdiv(n, g.k_split);
   const int64_t most = pieces * g.p_tiles * cdiv(g.nq, 64 * W);
   const bool shared = shared_places(n, n_groups, g.k_split);
-  auto kernel = by_group ? shared ? sums_kernel<W, kTiles, true> : sums_kernel<W, kTiles, false>
-                         : shared ? sums_kernel<W, kShares, true> : sums_kernel<W, kShares, false>;
+  auto kernel = by_group ? sums_kernel<W, kTiles, false> : shared ? sums_kernel<W, kShares, true> : sums_kernel<W, kShares, false>;
+  if constexpr (W == 1)                                     // large tiles by group: units by the hundred, more than half the groups
+    if (by_group && shared) kernel = sums_kernel<W, kTiles, true>;
   kernel<<<(unsigned)(most < 65536 ? most : 65536), kThreads, 0, stream>>>(g, out, offsets, n_groups, n, alone);
 }
 
@@ -231,7 +232,8 @@ maestro_status launch_join_groups(int64_t n, int32_t n_groups, const int64_t* of
   const int64_t blocks = cdiv(quads, dealt ? kThreads / 16 : kThreads);
   auto of = [&](auto shared) {
     constexpr bool kShared = decltype(shared)::value;
-    return dealt ? by_group ? join_groups_kernel<kTiles, kShared, 16> : join_groups_kernel<kShares, kShared, 16>
+    // few values by shares: units by the hundred, more than half the groups
+    return dealt ? by_group ? join_groups_kernel<kTiles, kShared, 16> : join_groups_kernel<kShares, false, 16>
                  : by_group ? join_groups_kernel<kTiles, kShared, 1> : join_groups_kernel<kShares, kShared, 1>;
   };
   auto kernel = shared_places(n, n_groups, k_split) ? of(std::true_type{}) : of(std::false_type{});

@@ -127,14 +127,18 @@ def test_every_form_is_tested(forms, op, bf16):
 
 def test_forms_that_no_size_chooses(forms):
     """The launchers have no kernel for these: bfloat16 gradients of kept bytes in one launch beside 256-wide tiles of the weights', and
-    256 x 256 tiles of the groups' weights' gradient by group, 64 x 64 ones by shares."""
+    256 x 256 tiles of the groups' weights' gradient by group, 64 x 64 ones by shares; nor,
+    where only groups of two units have places, 128 x 128 float32 ones by group and a join of few values' shares."""
     r = random.Random(7)
     span = lambda low, most: int(round(low * (most / low) ** r.random()))
     for _ in range(60000):
         n, i, o = span(1, 1 << 28), 16 * span(1, 1024), 16 * span(1, 1024)
         narrow = 16 * r.randint(1, 4)                         # 256 x 64 tiles' outputs
         assert not {f for f in (*forms(1, n, 1, i, o, 1, 1), *forms(1, n, 1, i, narrow, 1, 1)) if f.startswith("pair256")}, (n, i, o, narrow)
-        assert not {f for f in forms(0, n, span(1, 256), i, o, 1, 0) if f.startswith(("gw256x256g", "gw64x64s"))}, (n, i, o)
+        groups, few = span(1, 256), 16 * span(1, 16)
+        none = ("gw256x256g", "gw64x64s", "gw128g+", "joins+16")
+        for bf16 in (0, 1):
+            assert not {f for f in (*forms(0, n, groups, i, o, bf16, 0), *forms(0, n, 256, few, narrow, bf16, 0)) if f.startswith(none)}, (n, groups, i, o)
     # at the edges of both rules: the least rows that leave a 64-wide tile, and the most that stay in one
     for i in range(144, 16385, 16):
         for o in (16, 48, 64):
